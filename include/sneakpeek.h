@@ -410,6 +410,90 @@ sp_status sp_debug_mfma_rate(int device_id, int32_t random_bits, int32_t idle, i
  */
 sp_status sp_debug_copy_rate(int device_id, int64_t bytes, void* stream, double* gbs_out);
 
+/*
+ * Operators that train the heads.
+ *
+ * sp_create takes heads that are trained already.  What follows fits all applications' heads together on the GPU that serves
+ * them, from labelled feature rows: rows are sorted by application, application g owns rows offsets[g] .. offsets[g + 1] - 1,
+ * and one call takes all of them: layer norm of the features, linear layers with every application's own weights, the softmax
+ * loss with the gradient of the logits (the posterior of Def. 4.1.1 against the label), the layers' gradients, and the norm of
+ * all gradients with clipping.  The first two serve as well: features and hidden layers of a single request up to a whole window.
+ *
+ * An sp_ops holds what the calls need besides the caller's arrays: a workspace of device memory and a word in which kernels
+ * note bad data.  Calls are enqueued on `stream` and return without waiting, allocate nothing, record no memory operation
+ * other than kernels (they may be captured into a graph), and keep nothing of one call for the next.  Calls that share an
+ * sp_ops must not overlap on the device: one stream at a time, as for a context.  Results depend on the inputs alone, bit for
+ * bit, not on timing.  All arrays are DEVICE arrays unless said otherwise; elements lie at multiples of their own size (4 or 2
+ * bytes), rows of a matrix are contiguous and `*_stride` elements apart (at least the row's length).  Outputs must not overlap
+ * inputs or each other unless said otherwise.  Types are sp_dtype; sums, statistics, losses, biases and weight gradients are
+ * float32 or wider; an output of fewer bits is rounded once, to the nearest.
+ */
+typedef struct sp_ops sp_ops;
+typedef enum { SP_ACT_NONE = 0, SP_ACT_RELU = 1 } sp_activation;
+
+/* Limits (SP_ECAPACITY beyond them). */
+#define SP_OPS_MIN_WORKSPACE 1048576      /* bytes                                */
+#define SP_MAX_NORM_DIM 16384             /* columns of a normalised row          */
+#define SP_MAX_LINEAR_DIM 1048576         /* inputs and outputs of a layer        */
+
+/* workspace_bytes >= SP_OPS_MIN_WORKSPACE: more of it lets long sums (weight gradients of many rows) be split over more of the
+ * device; 64 MiB serve every size that was measured.  SP_EINVAL: less, or out NULL. */
+sp_status sp_ops_create(int device_id, int64_t workspace_bytes, sp_ops** out);
+void sp_ops_destroy(sp_ops* ops);
+/* Waits for the stream.  SP_EINVAL if a call on these ops since the last check (or since sp_ops_create) met bad data:
+ * offsets that do not rise from 0 to at most n, an application id, class count or label out of range.  Such data is never
+ * followed out of the arrays; results of the rows concerned are unspecified (sp_cross_entropy: 0). */
+sp_status sp_ops_check(sp_ops* ops, void* stream);
+const char* sp_ops_last_hip_error(const sp_ops* ops);
+
+/* y = (x - mean) * rstd * gamma + beta per row, mean over its d columns, rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
+ *   x, y [n, d] dtype (y may be x)     gamma, beta [d] float or NULL (1, 0)     mean_out, rstd_out [n] float or NULL */
+sp_status sp_layer_norm(sp_ops* ops, int32_t n, int32_t d, int32_t dtype, const void* x, int64_t x_stride, const float* gamma,
+                        const float* beta, float eps, void* y, int64_t y_stride, float* mean_out, float* rstd_out, void* stream);
+/* Gradients of the above from dy and the statistics it handed out.  dx [n, d] dtype or NULL (may be dy or x); dgamma, dbeta [d]
+ * float or NULL, each the sum over all rows (0 for n == 0). */
+sp_status sp_layer_norm_backward(sp_ops* ops, int32_t n, int32_t d, int32_t dtype, const void* dy, int64_t dy_stride, const void* x,
+                                 int64_t x_stride, const float* gamma, const float* mean, const float* rstd, void* dx, int64_t dx_stride,
+                                 float* dgamma, float* dbeta, void* stream);
+
+/* y_i = act(x_i W_g + b_g) + residual_i for every row i of every group g.
+ *   x [n, k] dtype       w [groups, k, m] dtype, contiguous       bias [groups, m] float or NULL
+ *   offsets int32 [groups + 1], 0 = offsets[0] <= ... <= offsets[groups] <= n; groups may be empty; rows from offsets[groups]
+ *     on belong to no group and get y = 0
+ *   y [n, m] out_dtype (dtype, or SP_F32 from SP_BF16); residual [n, m] out_dtype or NULL (may be y)
+ *   act_out [n, m] out_dtype or NULL: act(x_i W_g + b_g) without the residual, which the backward pass of a layer with both an
+ *     activation and a residual asks for */
+sp_status sp_grouped_linear(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype, const void* x, int64_t x_stride,
+                            const int32_t* offsets, const void* w, const float* bias, int32_t activation, int32_t out_dtype,
+                            const void* residual, int64_t residual_stride, void* y, int64_t y_stride, void* act_out, int64_t act_stride,
+                            void* stream);
+/* With dz_i = dy_i where act_i > 0, else 0 (act NULL: dz = dy):
+ *   dx_i = dz_i W_g^T      dw_g = sum over the group's rows of x_i^T dz_i      db_g = sum of dz_i
+ *   dy [n, m] dtype; act [n, m] dtype or NULL: the layer's y (or act_out, if it has a residual), for SP_ACT_RELU
+ *   dx [n, k] dtype or NULL (0 for rows of no group); dw [groups, k, m] float or NULL; db [groups, m] float or NULL (0 for empty
+ *     groups).  x is read for dw only, w for dx only (either may be NULL otherwise).  The residual's gradient is dy itself. */
+sp_status sp_grouped_linear_backward(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype, const void* dy,
+                                     int64_t dy_stride, const void* act, int64_t act_stride, const void* x, int64_t x_stride,
+                                     const int32_t* offsets, const void* w, void* dx, int64_t dx_stride, float* dw, float* db,
+                                     void* stream);
+
+/* loss_i = weight_i (log sum_{c < C} exp z_ic - z_i,label), dlogits_ic = scale weight_i (softmax(z_i)_c - [c = label_i]), C the
+ * number of classes of the row's application; dlogits are 0 from C on.
+ *   logits [n, c_max] dtype, columns from C on are not read      label int32 [n]; -1: loss and gradient 0
+ *   app int32 [n] in [0, n_apps) with n_classes int32 [n_apps], or both NULL (C = c_max)      weight [n] float or NULL (1)
+ *   loss [n] float; dlogits [n, c_max] grad_dtype (dtype, or SP_BF16 from SP_F32) or NULL; may be logits if type and stride are
+ * A logit of -inf is a class that cannot be; a row that has no other counts as one without a label. */
+sp_status sp_cross_entropy(sp_ops* ops, int32_t n, int32_t c_max, int32_t dtype, const void* logits, int64_t logits_stride, int32_t n_apps,
+                           const int32_t* app, const int32_t* n_classes, const int32_t* label, const float* weight, float scale,
+                           float* loss, int32_t grad_dtype, void* dlogits, int64_t dlogits_stride, void* stream);
+
+/* norm = sqrt(sum of squares over all tensors), summed in 64 bits; out = grads * min(1, max_norm / (norm + 1e-6)).
+ *   grads: HOST array of n_tensors device pointers, contiguous tensors of sizes[i] elements of dtype; out: HOST array of device
+ *   pointers of the same sizes, or NULL to scale in place (an out[i] may be grads[i]); norm_out [1] float.  The tensors must not
+ *   overlap. */
+sp_status sp_clip_grad_norm(sp_ops* ops, int32_t n_tensors, int32_t dtype, const void* const* grads, const int64_t* sizes, float max_norm,
+                            void* const* out, float* norm_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

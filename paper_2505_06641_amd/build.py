@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsneakpeek_hip.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC", "-shared",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function", "-Wno-unknown-attributes",
     "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
@@ -19,7 +19,7 @@ HIPCC_FLAGS = [
 
 
 def sources():
-    return [os.path.join(CSRC, "sp_api.hip")]
+    return [os.path.join(CSRC, "sp_api.hip"), os.path.join(CSRC, "sp_ops.hip")]
 
 
 def build_library(verbose: bool = True) -> str:

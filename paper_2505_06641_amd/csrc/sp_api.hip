@@ -16,6 +16,7 @@
 
 #include "sneakpeek.h"
 #include "sp_common.h"
+#include "sp_host.h"
 #include "sp_rounds.h"
 #include "sp_score_generic.h"
 #include "sp_score_split.h"
@@ -191,27 +192,6 @@ class ResidentRoom {
   int64_t workgroups_ = 0;
   int kind_ = 0;
 };
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-    if (prev != dev) ok = hipSetDevice(dev) == hipSuccess;
-  }
-  ~DeviceGuard() {
-    if (prev >= 0) (void)hipSetDevice(prev);
-  }
-};
-
-#define SP_HIP(ctx, call)                                                          \
-  do {                                                                             \
-    hipError_t e_ = (call);                                                        \
-    if (e_ != hipSuccess) {                                                        \
-      (ctx)->hip_err = std::string(#call) + ": " + hipGetErrorString(e_);          \
-      return SP_EDEVICE;                                                           \
-    }                                                                              \
-  } while (0)
 
 template <typename T>
 sp_status dev_alloc(sp_ctx* c, T** out, size_t count) {

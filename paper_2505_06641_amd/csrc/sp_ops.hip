@@ -1,0 +1,345 @@
+// C entry points of the operators that train the heads: argument checks, workspace, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <new>
+#include <string>
+
+#include "sneakpeek.h"
+#include "sp_host.h"
+#include "sp_ops_clip.h"
+#include "sp_ops_common.h"
+#include "sp_ops_linear.h"
+#include "sp_ops_loss.h"
+#include "sp_ops_norm.h"
+
+using namespace sp;
+
+struct sp_ops {
+  int device = 0;
+  char* ws = nullptr;              // the caller's share of the device memory: partial sums
+  int64_t ws_bytes = 0;
+  uint32_t* err = nullptr;         // device: kErr* bits since the last sp_ops_check
+  uint32_t* err_host = nullptr;    // pinned
+  ClipSum* clip = nullptr;
+  bool clip_broken = false;        // a call ended between its launches: the counter has to be cleared
+  std::string hip_err;
+};
+
+namespace {
+
+__global__ void k_ops_clear(uint32_t* err, ClipSum* clip) {
+  if (err) *err = 0u;
+  if (clip) { clip->ended = 0u; clip->coefficient = 0.f; }
+}
+__global__ void k_ops_report(uint32_t* err, uint32_t* host) {
+  *host = atomicExch(err, 0u);
+  __threadfence_system();
+}
+__global__ void k_clip_none(float* norm_out) { *norm_out = 0.f; }
+
+bool dtype_ok(int32_t t) { return t == SP_F32 || t == SP_BF16; }
+int64_t elem_bytes(int32_t t) { return t == SP_F32 ? 4 : 2; }
+// Elements at their own size's multiples; null passes.
+bool aligned(const void* p, int32_t t) { return ((uintptr_t)p & (uintptr_t)(elem_bytes(t) - 1)) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+sp_status launched(sp_ops* o) {
+  SP_HIP(o, hipGetLastError());
+  return SP_OK;
+}
+
+// Calls f<TEAM, C>() with the smallest team that holds rows of `pieces` 16-byte pieces: parts of a wavefront for narrow rows, so
+// that no lane idles, one wavefront with up to four pieces a lane (a sum over lanes costs a wavefront nothing but its own
+// instructions, one over a workgroup two barriers), then workgroups.  False where no team does.
+template <typename F>
+bool with_team(int64_t pieces, F&& f) {
+  if (pieces <= 8) f.template operator()<8, 1>();
+  else if (pieces <= 16) f.template operator()<16, 1>();
+  else if (pieces <= 32) f.template operator()<32, 1>();
+  else if (pieces <= 64) f.template operator()<64, 1>();
+  else if (pieces <= 128) f.template operator()<64, 2>();
+  else if (pieces <= 256) f.template operator()<64, 4>();
+  else if (pieces <= 512) f.template operator()<256, 2>();
+  else if (pieces <= 1024) f.template operator()<256, 4>();
+  else if (pieces <= 2048) f.template operator()<1024, 2>();
+  else if (pieces <= 4096) f.template operator()<1024, 4>();
+  else return false;
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+sp_status sp_ops_create(int device_id, int64_t workspace_bytes, sp_ops** out) {
+  if (!out) return SP_EINVAL;
+  *out = nullptr;
+  if (workspace_bytes < SP_OPS_MIN_WORKSPACE) return SP_EINVAL;
+  int ndev = 0;
+  if (hipGetDeviceCount(&ndev) != hipSuccess || device_id < 0 || device_id >= ndev) return SP_EDEVICE;
+  sp_ops* o = new (std::nothrow) sp_ops;
+  if (!o) return SP_ENOMEM;
+  o->device = device_id;
+  DeviceGuard g(device_id);
+  sp_status rc = g.ok ? SP_OK : SP_EDEVICE;
+  auto need = [&](hipError_t e) { if (rc == SP_OK && e != hipSuccess) rc = e == hipErrorOutOfMemory ? SP_ENOMEM : SP_EDEVICE; };
+  if (rc == SP_OK) need(hipMalloc((void**)&o->ws, (size_t)workspace_bytes));
+  if (rc == SP_OK) need(hipMalloc((void**)&o->err, 256));
+  if (rc == SP_OK) need(hipHostMalloc((void**)&o->err_host, sizeof(uint32_t), hipHostMallocDefault));
+  if (rc == SP_OK) {
+    o->ws_bytes = workspace_bytes;
+    o->clip = reinterpret_cast<ClipSum*>(o->err + 16);
+    hipLaunchKernelGGL(k_ops_clear, dim3(1), dim3(1), 0, nullptr, o->err, o->clip);
+    need(hipGetLastError());
+    need(hipDeviceSynchronize());
+  }
+  if (rc != SP_OK) {
+    sp_ops_destroy(o);
+    return rc;
+  }
+  *out = o;
+  return SP_OK;
+}
+
+void sp_ops_destroy(sp_ops* o) {
+  if (!o) return;
+  DeviceGuard g(o->device);
+  (void)hipDeviceSynchronize();
+  if (o->ws) (void)hipFree(o->ws);
+  if (o->err) (void)hipFree(o->err);
+  if (o->err_host) (void)hipHostFree(o->err_host);
+  delete o;
+}
+
+const char* sp_ops_last_hip_error(const sp_ops* o) { return o ? o->hip_err.c_str() : ""; }
+
+sp_status sp_ops_check(sp_ops* o, void* stream) {
+  if (!o) return SP_EINVAL;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  hipStream_t s = (hipStream_t)stream;
+  hipLaunchKernelGGL(k_ops_report, dim3(1), dim3(1), 0, s, o->err, o->err_host);
+  SP_HIP(o, hipGetLastError());
+  SP_HIP(o, hipStreamSynchronize(s));
+  return *o->err_host ? SP_EINVAL : SP_OK;
+}
+
+sp_status sp_layer_norm(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const void* x, int64_t x_stride, const float* gamma,
+                        const float* beta, float eps, void* y, int64_t y_stride, float* mean_out, float* rstd_out, void* stream) {
+  if (!o || n < 0 || d < 1 || !dtype_ok(dtype) || x_stride < d || y_stride < d || !(eps >= 0.f) || !std::isfinite(eps)) return SP_EINVAL;
+  if (n > 0 && (!x || !y)) return SP_EINVAL;
+  if (!aligned(x, dtype) || !aligned(y, dtype) || !aligned4(gamma) || !aligned4(beta) || !aligned4(mean_out) || !aligned4(rstd_out))
+    return SP_EINVAL;
+  if (d > SP_MAX_NORM_DIM) return SP_ECAPACITY;
+  if (n == 0) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  auto run = [&]<typename T>() {
+    const bool fits = with_team((d + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
+      constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
+      const int blocks = std::min((n + rows - 1) / rows, kNormBlocks);
+      hipLaunchKernelGGL((k_norm<T, TEAM, C>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)x, x_stride, gamma,
+                         beta, eps, (T*)y, y_stride, mean_out, rstd_out);
+    });
+    return fits;
+  };
+  if (!(dtype == SP_F32 ? run.template operator()<float>() : run.template operator()<bf16>())) return SP_ECAPACITY;
+  return launched(o);
+}
+
+sp_status sp_layer_norm_backward(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const void* dy, int64_t dy_stride, const void* x,
+                                 int64_t x_stride, const float* gamma, const float* mean, const float* rstd, void* dx, int64_t dx_stride,
+                                 float* dgamma, float* dbeta, void* stream) {
+  if (!o || n < 0 || d < 1 || !dtype_ok(dtype) || dy_stride < d || x_stride < d || (dx && dx_stride < d)) return SP_EINVAL;
+  if (n > 0 && (!dy || !x || !mean || !rstd)) return SP_EINVAL;
+  if (!aligned(x, dtype) || !aligned(dy, dtype) || !aligned(dx, dtype) || !aligned4(gamma) || !aligned4(mean) || !aligned4(rstd) ||
+      !aligned4(dgamma) || !aligned4(dbeta))
+    return SP_EINVAL;
+  if (d > SP_MAX_NORM_DIM) return SP_ECAPACITY;
+  const bool sums = dgamma || dbeta;
+  if ((n == 0 || !dx) && !sums) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  const int64_t most = o->ws_bytes / (2 * (int64_t)d * (int64_t)sizeof(float));
+  int parts = 0;
+  if (n > 0) {
+    auto run = [&]<typename T>() {
+      return with_team((d + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
+        constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
+        parts = (int)std::min<int64_t>({((int64_t)n + rows - 1) / rows, 1024, sums ? most : 1024});
+        hipLaunchKernelGGL((k_norm_back<T, TEAM, C>), dim3(parts), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)dy, dy_stride,
+                           (const T*)x, x_stride, gamma, mean, rstd, (T*)dx, dx_stride, sums ? (float*)o->ws : nullptr);
+      });
+    };
+    if (!(dtype == SP_F32 ? run.template operator()<float>() : run.template operator()<bf16>())) return SP_ECAPACITY;
+  }
+  if (sums)
+    hipLaunchKernelGGL(k_norm_join, dim3((2 * d + 31) / 32), dim3(256), 0, (hipStream_t)stream, parts, d, (const float*)o->ws, dgamma,
+                       dbeta);
+  return launched(o);
+}
+
+sp_status sp_cross_entropy(sp_ops* o, int32_t n, int32_t c_max, int32_t dtype, const void* logits, int64_t logits_stride, int32_t n_apps,
+                           const int32_t* app, const int32_t* n_classes, const int32_t* label, const float* weight, float scale,
+                           float* loss, int32_t grad_dtype, void* dlogits, int64_t dlogits_stride, void* stream) {
+  if (!o || n < 0 || c_max < 1 || !dtype_ok(dtype) || logits_stride < c_max || !std::isfinite(scale)) return SP_EINVAL;
+  if (dlogits && (!dtype_ok(grad_dtype) || dlogits_stride < c_max || (dtype == SP_BF16 && grad_dtype == SP_F32))) return SP_EINVAL;
+  if ((app != nullptr) != (n_classes != nullptr) || (app && n_apps < 1)) return SP_EINVAL;
+  if (n > 0 && (!logits || !label || !loss)) return SP_EINVAL;
+  if (!aligned(logits, dtype) || (dlogits && !aligned(dlogits, grad_dtype)) || !aligned4(app) || !aligned4(n_classes) || !aligned4(label) ||
+      !aligned4(weight) || !aligned4(loss))
+    return SP_EINVAL;
+  if (n == 0) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  auto run = [&]<typename T, typename TO>() {
+    const bool fits = with_team(((int64_t)c_max + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
+      constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
+      const int blocks = std::min((n + rows - 1) / rows, kLossBlocks);
+      hipLaunchKernelGGL((k_loss<T, TO, TEAM, C>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, c_max, (const T*)logits,
+                         logits_stride, n_apps, app, n_classes, label, weight, scale, loss, (TO*)dlogits, dlogits_stride, o->err);
+    });
+    if (!fits)
+      hipLaunchKernelGGL((k_loss_wide<T, TO>), dim3(std::min(n, kLossBlocks)), dim3(1024), 0, (hipStream_t)stream, n, c_max,
+                         (const T*)logits, logits_stride, n_apps, app, n_classes, label, weight, scale, loss, (TO*)dlogits,
+                         dlogits_stride, o->err);
+  };
+  if (dtype == SP_BF16) run.template operator()<bf16, bf16>();
+  else if (dlogits && grad_dtype == SP_BF16) run.template operator()<float, bf16>();
+  else run.template operator()<float, float>();
+  return launched(o);
+}
+
+sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const void* const* grads, const int64_t* sizes, float max_norm,
+                            void* const* out, float* norm_out, void* stream) {
+  if (!o || n_tensors < 0 || !dtype_ok(dtype) || !norm_out || !aligned4(norm_out) || !(max_norm >= 0.f) || !std::isfinite(max_norm))
+    return SP_EINVAL;
+  if (n_tensors > 0 && (!grads || !sizes)) return SP_EINVAL;
+  int64_t pieces = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (sizes[i] < 0 || (sizes[i] > 0 && (!grads[i] || (out && !out[i])))) return SP_EINVAL;
+    if (!aligned(grads[i], dtype) || (out && !aligned(out[i], dtype))) return SP_EINVAL;
+  }
+  for (int i = 0; i < n_tensors; ++i) {
+    if (sizes[i] > ((int64_t)1 << 44)) return SP_ECAPACITY;
+    pieces += (sizes[i] + kClipPiece - 1) / kClipPiece;
+    if (pieces > INT_MAX || pieces * (int64_t)sizeof(double) > o->ws_bytes) return SP_ECAPACITY;
+  }
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  hipStream_t s = (hipStream_t)stream;
+  if (pieces == 0) {
+    hipLaunchKernelGGL(k_clip_none, dim3(1), dim3(1), 0, s, norm_out);
+    return launched(o);
+  }
+  if (o->clip_broken) hipLaunchKernelGGL(k_ops_clear, dim3(1), dim3(1), 0, s, (uint32_t*)nullptr, o->clip);
+  o->clip_broken = true;
+  for (int pass = 0; pass < 2; ++pass) {
+    int piece0 = 0;
+    for (int at = 0; at < n_tensors;) {
+      ClipTable tb;
+      tb.count = 0;
+      int64_t k = 0;
+      for (; at < n_tensors && tb.count < kClipTensors; ++at) {
+        if (sizes[at] == 0) continue;
+        tb.src[tb.count] = grads[at];
+        tb.dst[tb.count] = out ? out[at] : const_cast<void*>(grads[at]);
+        tb.size[tb.count] = sizes[at];
+        tb.first[tb.count++] = (int32_t)k;
+        k += (sizes[at] + kClipPiece - 1) / kClipPiece;
+      }
+      if (tb.count == 0) continue;
+      tb.first[tb.count] = (int32_t)k;
+      if (pass == 0 && dtype == SP_F32)
+        hipLaunchKernelGGL(k_clip_sum<float>, dim3((unsigned)k), dim3(256), 0, s, tb, piece0, (int)pieces, (double*)o->ws, o->clip, max_norm, norm_out);
+      else if (pass == 0)
+        hipLaunchKernelGGL(k_clip_sum<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, piece0, (int)pieces, (double*)o->ws, o->clip, max_norm, norm_out);
+      else if (dtype == SP_F32)
+        hipLaunchKernelGGL(k_clip_scale<float>, dim3((unsigned)k), dim3(256), 0, s, tb, (const ClipSum*)o->clip);
+      else
+        hipLaunchKernelGGL(k_clip_scale<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, (const ClipSum*)o->clip);
+      SP_HIP(o, hipGetLastError());
+      piece0 += (int)k;
+    }
+  }
+  o->clip_broken = false;
+  return SP_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Shared checks of the grouped linear layers.
+sp_status linear_sizes(const sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype) {
+  if (!o || n < 0 || k < 1 || m < 1 || groups < 1 || !dtype_ok(dtype)) return SP_EINVAL;
+  if (groups > SP_MAX_APPS || k > SP_MAX_LINEAR_DIM || m > SP_MAX_LINEAR_DIM) return SP_ECAPACITY;
+  return SP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+sp_status sp_grouped_linear(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype, const void* x, int64_t x_stride,
+                            const int32_t* offsets, const void* w, const float* bias, int32_t activation, int32_t out_dtype,
+                            const void* residual, int64_t residual_stride, void* y, int64_t y_stride, void* act_out,
+                            int64_t act_stride, void* stream) {
+  const sp_status bad = linear_sizes(o, n, k, m, groups, dtype);
+  if (bad != SP_OK) return bad;
+  if (x_stride < k || y_stride < m || (residual && residual_stride < m) || (act_out && act_stride < m)) return SP_EINVAL;
+  if (activation != SP_ACT_NONE && activation != SP_ACT_RELU) return SP_EINVAL;
+  if (!dtype_ok(out_dtype) || (dtype == SP_F32 && out_dtype == SP_BF16)) return SP_EINVAL;
+  if (n > 0 && (!x || !offsets || !w || !y)) return SP_EINVAL;
+  if (!aligned(x, dtype) || !aligned(w, dtype) || !aligned(y, out_dtype) || !aligned(residual, out_dtype) || !aligned(act_out, out_dtype) ||
+      !aligned4(offsets) || !aligned4(bias))
+    return SP_EINVAL;
+  if (n == 0) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  LinearArgs a{};
+  a.n = n; a.k = k; a.m = m; a.groups = groups; a.x = x; a.x_stride = x_stride; a.offsets = offsets; a.w = w; a.bias = bias;
+  a.relu = activation == SP_ACT_RELU; a.residual = residual; a.residual_stride = residual_stride; a.y = y; a.y_stride = y_stride;
+  a.act = act_out; a.act_stride = act_stride; a.err = o->err;
+  const dim3 grid((unsigned)((n + kSimpleTile - 1) / kSimpleTile + groups), (unsigned)((m + kSimpleTile - 1) / kSimpleTile));
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == SP_F32) hipLaunchKernelGGL((k_linear_simple<float, float, 0>), grid, dim3(256), 0, s, a);
+  else if (out_dtype == SP_F32) hipLaunchKernelGGL((k_linear_simple<bf16, float, 0>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_linear_simple<bf16, bf16, 0>), grid, dim3(256), 0, s, a);
+  return launched(o);
+}
+
+sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype, const void* dy,
+                                     int64_t dy_stride, const void* act, int64_t act_stride, const void* x, int64_t x_stride,
+                                     const int32_t* offsets, const void* w, void* dx, int64_t dx_stride, float* dw, float* db,
+                                     void* stream) {
+  const sp_status bad = linear_sizes(o, n, k, m, groups, dtype);
+  if (bad != SP_OK) return bad;
+  if (dy_stride < m || (act && act_stride < m) || (dw && x_stride < k) || (dx && dx_stride < k)) return SP_EINVAL;
+  if (!offsets || (n > 0 && (!dy || (dx && !w) || (dw && !x)))) return SP_EINVAL;
+  if (!aligned(dy, dtype) || !aligned(act, dtype) || !aligned(x, dtype) || !aligned(w, dtype) || !aligned(dx, dtype) || !aligned4(offsets) ||
+      !aligned4(dw) || !aligned4(db))
+    return SP_EINVAL;
+  if ((n == 0 || !dx) && !dw && !db) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  LinearArgs a{};
+  a.n = n; a.k = k; a.m = m; a.groups = groups; a.x = x; a.x_stride = x_stride; a.offsets = offsets; a.w = w;
+  a.act = const_cast<void*>(act); a.act_stride = act_stride; a.dy = dy; a.dy_stride = dy_stride; a.dx = dx; a.dx_stride = dx_stride;
+  a.dw = dw; a.db = db; a.err = o->err;
+  hipStream_t s = (hipStream_t)stream;
+  const unsigned kt = (k + kSimpleTile - 1) / kSimpleTile, mt = (m + kSimpleTile - 1) / kSimpleTile;
+  auto run = [&]<typename T>() {
+    if (dx && n > 0)
+      hipLaunchKernelGGL((k_linear_simple<T, T, 1>), dim3((unsigned)((n + kSimpleTile - 1) / kSimpleTile + groups), kt), dim3(256), 0, s, a);
+    if (dw) hipLaunchKernelGGL((k_linear_simple<T, float, 2>), dim3(kt, mt, groups), dim3(256), 0, s, a);
+    if (db) hipLaunchKernelGGL((k_bias_grad<T>), dim3(mt, groups), dim3(256), 0, s, a);
+  };
+  if (dtype == SP_F32) run.template operator()<float>(); else run.template operator()<bf16>();
+  return launched(o);
+}
+
+}  // extern "C"

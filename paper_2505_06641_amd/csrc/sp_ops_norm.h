@@ -1,0 +1,164 @@
+// Layer norm of rows and its gradients.
+//   mu = mean x, rstd = 1 / sqrt(mean (x - mu)^2 + eps), xh = (x - mu) rstd, y = xh gamma + beta
+//   q = dy gamma;  dx = rstd (q - mean q - xh mean(q xh));  dgamma = sum over rows dy xh;  dbeta = sum over rows dy
+// A row belongs to a team of lanes that keeps it in registers: one pass over memory, the variance from the differences to the
+// mean (no sum of squares less a square: that loses everything where the mean is far from 0).  Bound by memory.
+#pragma once
+#include "sp_ops_common.h"
+
+namespace sp {
+
+constexpr int kNormDimMax = 16384;          // a workgroup of 1024 threads with 16 elements each
+constexpr int kNormBlocks = 2048;           // workgroups that share out the rows of a forward pass
+
+// A team's columns: piece c of lane t holds columns (c * TEAM + t) * V on.
+template <typename T, int TEAM, int C>
+__global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm(int n, int d, const T* x, int64_t x_stride,
+                                                             const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
+                                                             T* y, int64_t y_stride, float* __restrict__ mean_out,
+                                                             float* __restrict__ rstd_out) {
+  constexpr int V = kPiece<T>, ROWS = kTeamThreads<TEAM> / TEAM;
+  __shared__ float red[2][TEAM > 64 ? TEAM / 64 : 1];
+  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  float ga[C][V], be[C][V];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int col = (c * TEAM + t) * V + i;
+      ga[c][i] = gamma && col < d ? gamma[col] : 1.f;
+      be[c][i] = beta && col < d ? beta[col] : 0.f;
+    }
+  const float fd = (float)d;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS) {
+    float v[C][V];
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TEAM + t) * V;
+      load_some(x + row * x_stride + col, d - col, 0.f, v[c]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s += v[c][i];
+    }
+    const float mu = team_sum<TEAM>(s, red[0]) / fd;
+    float q = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TEAM + t) * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        v[c][i] -= mu;
+        q += col + i < d ? v[c][i] * v[c][i] : 0.f;
+      }
+    }
+    const float rstd = 1.f / sqrtf(team_sum<TEAM>(q, red[1]) / fd + eps);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TEAM + t) * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[c][i] = v[c][i] * rstd * ga[c][i] + be[c][i];
+      store_some(y + row * y_stride + col, d - col, v[c]);
+    }
+    if (t == 0) {
+      if (mean_out) mean_out[row] = mu;
+      if (rstd_out) rstd_out[row] = rstd;
+    }
+  }
+}
+
+// Every team walks its rows with dgamma's and dbeta's sums of its columns in registers; the workgroup's teams add theirs up in LDS,
+// one after the other, and write one row of partial sums: part[workgroup][2][d].
+template <typename T, int TEAM, int C>
+__global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, const T* dy, int64_t dy_stride,
+                                                                  const T* x, int64_t x_stride,
+                                                                  const float* __restrict__ gamma, const float* __restrict__ mean,
+                                                                  const float* __restrict__ rstd, T* dx, int64_t dx_stride,
+                                                                  float* __restrict__ part) {
+  constexpr int V = kPiece<T>, ROWS = kTeamThreads<TEAM> / TEAM;
+  __shared__ float red[2][TEAM > 64 ? TEAM / 64 : 1];
+  __shared__ float sums[ROWS > 1 ? TEAM * C * V : 1][2];
+  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  float ga[C][V], dg[C][V], db[C][V];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int col = (c * TEAM + t) * V + i;
+      ga[c][i] = col < d ? (gamma ? gamma[col] : 1.f) : 0.f;
+      dg[c][i] = db[c][i] = 0.f;
+    }
+  const float fd = (float)d;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS) {
+    float g[C][V], xh[C][V];
+    const float mu = mean[row], rs = rstd[row];
+    float sq = 0.f, sqx = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TEAM + t) * V;
+      load_some(dy + row * dy_stride + col, d - col, 0.f, g[c]);
+      load_some(x + row * x_stride + col, d - col, mu, xh[c]);     // (columns beyond the row: xh = 0, dy = 0)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        xh[c][i] = (xh[c][i] - mu) * rs;
+        db[c][i] += g[c][i];
+        dg[c][i] += g[c][i] * xh[c][i];
+        g[c][i] *= ga[c][i];
+        sq += g[c][i];
+        sqx += g[c][i] * xh[c][i];
+      }
+    }
+    if (!dx) continue;
+    const float mq = team_sum<TEAM>(sq, red[0]) / fd, mqx = team_sum<TEAM>(sqx, red[1]) / fd;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TEAM + t) * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) g[c][i] = rs * (g[c][i] - mq - xh[c][i] * mqx);
+      store_some(dx + row * dx_stride + col, d - col, g[c]);
+    }
+  }
+  if (!part) return;
+  if (ROWS > 1) {
+    for (int turn = 0; turn < ROWS; ++turn) {
+      if (turn == team) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            float* at = sums[(c * V + i) * TEAM + t];
+            if (turn > 0) { dg[c][i] += at[0]; db[c][i] += at[1]; }
+            if (turn < ROWS - 1) { at[0] = dg[c][i]; at[1] = db[c][i]; }
+          }
+      }
+      __syncthreads();
+    }
+    if (team != ROWS - 1) return;
+  }
+  float* out = part + (int64_t)blockIdx.x * 2 * d;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * TEAM + t) * V;
+    store_some(out + col, d - col, dg[c]);
+    store_some(out + d + col, d - col, db[c]);
+  }
+}
+
+// Sums of the workgroups' rows of partial sums: 32 columns to a workgroup of 256, eight threads to a column.
+__global__ __launch_bounds__(256) void k_norm_join(int parts, int d, const float* __restrict__ part, float* __restrict__ dgamma,
+                                                   float* __restrict__ dbeta) {
+  __shared__ float sums[8][33];
+  const int lane = threadIdx.x % 32, slice = threadIdx.x / 32;
+  const int col = blockIdx.x * 32 + lane;              // of 2 d
+  float s = 0.f;
+  if (col < 2 * d)
+    for (int p = slice; p < parts; p += 8) s += part[(int64_t)p * 2 * d + col];
+  sums[slice][lane] = s;
+  __syncthreads();
+  if (slice == 0 && col < 2 * d) {
+    for (int j = 1; j < 8; ++j) s += sums[j][lane];
+    float* out = col < d ? dgamma : dbeta;
+    if (out) out[col < d ? col : col - d] = s;
+  }
+}
+
+}  // namespace sp
