@@ -273,6 +273,21 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
 
 namespace {
 
+constexpr int kDwWorkgroups = 1024;        // four to a compute unit
+constexpr int kDwMinRows = 256;
+
+// The launch's tiles; false where there are more than a launch holds.
+bool linear_grid(LinearArgs* a, int64_t row_tiles, int64_t col_tiles) {
+  if (row_tiles * col_tiles > INT_MAX - kXcds) return false;
+  a->row_tiles = (int)row_tiles;
+  a->col_tiles = (int)col_tiles;
+  return true;
+}
+void launch_linear(void (*kernel)(LinearArgs), const LinearArgs& a, void* stream) {
+  const int tiles = a.row_tiles * a.col_tiles;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(kLinearThreads), 0, (hipStream_t)stream, a);
+}
+
 // Shared checks of the grouped linear layers.
 sp_status linear_sizes(const sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype) {
   if (!o || n < 0 || k < 1 || m < 1 || groups < 1 || !dtype_ok(dtype)) return SP_EINVAL;
@@ -304,11 +319,15 @@ sp_status sp_grouped_linear(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t 
   a.n = n; a.k = k; a.m = m; a.groups = groups; a.x = x; a.x_stride = x_stride; a.offsets = offsets; a.w = w; a.bias = bias;
   a.relu = activation == SP_ACT_RELU; a.residual = residual; a.residual_stride = residual_stride; a.y = y; a.y_stride = y_stride;
   a.act = act_out; a.act_stride = act_stride; a.err = o->err;
-  const dim3 grid((unsigned)((n + kSimpleTile - 1) / kSimpleTile + groups), (unsigned)((m + kSimpleTile - 1) / kSimpleTile));
-  hipStream_t s = (hipStream_t)stream;
-  if (dtype == SP_F32) hipLaunchKernelGGL((k_linear_simple<float, float, 0>), grid, dim3(256), 0, s, a);
-  else if (out_dtype == SP_F32) hipLaunchKernelGGL((k_linear_simple<bf16, float, 0>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_linear_simple<bf16, bf16, 0>), grid, dim3(256), 0, s, a);
+  const bool narrow = m <= 64;
+  if (!linear_grid(&a, (int64_t)(n + kLinearRows - 1) / kLinearRows + groups, (m + (narrow ? 63 : 127)) / (narrow ? 64 : 128))) return SP_ECAPACITY;
+  auto run = [&]<typename T, typename TO>() {
+    if (narrow) launch_linear(k_linear<T, TO, kFormY, 64, false>, a, stream);
+    else launch_linear(k_linear<T, TO, kFormY, 128, false>, a, stream);
+  };
+  if (dtype == SP_F32) run.template operator()<float, float>();
+  else if (out_dtype == SP_F32) run.template operator()<bf16, float>();
+  else run.template operator()<bf16, bf16>();
   return launched(o);
 }
 
@@ -331,14 +350,45 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
   a.act = const_cast<void*>(act); a.act_stride = act_stride; a.dy = dy; a.dy_stride = dy_stride; a.dx = dx; a.dx_stride = dx_stride;
   a.dw = dw; a.db = db; a.err = o->err;
   hipStream_t s = (hipStream_t)stream;
-  const unsigned kt = (k + kSimpleTile - 1) / kSimpleTile, mt = (m + kSimpleTile - 1) / kSimpleTile;
-  auto run = [&]<typename T>() {
-    if (dx && n > 0)
-      hipLaunchKernelGGL((k_linear_simple<T, T, 1>), dim3((unsigned)((n + kSimpleTile - 1) / kSimpleTile + groups), kt), dim3(256), 0, s, a);
-    if (dw) hipLaunchKernelGGL((k_linear_simple<T, float, 2>), dim3(kt, mt, groups), dim3(256), 0, s, a);
-    if (db) hipLaunchKernelGGL((k_bias_grad<T>), dim3(mt, groups), dim3(256), 0, s, a);
+  sp_status rc = SP_OK;
+  auto run = [&]<typename T, bool MASK>() {
+    if (dx && n > 0) {
+      const bool narrow = k <= 64;
+      if (!linear_grid(&a, (int64_t)(n + kLinearRows - 1) / kLinearRows + groups, (k + (narrow ? 63 : 127)) / (narrow ? 64 : 128))) {
+        rc = SP_ECAPACITY;
+        return;
+      }
+      if (narrow) launch_linear(k_linear<T, T, kFormDx, 64, MASK>, a, stream);
+      else launch_linear(k_linear<T, T, kFormDx, 128, MASK>, a, stream);
+    }
+    if (dw) {
+      const bool narrow = m <= 64;
+      const int64_t k_tiles = (k + kLinearRows - 1) / kLinearRows, m_tiles = (m + (narrow ? 63 : 127)) / (narrow ? 64 : 128);
+      // Rows to a workgroup: so many that about kDwWorkgroups share the work, however the rows are spread over the groups; fewer
+      // chunks where the workspace does not hold their sums.
+      int64_t chunk = std::max<int64_t>(kDwMinRows, ((int64_t)n * k_tiles * m_tiles + kDwWorkgroups - 1) / kDwWorkgroups);
+      const int64_t most = o->ws_bytes / (((int64_t)k * m + m) * (int64_t)sizeof(float)) - groups;   // chunks: at most n / chunk + groups
+      if (most > 0) chunk = std::max(chunk, (n + most - 1) / most);
+      a.chunk = most > 0 && chunk < n ? (int)((chunk + 63) / 64 * 64) : 0;
+      a.part = (float*)o->ws;
+      const int64_t items = a.chunk ? (n + a.chunk - 1) / a.chunk + groups : groups;
+      if (!linear_grid(&a, items * k_tiles, m_tiles)) {
+        rc = SP_ECAPACITY;
+        return;
+      }
+      if (narrow) launch_linear(k_linear<T, float, kFormDw, 64, MASK>, a, stream);
+      else launch_linear(k_linear<T, float, kFormDw, 128, MASK>, a, stream);
+      if (a.chunk)
+        hipLaunchKernelGGL(k_join_chunks, dim3((unsigned)std::min<int64_t>(((int64_t)k * m + m + 255) / 256, 1024), groups), dim3(256), 0, s, a);
+    } else if (db) {
+      hipLaunchKernelGGL((k_bias_grad<T>), dim3((m + 63) / 64, groups), dim3(256), 0, s, a);
+    }
   };
-  if (dtype == SP_F32) run.template operator()<float>(); else run.template operator()<bf16>();
+  if (dtype == SP_F32 && act) run.template operator()<float, true>();
+  else if (dtype == SP_F32) run.template operator()<float, false>();
+  else if (act) run.template operator()<bf16, true>();
+  else run.template operator()<bf16, false>();
+  if (rc != SP_OK) return rc;
   return launched(o);
 }
 

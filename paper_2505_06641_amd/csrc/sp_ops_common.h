@@ -130,14 +130,14 @@ __device__ __forceinline__ void group_rows(const int32_t* offsets, int n, int g,
   *hi = min(max(offsets[g + 1], a), n);
 }
 
-// Which rows a workgroup's tile of TILE rows holds.  The tiles of group 0 come first, then those of group 1, ...; a group
+// Which rows a workgroup's tile of at most tile_rows rows holds.  The tiles of group 0 come first, then those of group 1, ...; a group
 // without rows has none.  Rows behind the last group form one more group (g == n_groups).  Every wavefront looks for itself:
 // 64 groups at a time, each lane one of them.  Returns false where there are fewer tiles than `tile` + 1.
 struct RowTile {
   int g, lo, hi;      // rows lo .. hi of group g
+  bool whole;         // they are all of the group's rows
 };
-template <int TILE>
-__device__ __forceinline__ bool find_row_tile(const int32_t* offsets, int n_groups, int n, int tile, RowTile* out) {
+__device__ __forceinline__ bool find_row_tile(const int32_t* offsets, int n_groups, int n, int tile_rows, int tile, RowTile* out) {
   const int lane = threadIdx.x & 63;
   int before = 0, end = 0;                       // tiles and rows of the groups before this turn's
   for (int base = 0; base <= n_groups; base += 64) {
@@ -151,15 +151,16 @@ __device__ __forceinline__ bool find_row_tile(const int32_t* offsets, int n_grou
     }
     int s0 = __shfl_up(e, 1);
     if (lane == 0) s0 = end;
-    const int tiles = g <= n_groups ? (e - s0 + TILE - 1) / TILE : 0;
+    const int tiles = g <= n_groups ? (e - s0 + tile_rows - 1) / tile_rows : 0;
     const int upto = before + (int)wave_scan_incl((uint32_t)tiles);
     const unsigned long long has = __ballot(upto > tile);
     if (has) {
       const int l = __ffsll(has) - 1;
-      const int first = __shfl(s0 + (tile - (upto - tiles)) * TILE, l), last = __shfl(e, l);
+      const int first = __shfl(s0 + (tile - (upto - tiles)) * tile_rows, l), last = __shfl(e, l);
       out->g = base + l;
       out->lo = first;
-      out->hi = min(first + TILE, last);
+      out->hi = last - first < tile_rows ? last : first + tile_rows;
+      out->whole = __shfl(tiles, l) == 1;
       return true;
     }
     before = __shfl(upto, 63);

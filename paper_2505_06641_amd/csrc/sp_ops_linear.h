@@ -1,10 +1,35 @@
 // Linear layers of rows that are grouped by application, and their gradients.
 //   y_i = act(x_i W_g + b_g) + r_i      dx_i = dz_i W_g^T      dW_g = sum over the group's rows x_i^T dz_i      db_g = sum dz_i
 // with dz = dy where the activation passed something, 0 elsewhere.
+//
+// All three are products of a "row side" and a "column side" over a common depth:
+//   y   rows x [n, k]         columns w [k, m]           depth k
+//   dx  rows dz [n, m]        columns w^T                depth m
+//   dW  rows x^T              columns dz                 depth: the group's rows
+// A workgroup computes a tile of 128 rows by BN columns with the matrix cores (v_mfma_f32_32x32x16_bf16, sums in float32).  Both
+// sides of a piece of the depth go from memory through registers into LDS, while the matrix cores work on the piece before: on the
+// way the mask of the activation is applied, what lies beyond the tile, the group or the depth becomes 0, and float32 is split.
+// A side whose depth is the contiguous one in memory lies in LDS as it came and is read 8 elements of the depth at a time; one
+// whose depth is strided is read by the LDS's transposing loads.
+//
+// Float32: a value is the sum of three bfloat16 numbers, each the rounded rest of the ones before it (8 + 8 + 8 significant bits: what
+// is left is below 2^-27 of the value).  Of the nine products of two such sums the six largest are taken, each exact in the float32
+// sum; the three others are below 2^-25 of the product together.  Six instructions of the bfloat16 rate are 2.6 times the float32
+// instruction's rate.  An infinite factor (or one that rounds to one in bfloat16, from 3.39e38 on) gives NaN.
 #pragma once
+#include "sp_common.h"
 #include "sp_ops_common.h"
 
 namespace sp {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
 struct LinearArgs {
   int n, k, m, groups;
@@ -21,98 +46,357 @@ struct LinearArgs {
   float* dw;                             // [groups, k, m] or null
   float* db;                             // [groups, m] or null
   uint32_t* err;
+  int row_tiles, col_tiles;              // of the launch (dW: tiles of k and of m)
+  int chunk;                             // dW: rows of a group that a workgroup adds up, 0: all of them
+  float* part;                           // dW: [chunks, k * m + m] sums of the chunks
 };
 
-constexpr int kSimpleTile = 64, kSimpleDepth = 16;
+enum LinearForm { kFormY = 0, kFormDx = 1, kFormDw = 2 };
+
+constexpr int kLinearThreads = 256;
+constexpr int kLinearRows = 128;                                      // rows of a tile
+template <typename T> constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1; // bfloat16 numbers that make up a value
+template <typename T> constexpr int kDepth = sizeof(T) == 4 ? 32 : 64; // depth of a piece: 48 KB of LDS with 128 columns, 32 KB
 
 // Where NaN has to stay NaN: only what is below 0 becomes 0.
 __device__ __forceinline__ float relu_of(float z) { return z < 0.f ? 0.f : z; }
 
-template <typename T>
-__device__ __forceinline__ float dz_at(const LinearArgs& a, int64_t row, int col) {
-  const float g = to_float(((const T*)a.dy)[row * a.dy_stride + col]);
-  if (!a.act) return g;
-  return to_float(((const T*)a.act)[row * a.act_stride + col]) <= 0.f ? 0.f : g;
+__device__ __forceinline__ u32x4 load_raw(const void* p) {
+  const u32x4_any q = *reinterpret_cast<const u32x4_any*>(p);
+  return u32x4{q[0], q[1], q[2], q[3]};
 }
-
-// One 64 x 64 tile of a product a workgroup, operands staged through LDS, float32 multiply-adds.
-// FORM 0: y, 1: dx, 2: dW.
-template <typename T, typename TO, int FORM>
-__global__ __launch_bounds__(256) void k_linear_simple(LinearArgs a) {
-  __shared__ float A[kSimpleDepth][kSimpleTile + 1], B[kSimpleDepth][kSimpleTile + 1];
-  RowTile rt;
-  int depth, r0, c0, rows, cols;
-  const int width = FORM == 1 ? a.k : a.m;
-  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
-  if (FORM == 2) {
-    rt.g = blockIdx.z;
-    group_rows(a.offsets, a.n, rt.g, &rt.lo, &rt.hi);
-    depth = rt.hi - rt.lo;
-    r0 = blockIdx.x * kSimpleTile;
-    rows = min(kSimpleTile, a.k - r0);
-  } else {
-    if (!find_row_tile<kSimpleTile>(a.offsets, a.groups, a.n, blockIdx.x, &rt)) return;
-    depth = rt.g < a.groups ? (FORM == 0 ? a.k : a.m) : 0;
-    r0 = rt.lo;
-    rows = rt.hi - rt.lo;
+__device__ __forceinline__ u32x4 load_raw_some(const float* p, int count) {
+  u32x4 q = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < count) q[i] = __float_as_uint(p[i]);
+  return q;
+}
+__device__ __forceinline__ u32x4 load_raw_some(const bf16* p, int count) {
+  const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+  u32x4 q = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < count) q[i / 2] |= (uint32_t)h[i] << (16 * (i % 2));
+  return q;
+}
+// dz: dy where act is not <= 0 (as the comparison has it, NaN passes).
+__device__ __forceinline__ u32x4 masked(const float*, u32x4 dy, u32x4 act) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) dy[i] = __uint_as_float(act[i]) <= 0.f ? 0u : dy[i];
+  return dy;
+}
+__device__ __forceinline__ u32x4 masked(const bf16*, u32x4 dy, u32x4 act) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = __uint_as_float(act[i] << 16) <= 0.f ? 0u : 0xffffu;
+    const uint32_t hi = __uint_as_float(act[i] & 0xffff0000u) <= 0.f ? 0u : 0xffff0000u;
+    dy[i] &= lo | hi;
   }
-  c0 = blockIdx.y * kSimpleTile;
-  cols = min(kSimpleTile, width - c0);
-  const T* w = (const T*)a.w + (int64_t)rt.g * a.k * a.m;
-  const T* x = (const T*)a.x;
-  float acc[4][4] = {};
-  const int tr = threadIdx.x / 16, tc = threadIdx.x % 16;
-  for (int t0 = 0; t0 < depth; t0 += kSimpleDepth) {
-    for (int i = threadIdx.x; i < kSimpleTile * kSimpleDepth; i += 256) {
-      if (FORM == 2) {
-        const int t = i / kSimpleTile, r = i % kSimpleTile;
-        const bool in = t0 + t < depth;
-        const int64_t row = rt.lo + t0 + t;
-        A[t][r] = in && r < rows ? to_float(x[row * a.x_stride + r0 + r]) : 0.f;
-        B[t][r] = in && r < cols ? dz_at<T>(a, row, c0 + r) : 0.f;
-      } else {
-        const int r = i / kSimpleDepth, t = i % kSimpleDepth;
-        const int64_t row = r0 + r;
-        const bool in = t0 + t < depth;
-        A[t][r] = in && r < rows ? (FORM == 0 ? to_float(x[row * a.x_stride + t0 + t]) : dz_at<T>(a, row, t0 + t)) : 0.f;
-        if (FORM == 0) {
-          const int t2 = i / kSimpleTile, c = i % kSimpleTile;
-          B[t2][c] = t0 + t2 < depth && c < cols ? to_float(w[(int64_t)(t0 + t2) * a.m + c0 + c]) : 0.f;
-        } else {
-          B[t][r] = in && r < cols ? to_float(w[(int64_t)(c0 + r) * a.m + t0 + t]) : 0.f;
+  return dy;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+__device__ __forceinline__ float low_bf16(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+
+// One side of a tile: W rows (or columns) by kDepth<T> of the depth.
+// LDS, per plane: contiguous depth [W][depth], the 16-byte pieces of a row permuted by the row, so that the eight rows that are
+// read together lie in different banks; strided depth [depth][W], the 64-byte pieces permuted likewise by the depth.
+template <typename T, int W, bool STRIDED, bool MASK>
+struct Side {
+  static constexpr int V = kPiece<T>, D = kDepth<T>, P = kPlanes<T>;
+  static constexpr int kPieces = W * D / V / kLinearThreads;        // of 16 bytes, each thread's
+  static constexpr int kAcross = (STRIDED ? W : D) / V;             // pieces of a contiguous run in memory
+  static constexpr int kElems = W * D;
+  u32x4 raw[kPieces];
+  u32x4 act[MASK ? kPieces : 1];
+
+  // base: element (first row, depth 0) of a contiguous side, (depth 0, first column) of a strided one.
+  __device__ __forceinline__ void load(const T* base, int64_t stride, const T* act_base, int64_t act_stride, int valid, int t0, int depth) {
+    if (valid >= W && t0 + D <= depth) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int p = threadIdx.x + i * kLinearThreads, major = p / kAcross, minor = (p % kAcross) * V;
+        const int64_t row = STRIDED ? t0 + major : major;
+        const int col = STRIDED ? minor : t0 + minor;
+        raw[i] = load_raw(base + row * stride + col);
+        if (MASK) act[i] = load_raw(act_base + row * act_stride + col);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int p = threadIdx.x + i * kLinearThreads, major = p / kAcross, minor = (p % kAcross) * V;
+        const int64_t row = STRIDED ? t0 + major : major;
+        const int col = STRIDED ? minor : t0 + minor;
+        const bool in = STRIDED ? t0 + major < depth : major < valid;
+        const int count = in ? (STRIDED ? valid : depth) - col : 0;
+        raw[i] = u32x4{0, 0, 0, 0};
+        if (MASK) act[i] = u32x4{0, 0, 0, 0};
+        if (count >= V) {
+          raw[i] = load_raw(base + row * stride + col);
+          if (MASK) act[i] = load_raw(act_base + row * act_stride + col);
+        } else if (count > 0) {
+          raw[i] = load_raw_some(base + row * stride + col, count);
+          if (MASK) act[i] = load_raw_some(act_base + row * act_stride + col, count);
         }
       }
     }
-    __syncthreads();
-    for (int t = 0; t < kSimpleDepth; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += A[t][tr * 4 + i] * B[t][tc + 16 * j];
-    __syncthreads();
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int r = tr * 4 + i, c = tc + 16 * j;
-      if (r >= rows || c >= cols) continue;
-      float v = acc[i][j];
-      const int64_t row = r0 + r;
-      if (FORM == 2) {
-        a.dw[((int64_t)rt.g * a.k + row) * a.m + c0 + c] = v;
-      } else if (FORM == 1) {
-        ((TO*)a.dx)[row * a.dx_stride + c0 + c] = from_float<TO>(v);
+
+  __device__ __forceinline__ static int place(int major, int minor) {     // element of a plane, minor a multiple of 4
+    if (STRIDED) {
+      const int swap = W == 128 ? major & 3 : (major >> 1) & 1;
+      return major * W + (((minor / 32) ^ swap) * 32) + minor % 32;
+    }
+    const int swap = D == 64 ? major & 7 : (major >> 1) & 3;
+    return major * D + (((minor / 8) ^ swap) * 8) + minor % 8;
+  }
+
+  __device__ __forceinline__ void store(uint16_t* lds) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int p = threadIdx.x + i * kLinearThreads, major = p / kAcross, minor = (p % kAcross) * V;
+      if (MASK) raw[i] = masked((const T*)nullptr, raw[i], act[i]);
+      uint16_t* at = lds + place(major, minor);
+      if constexpr (P == 1) {
+        *reinterpret_cast<u32x4*>(at) = raw[i];
       } else {
-        const bool in = rt.g < a.groups;
-        if (in && a.bias) v += a.bias[(int64_t)rt.g * a.m + c0 + c];
-        if (a.relu) v = relu_of(v);
-        if (a.act) ((TO*)a.act)[row * a.act_stride + c0 + c] = from_float<TO>(v);
-        if (in && a.residual) v += to_float(((const TO*)a.residual)[row * a.residual_stride + c0 + c]);
-        ((TO*)a.y)[row * a.y_stride + c0 + c] = from_float<TO>(v);
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(raw[i][j]);
+#pragma unroll
+        for (int pl = 0; pl < 3; ++pl) {
+          const u32x2 h = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+          *reinterpret_cast<u32x2*>(at + pl * kElems) = h;
+          v[0] -= low_bf16(h[0]);
+          v[1] -= high_bf16(h[0]);
+          v[2] -= low_bf16(h[1]);
+          v[3] -= high_bf16(h[1]);
+        }
       }
     }
+  }
+
+  // Columns' sums of what the thread has loaded (strided sides: a thread's pieces share their columns).
+  __device__ __forceinline__ void add_columns(float (&sum)[V]) const {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if constexpr (P == 3) sum[j] += __uint_as_float(raw[i][j]);
+        else sum[j] += j % 2 ? high_bf16(raw[i][j / 2]) : low_bf16(raw[i][j / 2]);
+      }
+  }
+
+  // The fragment of 32 rows (columns) from w0 on and 16 of the depth: lane l holds w0 + l % 32, 8 (l / 32) .. + 7 of the depth.
+  __device__ __forceinline__ static bf16x8 fragment(const uint16_t* lds, int w0, int step) {
+    const int l = threadIdx.x & 63;
+    if (!STRIDED) return *reinterpret_cast<const bf16x8*>(lds + place(w0 + (l & 31), step * 16 + 8 * (l >> 5)));
+    // transposing load: of every 16 lanes, lane s gives 4 columns from 4 (s % 4) on at depth s / 4, and gets column s at 4 depths
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    const int t = step * 16 + 8 * (l >> 5) + (l & 15) / 4, c = w0 + 16 * ((l >> 4) & 1) + 4 * (l & 3);
+    union { s16x4 h[2]; bf16x8 v; } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + place(t, c)));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + place(t + 4, c)));
+    return u.v;
+  }
+};
+
+// Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, two by two: 64 rows and BN / 2 columns each.
+template <typename T, typename TO, int FORM, int BN, bool MASK>
+__global__ __launch_bounds__(kLinearThreads, 2) void k_linear(LinearArgs a) {
+  constexpr int BM = kLinearRows, D = kDepth<T>, P = kPlanes<T>, FR = 2, FC = BN / 64, V = kPiece<T>;
+  typedef Side<T, BM, FORM == kFormDw, FORM == kFormDx && MASK> Rows;
+  typedef Side<T, BN, FORM != kFormDx, FORM == kFormDw && MASK> Cols;
+  __shared__ __align__(16) uint16_t lds_rows[P * Rows::kElems], lds_cols[P * Cols::kElems];
+  if (blockIdx.x == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
+
+  // the tile: consecutive ones share rows, and go to one die as far as that is possible
+  const int tile = xcd_tile(blockIdx.x, a.row_tiles * a.col_tiles);
+  if (tile < 0) return;
+  const int rt = tile / a.col_tiles, ct = tile % a.col_tiles, c0 = ct * BN;
+  RowTile rows;
+  int r0, n_rows, depth;
+  int64_t slot = -1;                                       // dW: where a chunk's sums go
+  const int width = FORM == kFormDx ? a.k : a.m;
+  if (FORM == kFormDw) {
+    const int k_tiles = (a.k + BM - 1) / BM, kt = rt % k_tiles, item = rt / k_tiles;
+    if (a.chunk == 0) {
+      rows.g = item;
+      group_rows(a.offsets, a.n, item, &rows.lo, &rows.hi);
+    } else {
+      if (!find_row_tile(a.offsets, a.groups, a.n, a.chunk, item, &rows) || rows.g >= a.groups) return;
+      if (!rows.whole) slot = item;
+    }
+    r0 = kt * BM;
+    n_rows = a.k - r0;
+    depth = rows.hi - rows.lo;
+  } else {
+    if (!find_row_tile(a.offsets, a.groups, a.n, BM, rt, &rows)) return;
+    r0 = rows.lo;
+    n_rows = rows.hi - rows.lo;
+    depth = rows.g < a.groups ? (FORM == kFormY ? a.k : a.m) : 0;
+  }
+  const T* x = (const T*)a.x;
+  const T* w = (const T*)a.w + (int64_t)(FORM != kFormDw ? min(rows.g, a.groups - 1) : 0) * a.k * a.m;
+  const T* dy = (const T*)a.dy;
+  const T* act = (const T*)a.act;
+
+  Rows sr;
+  Cols sc;
+  auto load = [&](int t0) {
+    if (FORM == kFormY) {
+      sr.load(x + (int64_t)r0 * a.x_stride, a.x_stride, nullptr, 0, n_rows, t0, depth);
+      sc.load(w + c0, a.m, nullptr, 0, width - c0, t0, depth);
+    } else if (FORM == kFormDx) {
+      sr.load(dy + (int64_t)r0 * a.dy_stride, a.dy_stride, act + (int64_t)r0 * a.act_stride, a.act_stride, n_rows, t0, depth);
+      sc.load(w + (int64_t)c0 * a.m, a.m, nullptr, 0, width - c0, t0, depth);
+    } else {
+      sr.load(x + (int64_t)rows.lo * a.x_stride + r0, a.x_stride, nullptr, 0, n_rows, t0, depth);
+      sc.load(dy + (int64_t)rows.lo * a.dy_stride + c0, a.dy_stride, act + (int64_t)rows.lo * a.act_stride + c0, a.act_stride, width - c0,
+              t0, depth);
+    }
+  };
+
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wr = (wave >> 1) * 64, wc = (wave & 1) * (BN / 2);
+  f32x16 acc[FR][FC];
+#pragma unroll
+  for (int i = 0; i < FR; ++i)
+#pragma unroll
+    for (int j = 0; j < FC; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  const bool sum_columns = FORM == kFormDw && a.db && r0 == 0;
+  float sums[V] = {};
+
+  if (depth > 0) load(0);
+  for (int t0 = 0; t0 < depth; t0 += D) {
+    sr.store(lds_rows);
+    sc.store(lds_cols);
+    if (FORM == kFormDw && sum_columns) sc.add_columns(sums);
+    __syncthreads();
+    if (t0 + D < depth) load(t0 + D);
+#pragma unroll
+    for (int step = 0; step < D / 16; ++step) {
+      bf16x8 fr[FR][P], fc[FC][P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+#pragma unroll
+        for (int i = 0; i < FR; ++i) fr[i][p] = Rows::fragment(lds_rows + p * Rows::kElems, wr + i * 32, step);
+#pragma unroll
+        for (int j = 0; j < FC; ++j) fc[j][p] = Cols::fragment(lds_cols + p * Cols::kElems, wc + j * 32, step);
+      }
+#pragma unroll
+      for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+        for (int q = P - 1 - p; q >= 0; --q)
+#pragma unroll
+          for (int i = 0; i < FR; ++i)
+#pragma unroll
+            for (int j = 0; j < FC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fc[j][q], fr[i][p], acc[i][j], 0, 0, 0);
+    }
+    __syncthreads();
+  }
+
+  // lane l has row l % 32 of a 32 x 32 block, and of its columns 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3
+#pragma unroll
+  for (int i = 0; i < FR; ++i) {
+    const int r = wr + i * 32 + (lane & 31);
+    if (r >= n_rows) continue;
+    const int64_t row = r0 + r;
+#pragma unroll
+    for (int j = 0; j < FC; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = c0 + wc + j * 32 + 8 * q + 4 * (lane >> 5), left = width - c;
+        if (left <= 0) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+        if (FORM == kFormDw) {
+          float* out = slot < 0 ? a.dw + (int64_t)rows.g * a.k * a.m : a.part + slot * ((int64_t)a.k * a.m + a.m);
+          store_some(out + row * a.m + c, left, v);
+        } else if (FORM == kFormDx) {
+          store_some((TO*)a.dx + row * a.dx_stride + c, left, v);
+        } else {
+          const bool in = rows.g < a.groups;
+          if (in && a.bias) {
+            float b[4];
+            load_some(a.bias + (int64_t)rows.g * a.m + c, left, 0.f, b);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += b[e];
+          }
+          if (a.relu) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = relu_of(v[e]);
+          }
+          if (a.act) store_some((TO*)a.act + row * a.act_stride + c, left, v);
+          if (in && a.residual) {
+            const TO* from = (const TO*)a.residual + row * a.residual_stride + c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += e < left ? to_float(from[e]) : 0.f;
+          }
+          store_some((TO*)a.y + row * a.y_stride + c, left, v);
+        }
+      }
+  }
+  if (FORM == kFormDw && sum_columns) {                    // the threads that have loaded the same columns: their sums through LDS
+    constexpr int across = Cols::kAcross, same = kLinearThreads / across;
+    float* s = reinterpret_cast<float*>(lds_rows);         // [same][BN]; the last fragments have been read
+    static_assert(same * BN * sizeof(float) <= sizeof(lds_rows), "sums of columns fit");
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[(threadIdx.x / across) * BN + (threadIdx.x % across) * V + j] = sums[j];
+    __syncthreads();
+    const int c = c0 + threadIdx.x;
+    if (threadIdx.x < BN && c < a.m) {
+      float v = 0.f;
+      for (int u = 0; u < same; ++u) v += s[u * BN + threadIdx.x];
+      float* out = slot < 0 ? a.db + (int64_t)rows.g * a.m : a.part + slot * ((int64_t)a.k * a.m + a.m) + (int64_t)a.k * a.m;
+      out[c] = v;
+    }
+  }
 }
 
-// db: 64 columns of one group to a workgroup, four rows at a time.
+// Adds up the chunks of the groups that have several, in their order, and clears the gradients of the empty groups.
+__global__ __launch_bounds__(256) void k_join_chunks(LinearArgs a) {
+  const int g = blockIdx.y;
+  const int64_t km = (int64_t)a.k * a.m, all = km + (a.db ? a.m : 0);
+  // the chunks of the groups before this one, and its own
+  int lo, hi, end = 0, before = 0;
+  const int lane = threadIdx.x & 63;
+  for (int base = 0; base <= g; base += 64) {
+    const int q = base + lane;
+    int e = q <= g ? min(max(a.offsets[q + 1], 0), a.n) : 0;
+    e = max(e, end);
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const int o = __shfl_up(e, s);
+      if (lane >= s) e = max(e, o);
+    }
+    int s0 = __shfl_up(e, 1);
+    if (lane == 0) s0 = end;
+    const int chunks = q <= g ? (e - s0 + a.chunk - 1) / a.chunk : 0;
+    const int upto = before + (int)wave_scan_incl((uint32_t)chunks);
+    if (g - base < 64) {
+      lo = __shfl(upto - chunks, g - base);
+      hi = __shfl(upto, g - base);
+    }
+    before = __shfl(upto, 63);
+    end = __shfl(e, 63);
+  }
+  if (hi - lo == 1) return;                                // written by the one chunk's workgroups
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    float v = 0.f;
+    for (int s = lo; s < hi; ++s) v += a.part[s * (km + a.m) + i];
+    if (i < km) a.dw[g * km + i] = v; else a.db[(int64_t)g * a.m + i - km] = v;
+  }
+}
+
+// db alone: 64 columns of one group to a workgroup, four rows at a time.
 template <typename T>
 __global__ __launch_bounds__(256) void k_bias_grad(LinearArgs a) {
   __shared__ float sums[4][64];
@@ -122,7 +406,10 @@ __global__ __launch_bounds__(256) void k_bias_grad(LinearArgs a) {
   const int lane = threadIdx.x % 64, slice = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
   float s = 0.f;
   if (col < a.m)
-    for (int row = lo + slice; row < hi; row += 4) s += dz_at<T>(a, row, col);
+    for (int64_t row = lo + slice; row < hi; row += 4) {
+      const float g = to_float(((const T*)a.dy)[row * a.dy_stride + col]);
+      s += a.act && to_float(((const T*)a.act)[row * a.act_stride + col]) <= 0.f ? 0.f : g;
+    }
   sums[slice][lane] = s;
   __syncthreads();
   if (slice == 0 && col < a.m)
