@@ -41,6 +41,11 @@ __device__ __forceinline__ void load_piece(const bf16* p, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = __uint_as_float((uint32_t)q[i] << 16);
 }
+__device__ __forceinline__ void load_piece(const float* p, float (&v)[8]) {
+  const f32x4_any a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+}
 __device__ __forceinline__ void store_piece(float* p, const float (&v)[4]) {
   f32x4_any q;
 #pragma unroll

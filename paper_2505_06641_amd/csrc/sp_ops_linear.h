@@ -207,11 +207,14 @@ struct Side {
 
 // Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, two by two: 64 rows and BN / 2 columns each.
 template <typename T, typename TO, int FORM, int BN, bool MASK>
-__global__ __launch_bounds__(kLinearThreads, 2) void k_linear(LinearArgs a) {
+__global__ __launch_bounds__(kLinearThreads, FORM == kFormDw ? 2 : 3) void k_linear(LinearArgs a) {
   constexpr int BM = kLinearRows, D = kDepth<T>, P = kPlanes<T>, FR = 2, FC = BN / 64, V = kPiece<T>;
   typedef Side<T, BM, FORM == kFormDw, FORM == kFormDx && MASK> Rows;
   typedef Side<T, BN, FORM != kFormDx, FORM == kFormDw && MASK> Cols;
-  __shared__ __align__(16) uint16_t lds_rows[P * Rows::kElems], lds_cols[P * Cols::kElems];
+  __shared__ __align__(16) uint16_t lds[P * (Rows::kElems + Cols::kElems)];
+  uint16_t* lds_rows = lds;
+  uint16_t* lds_cols = lds + P * Rows::kElems;
+  static_assert(sizeof(lds) >= 64 * BN * sizeof(float), "half a tile of sums fits");
   if (blockIdx.x == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
 
   // the tile: consecutive ones share rows, and go to one die as far as that is possible
@@ -302,52 +305,70 @@ __global__ __launch_bounds__(kLinearThreads, 2) void k_linear(LinearArgs a) {
     __syncthreads();
   }
 
-  // lane l has row l % 32 of a 32 x 32 block, and of its columns 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3
+  // Sums to memory by way of LDS, 64 rows at a time, so that whole lines are read and written: lane l has row l % 32 of a 32 x 32
+  // block, and of its columns 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3.  In LDS the 16-byte pieces of a row are permuted
+  // by the row, so that neither side meets in a bank.
+  float* stage = reinterpret_cast<float*>(lds);            // [64][BN]
+  constexpr int VO = kPiece<TO>, kAcross = BN / VO;        // 16 bytes of output a time
 #pragma unroll
   for (int i = 0; i < FR; ++i) {
-    const int r = wr + i * 32 + (lane & 31);
-    if (r >= n_rows) continue;
-    const int64_t row = r0 + r;
+    const int mine = (wave >> 1) * 32 + (lane & 31);
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < FC; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int c = c0 + wc + j * 32 + 8 * q + 4 * (lane >> 5), left = width - c;
-        if (left <= 0) continue;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
-        if (FORM == kFormDw) {
-          float* out = slot < 0 ? a.dw + (int64_t)rows.g * a.k * a.m : a.part + slot * ((int64_t)a.k * a.m + a.m);
-          store_some(out + row * a.m + c, left, v);
-        } else if (FORM == kFormDx) {
-          store_some((TO*)a.dx + row * a.dx_stride + c, left, v);
-        } else {
-          const bool in = rows.g < a.groups;
-          if (in && a.bias) {
-            float b[4];
-            load_some(a.bias + (int64_t)rows.g * a.m + c, left, 0.f, b);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += b[e];
-          }
-          if (a.relu) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = relu_of(v[e]);
-          }
-          if (a.act) store_some((TO*)a.act + row * a.act_stride + c, left, v);
-          if (in && a.residual) {
-            const TO* from = (const TO*)a.residual + row * a.residual_stride + c;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += e < left ? to_float(from[e]) : 0.f;
-          }
-          store_some((TO*)a.y + row * a.y_stride + c, left, v);
-        }
+        const int piece = (wc + j * 32 + 8 * q) / 4 + (lane >> 5);
+        *reinterpret_cast<f32x4*>(stage + mine * BN + ((piece ^ (mine % (BN / 4))) * 4)) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
       }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 64 * kAcross / kLinearThreads; ++u) {
+      const int p = threadIdx.x + u * kLinearThreads, sr_ = p / kAcross, sc_ = (p % kAcross) * VO;
+      const int r = (sr_ >> 5) * 64 + i * 32 + (sr_ & 31), c = c0 + sc_, left = width - c;
+      if (r >= n_rows || left <= 0) continue;
+      const int64_t row = r0 + r;
+      float v[VO];
+#pragma unroll
+      for (int h = 0; h < VO / 4; ++h) {
+        const f32x4 f = *reinterpret_cast<const f32x4*>(stage + sr_ * BN + (((sc_ / 4 + h) ^ (sr_ % (BN / 4))) * 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * h + e] = f[e];
+      }
+      if (FORM == kFormDw) {
+        float* out = slot < 0 ? a.dw + (int64_t)rows.g * a.k * a.m : a.part + slot * ((int64_t)a.k * a.m + a.m);
+        store_some(out + row * a.m + c, left, v);
+      } else if (FORM == kFormDx) {
+        store_some((TO*)a.dx + row * a.dx_stride + c, left, v);
+      } else {
+        const bool in = rows.g < a.groups;
+        if (in && a.bias) {
+          float b[VO];
+          load_some(a.bias + (int64_t)rows.g * a.m + c, left, 0.f, b);
+#pragma unroll
+          for (int e = 0; e < VO; ++e) v[e] += b[e];
+        }
+        if (a.relu) {
+#pragma unroll
+          for (int e = 0; e < VO; ++e) v[e] = relu_of(v[e]);
+        }
+        if (a.act) store_some((TO*)a.act + row * a.act_stride + c, left, v);
+        if (in && a.residual) {
+          float b[VO];
+          load_some((const TO*)a.residual + row * a.residual_stride + c, left, 0.f, b);
+#pragma unroll
+          for (int e = 0; e < VO; ++e) v[e] += b[e];
+        }
+        store_some((TO*)a.y + row * a.y_stride + c, left, v);
+      }
+    }
   }
   if (FORM == kFormDw && sum_columns) {                    // the threads that have loaded the same columns: their sums through LDS
     constexpr int across = Cols::kAcross, same = kLinearThreads / across;
-    float* s = reinterpret_cast<float*>(lds_rows);         // [same][BN]; the last fragments have been read
-    static_assert(same * BN * sizeof(float) <= sizeof(lds_rows), "sums of columns fit");
+    float* s = stage;                                      // [same][BN]
+    static_assert(same <= 64, "sums of columns fit");
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < V; ++j) s[(threadIdx.x / across) * BN + (threadIdx.x % across) * V + j] = sums[j];
     __syncthreads();
