@@ -23,17 +23,12 @@ struct sp_ops {
   int64_t ws_bytes = 0;
   uint32_t* err = nullptr;         // device: kErr* bits since the last sp_ops_check
   uint32_t* err_host = nullptr;    // pinned
-  ClipSum* clip = nullptr;
-  bool clip_broken = false;        // a call ended between its launches: the counter has to be cleared
   std::string hip_err;
 };
 
 namespace {
 
-__global__ void k_ops_clear(uint32_t* err, ClipSum* clip) {
-  if (err) *err = 0u;
-  if (clip) { clip->ended = 0u; clip->coefficient = 0.f; }
-}
+__global__ void k_ops_clear(uint32_t* err) { *err = 0u; }
 __global__ void k_ops_report(uint32_t* err, uint32_t* host) {
   *host = atomicExch(err, 0u);
   __threadfence_system();
@@ -56,7 +51,9 @@ sp_status launched(sp_ops* o) {
 // instructions, one over a workgroup two barriers), then workgroups.  False where no team does.
 template <typename F>
 bool with_team(int64_t pieces, F&& f) {
-  if (pieces <= 8) f.template operator()<8, 1>();
+  if (pieces <= 2) f.template operator()<2, 1>();
+  else if (pieces <= 4) f.template operator()<4, 1>();
+  else if (pieces <= 8) f.template operator()<8, 1>();
   else if (pieces <= 16) f.template operator()<16, 1>();
   else if (pieces <= 32) f.template operator()<32, 1>();
   else if (pieces <= 64) f.template operator()<64, 1>();
@@ -91,8 +88,7 @@ sp_status sp_ops_create(int device_id, int64_t workspace_bytes, sp_ops** out) {
   if (rc == SP_OK) need(hipHostMalloc((void**)&o->err_host, sizeof(uint32_t), hipHostMallocDefault));
   if (rc == SP_OK) {
     o->ws_bytes = workspace_bytes;
-    o->clip = reinterpret_cast<ClipSum*>(o->err + 16);
-    hipLaunchKernelGGL(k_ops_clear, dim3(1), dim3(1), 0, nullptr, o->err, o->clip);
+    hipLaunchKernelGGL(k_ops_clear, dim3(1), dim3(1), 0, nullptr, o->err);
     need(hipGetLastError());
     need(hipDeviceSynchronize());
   }
@@ -138,15 +134,16 @@ sp_status sp_layer_norm(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const vo
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
   auto run = [&]<typename T>() {
-    const bool fits = with_team((d + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
-      constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
-      const int blocks = std::min((n + rows - 1) / rows, kNormBlocks);
-      hipLaunchKernelGGL((k_norm<T, TEAM, C>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)x, x_stride, gamma,
-                         beta, eps, (T*)y, y_stride, mean_out, rstd_out);
+    with_team((d + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
+      if constexpr (TEAM * C * kPiece<T> <= SP_MAX_NORM_DIM) {
+        constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
+        const int blocks = std::min((n + rows - 1) / rows, kNormBlocks);
+        hipLaunchKernelGGL((k_norm<T, TEAM, C>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)x, x_stride, gamma,
+                           beta, eps, (T*)y, y_stride, mean_out, rstd_out);
+      }
     });
-    return fits;
   };
-  if (!(dtype == SP_F32 ? run.template operator()<float>() : run.template operator()<bf16>())) return SP_ECAPACITY;
+  if (dtype == SP_F32) run.template operator()<float>(); else run.template operator()<bf16>();
   return launched(o);
 }
 
@@ -163,18 +160,20 @@ sp_status sp_layer_norm_backward(sp_ops* o, int32_t n, int32_t d, int32_t dtype,
   if ((n == 0 || !dx) && !sums) return SP_OK;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
-  const int64_t most = o->ws_bytes / (2 * (int64_t)d * (int64_t)sizeof(float));
+  const int64_t most = o->ws_bytes / (norm_part_stride(d) * (int64_t)sizeof(float));
   int parts = 0;
   if (n > 0) {
     auto run = [&]<typename T>() {
-      return with_team((d + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
-        constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
-        parts = (int)std::min<int64_t>({((int64_t)n + rows - 1) / rows, 1024, sums ? most : 1024});
-        hipLaunchKernelGGL((k_norm_back<T, TEAM, C>), dim3(parts), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)dy, dy_stride,
-                           (const T*)x, x_stride, gamma, mean, rstd, (T*)dx, dx_stride, sums ? (float*)o->ws : nullptr);
+      with_team((d + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
+        if constexpr (TEAM * C * kPiece<T> <= SP_MAX_NORM_DIM) {
+          constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
+          parts = (int)std::min<int64_t>({((int64_t)n + rows - 1) / rows, kNormBackBlocks, sums ? most : kNormBackBlocks});
+          hipLaunchKernelGGL((k_norm_back<T, TEAM, C>), dim3(parts), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)dy, dy_stride,
+                             (const T*)x, x_stride, gamma, mean, rstd, (T*)dx, dx_stride, sums ? (float*)o->ws : nullptr);
+        }
       });
     };
-    if (!(dtype == SP_F32 ? run.template operator()<float>() : run.template operator()<bf16>())) return SP_ECAPACITY;
+    if (dtype == SP_F32) run.template operator()<float>(); else run.template operator()<bf16>();
   }
   if (sums)
     hipLaunchKernelGGL(k_norm_join, dim3((2 * d + 31) / 32), dim3(256), 0, (hipStream_t)stream, parts, d, (const float*)o->ws, dgamma,
@@ -218,30 +217,34 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
   if (!o || n_tensors < 0 || !dtype_ok(dtype) || !norm_out || !aligned4(norm_out) || !(max_norm >= 0.f) || !std::isfinite(max_norm))
     return SP_EINVAL;
   if (n_tensors > 0 && (!grads || !sizes)) return SP_EINVAL;
-  int64_t pieces = 0;
+  int64_t total = 0, pieces = 0;
   for (int i = 0; i < n_tensors; ++i) {
     if (sizes[i] < 0 || (sizes[i] > 0 && (!grads[i] || (out && !out[i])))) return SP_EINVAL;
     if (!aligned(grads[i], dtype) || (out && !aligned(out[i], dtype))) return SP_EINVAL;
   }
   for (int i = 0; i < n_tensors; ++i) {
     if (sizes[i] > ((int64_t)1 << 44)) return SP_ECAPACITY;
-    pieces += (sizes[i] + kClipPiece - 1) / kClipPiece;
-    if (pieces > INT_MAX || pieces * (int64_t)sizeof(double) > o->ws_bytes) return SP_ECAPACITY;
+    total += sizes[i];
+    if (total > ((int64_t)1 << 46)) return SP_ECAPACITY;
   }
+  // some 2,000 workgroups share the elements, but none gets less than is worth a workgroup
+  const int piece = (int)std::clamp<int64_t>((total / 2048 + 4095) / 4096 * 4096, kClipPieceMin, kClipPieceMax);
+  for (int i = 0; i < n_tensors; ++i) pieces += (sizes[i] + piece - 1) / piece;
+  if (pieces > INT_MAX || pieces * (int64_t)sizeof(double) > o->ws_bytes) return SP_ECAPACITY;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
   hipStream_t s = (hipStream_t)stream;
+  double* part = (double*)o->ws;
   if (pieces == 0) {
     hipLaunchKernelGGL(k_clip_none, dim3(1), dim3(1), 0, s, norm_out);
     return launched(o);
   }
-  if (o->clip_broken) hipLaunchKernelGGL(k_ops_clear, dim3(1), dim3(1), 0, s, (uint32_t*)nullptr, o->clip);
-  o->clip_broken = true;
   for (int pass = 0; pass < 2; ++pass) {
-    int piece0 = 0;
+    int64_t done = 0;
     for (int at = 0; at < n_tensors;) {
       ClipTable tb;
       tb.count = 0;
+      tb.piece = piece;
       int64_t k = 0;
       for (; at < n_tensors && tb.count < kClipTensors; ++at) {
         if (sizes[at] == 0) continue;
@@ -249,23 +252,21 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
         tb.dst[tb.count] = out ? out[at] : const_cast<void*>(grads[at]);
         tb.size[tb.count] = sizes[at];
         tb.first[tb.count++] = (int32_t)k;
-        k += (sizes[at] + kClipPiece - 1) / kClipPiece;
+        k += (sizes[at] + piece - 1) / piece;
       }
       if (tb.count == 0) continue;
       tb.first[tb.count] = (int32_t)k;
-      if (pass == 0 && dtype == SP_F32)
-        hipLaunchKernelGGL(k_clip_sum<float>, dim3((unsigned)k), dim3(256), 0, s, tb, piece0, (int)pieces, (double*)o->ws, o->clip, max_norm, norm_out);
-      else if (pass == 0)
-        hipLaunchKernelGGL(k_clip_sum<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, piece0, (int)pieces, (double*)o->ws, o->clip, max_norm, norm_out);
+      float* first_norm = done == 0 ? norm_out : nullptr;
+      if (pass == 0 && dtype == SP_F32) hipLaunchKernelGGL(k_clip_sum<float>, dim3((unsigned)k), dim3(256), 0, s, tb, part + done);
+      else if (pass == 0) hipLaunchKernelGGL(k_clip_sum<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, part + done);
       else if (dtype == SP_F32)
-        hipLaunchKernelGGL(k_clip_scale<float>, dim3((unsigned)k), dim3(256), 0, s, tb, (const ClipSum*)o->clip);
+        hipLaunchKernelGGL(k_clip_scale<float>, dim3((unsigned)k), dim3(256), 0, s, tb, (int)pieces, part, max_norm, first_norm);
       else
-        hipLaunchKernelGGL(k_clip_scale<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, (const ClipSum*)o->clip);
+        hipLaunchKernelGGL(k_clip_scale<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, (int)pieces, part, max_norm, first_norm);
       SP_HIP(o, hipGetLastError());
-      piece0 += (int)k;
+      done += k;
     }
   }
-  o->clip_broken = false;
   return SP_OK;
 }
 
@@ -367,7 +368,7 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
       // Rows to a workgroup: so many that about kDwWorkgroups share the work, however the rows are spread over the groups; fewer
       // chunks where the workspace does not hold their sums.
       int64_t chunk = std::max<int64_t>(kDwMinRows, ((int64_t)n * k_tiles * m_tiles + kDwWorkgroups - 1) / kDwWorkgroups);
-      const int64_t most = o->ws_bytes / (((int64_t)k * m + m) * (int64_t)sizeof(float)) - groups;   // chunks: at most n / chunk + groups
+      const int64_t most = o->ws_bytes / (chunk_stride(a) * (int64_t)sizeof(float)) - groups;   // chunks: at most n / chunk + groups
       if (most > 0) chunk = std::max(chunk, (n + most - 1) / most);
       a.chunk = most > 0 && chunk < n ? (int)((chunk + 63) / 64 * 64) : 0;
       a.part = (float*)o->ws;
@@ -378,8 +379,13 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
       }
       if (narrow) launch_linear(k_linear<T, float, kFormDw, 64, MASK>, a, stream);
       else launch_linear(k_linear<T, float, kFormDw, 128, MASK>, a, stream);
-      if (a.chunk)
-        hipLaunchKernelGGL(k_join_chunks, dim3((unsigned)std::min<int64_t>(((int64_t)k * m + m + 255) / 256, 1024), groups), dim3(256), 0, s, a);
+      if (a.chunk) {
+        const int64_t elems = (int64_t)k * m + (db ? m : 0);
+        if ((n + a.chunk - 1) / a.chunk >= 24 * (int64_t)groups)
+          hipLaunchKernelGGL(k_join_chunks<32>, dim3((unsigned)((elems + 31) / 32), groups), dim3(256), 0, s, a);
+        else
+          hipLaunchKernelGGL(k_join_chunks<4>, dim3((unsigned)((elems + 255) / 256), groups), dim3(256), 0, s, a);
+      }
     } else if (db) {
       hipLaunchKernelGGL((k_bias_grad<T>), dim3((m + 63) / 64, groups), dim3(256), 0, s, a);
     }

@@ -1,23 +1,24 @@
 // The norm over all gradients of a model, and the gradients scaled to at most a given norm.
 //   norm = sqrt(sum g^2),  g' = g min(1, max_norm / (norm + 1e-6))
 // Squares are summed in 64 bits (no overflow, and sums over 10^8 values keep their last bits; the adds hide behind the loads).  The
-// tensors come as a table in the kernel's arguments, cut into pieces of kClipPiece elements, one workgroup each; every piece's
-// sum goes to a slot of its own, and the workgroup that ends last adds the slots up in their order: the norm does not depend on the
-// order in which workgroups run.  Bound by memory.
+// tensors come as a table in the kernels' arguments, cut into pieces, one workgroup each.  One pass leaves every piece's sum in a slot of
+// its own; in the next every workgroup adds up all slots, in the same order, and scales its piece: two launches for up to 128
+// tensors, and a norm that does not depend on the order in which workgroups run.  (A counter of ended workgroups instead of the kernel
+// boundary makes every workgroup write its die's L2 back: the sums over 1.2e8 elements took 391 us, now XX.)  Bound by memory.
 #pragma once
 #include "sp_ops_common.h"
 
 namespace sp {
 
 constexpr int kClipTensors = 128;          // to a launch: the table has to fit the kernel's arguments
-constexpr int kClipPiece = 16384;
+constexpr int kClipPieceMin = 8192, kClipPieceMax = 65536;       // elements; see clip_piece
 
 struct ClipTable {
   const void* src[kClipTensors];
   void* dst[kClipTensors];
   int64_t size[kClipTensors];
   int32_t first[kClipTensors + 1];         // each tensor's first piece within the launch
-  int32_t count;
+  int32_t count, piece;                    // tensors, elements of a piece
 };
 
 __device__ __forceinline__ int clip_tensor(const ClipTable& tb, int piece) {
@@ -35,64 +36,80 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
   return v;
 }
 
-// What the launches of a call share in the operators' workspace.
-struct ClipSum {
-  unsigned int ended;                      // pieces that have been summed: 0 between calls
-  float coefficient;
-};
+// The elements of a workgroup's piece.
+template <typename T>
+__device__ __forceinline__ int clip_piece_of(const ClipTable& tb, const T** src, T** dst) {
+  const int k = clip_tensor(tb, (int)blockIdx.x);
+  const int64_t at = (int64_t)((int)blockIdx.x - tb.first[k]) * tb.piece;
+  *src = (const T*)tb.src[k] + at;
+  *dst = (T*)tb.dst[k] + at;
+  return (int)min((int64_t)tb.piece, tb.size[k] - at);
+}
+
+// Sum of a value over the workgroup's four wavefronts, on every thread.
+__device__ __forceinline__ double block_sum_f64(double v, double* waves) {
+  v = wave_sum_f64(v);
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (waves[0] + waves[1]) + (waves[2] + waves[3]);
+}
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_clip_sum(ClipTable tb, int piece0, int pieces, double* __restrict__ part, ClipSum* sum,
-                                                  float max_norm, float* __restrict__ norm_out) {
+__global__ __launch_bounds__(256) void k_clip_sum(ClipTable tb, double* __restrict__ part) {
   constexpr int V = kPiece<T>;
   __shared__ double waves[4];
-  __shared__ bool last;
-  const int k = clip_tensor(tb, (int)blockIdx.x);
-  const int64_t at = (int64_t)((int)blockIdx.x - tb.first[k]) * kClipPiece;
-  const T* src = (const T*)tb.src[k] + at;
-  const int count = (int)min((int64_t)kClipPiece, tb.size[k] - at);
+  const T* src;
+  T* dst;
+  const int count = clip_piece_of(tb, &src, &dst);
   double s = 0.0;
-  for (int i = threadIdx.x * V; i < count; i += 256 * V) {
+  int i = threadIdx.x * V;
+  for (; i + 3 * 256 * V + V <= count; i += 4 * 256 * V) {           // four loads under way
+    float v[4][V];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load_piece(src + i + u * 256 * V, v[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int j = 0; j < V; ++j) s += (double)v[u][j] * (double)v[u][j];
+  }
+  for (; i < count; i += 256 * V) {
     float v[V];
     load_some(src + i, count - i, 0.f, v);
 #pragma unroll
     for (int j = 0; j < V; ++j) s += (double)v[j] * (double)v[j];
   }
-  s = wave_sum_f64(s);
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    s = (waves[0] + waves[1]) + (waves[2] + waves[3]);
-    __hip_atomic_store(part + piece0 + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(&sum->ended, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)pieces - 1u;
-  }
-  __syncthreads();
-  if (!last) return;
-  double all = 0.0;
-  for (int i = threadIdx.x; i < pieces; i += 256)
-    all += __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  all = wave_sum_f64(all);
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = all;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const double norm = sqrt((waves[0] + waves[1]) + (waves[2] + waves[3]));
-    *norm_out = (float)norm;
-    const double c = (double)max_norm / (norm + 1e-6);
-    sum->coefficient = c > 1.0 ? 1.f : (float)c;         // (a norm that is no number leaves none behind either)
-    sum->ended = 0u;
-  }
+  s = block_sum_f64(s, waves);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_clip_scale(ClipTable tb, const ClipSum* __restrict__ sum) {
+__global__ __launch_bounds__(256) void k_clip_scale(ClipTable tb, int pieces, const double* __restrict__ part, float max_norm,
+                                                    float* __restrict__ norm_out) {
   constexpr int V = kPiece<T>;
-  const int k = clip_tensor(tb, (int)blockIdx.x);
-  const int64_t at = (int64_t)((int)blockIdx.x - tb.first[k]) * kClipPiece;
-  const T* src = (const T*)tb.src[k] + at;
-  T* dst = (T*)tb.dst[k] + at;
-  const int count = (int)min((int64_t)kClipPiece, tb.size[k] - at);
-  const float c = sum->coefficient;
-  for (int i = threadIdx.x * V; i < count; i += 256 * V) {
+  __shared__ double waves[4];
+  double all = 0.0;
+  for (int i = threadIdx.x; i < pieces; i += 256) all += part[i];
+  const double norm = sqrt(block_sum_f64(all, waves));
+  if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+  const double ratio = (double)max_norm / (norm + 1e-6);
+  const float c = ratio > 1.0 ? 1.f : (float)ratio;        // (a norm that is no number leaves none behind either)
+  const T* src;
+  T* dst;
+  const int count = clip_piece_of(tb, &src, &dst);
+  if (c == 1.f && src == dst) return;                      // stays as it is
+  int i = threadIdx.x * V;
+  for (; i + 3 * 256 * V + V <= count; i += 4 * 256 * V) {
+    float v[4][V];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load_piece(src + i + u * 256 * V, v[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[u][j] *= c;
+      store_piece(dst + i + u * 256 * V, v[u]);
+    }
+  }
+  for (; i < count; i += 256 * V) {
     float v[V];
     load_some(src + i, count - i, 0.f, v);
 #pragma unroll

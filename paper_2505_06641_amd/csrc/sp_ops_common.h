@@ -92,13 +92,16 @@ __device__ __forceinline__ void store_some(T* p, int count, const float (&v)[V])
   }
 }
 
-// Sum and maximum over a team: TEAM consecutive lanes of a wavefront (8, 16, 32, 64), or the TEAM > 64 threads of a
+// Sum and maximum over a team: TEAM consecutive lanes of a wavefront (2 to 64), or the TEAM > 64 threads of a
 // workgroup.  Every lane of the team has the result, and every lane adds in the same order.  `lds`: one float per
 // wavefront; two reductions that follow each other take different arrays.
 template <int TEAM>
 __device__ __forceinline__ float team_sum(float v, float* lds) {
-  static_assert(TEAM == 8 || TEAM == 16 || TEAM == 32 || TEAM % 64 == 0, "teams are parts of a wavefront or whole ones");
-  v = TEAM == 8 ? sum8(v) : sum16(v);
+  static_assert(TEAM == 2 || TEAM == 4 || TEAM == 8 || TEAM == 16 || TEAM == 32 || TEAM % 64 == 0, "parts of a wavefront or whole ones");
+  if (TEAM == 2) v += __shfl_xor(v, 1);
+  else if (TEAM == 4) v = sum4(v);
+  else if (TEAM == 8) v = sum8(v);
+  else v = sum16(v);
   if (TEAM >= 32) v += __shfl_xor(v, 16);
   if (TEAM >= 64) v += __shfl_xor(v, 32);
   if (TEAM > 64) {

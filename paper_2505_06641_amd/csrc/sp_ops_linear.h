@@ -48,8 +48,11 @@ struct LinearArgs {
   uint32_t* err;
   int row_tiles, col_tiles;              // of the launch (dW: tiles of k and of m)
   int chunk;                             // dW: rows of a group that a workgroup adds up, 0: all of them
-  float* part;                           // dW: [chunks, k * m + m] sums of the chunks
+  float* part;                           // dW: sums of the chunks, [chunks][k * m + m]
 };
+
+// Elements from one chunk's sums (dW, then db) to the next: whole 16-byte pieces.
+__host__ __device__ __forceinline__ int64_t chunk_stride(const LinearArgs& a) { return ((int64_t)a.k * a.m + a.m + 3) / 4 * 4; }
 
 enum LinearForm { kFormY = 0, kFormDx = 1, kFormDw = 2 };
 
@@ -114,8 +117,10 @@ struct Side {
   u32x4 raw[kPieces];
   u32x4 act[MASK ? kPieces : 1];
 
-  // base: element (first row, depth 0) of a contiguous side, (depth 0, first column) of a strided one.
-  __device__ __forceinline__ void load(const T* base, int64_t stride, const T* act_base, int64_t act_stride, int valid, int t0, int depth) {
+  // base: element (first row, depth 0) of a contiguous side, (depth 0, first column) of a strided one; limit: elements from base to the
+  // end of the array.  A piece that reaches beyond the tile or the depth is read as far as the array goes and cut to what it may hold.
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t limit, const T* act_base, int64_t act_stride, int64_t act_limit,
+                                       int valid, int t0, int depth) {
     if (valid >= W && t0 + D <= depth) {
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
@@ -133,17 +138,23 @@ struct Side {
         const int col = STRIDED ? minor : t0 + minor;
         const bool in = STRIDED ? t0 + major < depth : major < valid;
         const int count = in ? (STRIDED ? valid : depth) - col : 0;
-        raw[i] = u32x4{0, 0, 0, 0};
-        if (MASK) act[i] = u32x4{0, 0, 0, 0};
-        if (count >= V) {
-          raw[i] = load_raw(base + row * stride + col);
-          if (MASK) act[i] = load_raw(act_base + row * act_stride + col);
-        } else if (count > 0) {
-          raw[i] = load_raw_some(base + row * stride + col, count);
-          if (MASK) act[i] = load_raw_some(act_base + row * act_stride + col, count);
-        }
+        raw[i] = load_cut(base, row * stride + col, limit, count);
+        if (MASK) act[i] = load_cut(act_base, row * act_stride + col, act_limit, count);
       }
     }
+  }
+  __device__ __forceinline__ static u32x4 load_cut(const T* base, int64_t at, int64_t limit, int count) {
+    u32x4 q = {0, 0, 0, 0};
+    if (count <= 0) return q;
+    if (count < V && at + V > limit) return load_raw_some(base + at, count);
+    q = load_raw(base + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int left = count - i * (V / 4);
+      if constexpr (V == 4) q[i] = left > 0 ? q[i] : 0u;
+      else q[i] &= left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
+    }
+    return q;
   }
 
   __device__ __forceinline__ static int place(int major, int minor) {     // element of a plane, minor a multiple of 4
@@ -207,7 +218,7 @@ struct Side {
 
 // Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, two by two: 64 rows and BN / 2 columns each.
 template <typename T, typename TO, int FORM, int BN, bool MASK>
-__global__ __launch_bounds__(kLinearThreads, FORM == kFormDw ? 2 : 3) void k_linear(LinearArgs a) {
+__global__ __launch_bounds__(kLinearThreads, BN == 128 ? 2 : 3) void k_linear(LinearArgs a) {
   constexpr int BM = kLinearRows, D = kDepth<T>, P = kPlanes<T>, FR = 2, FC = BN / 64, V = kPiece<T>;
   typedef Side<T, BM, FORM == kFormDw, FORM == kFormDx && MASK> Rows;
   typedef Side<T, BN, FORM != kFormDx, FORM == kFormDw && MASK> Cols;
@@ -245,6 +256,7 @@ __global__ __launch_bounds__(kLinearThreads, FORM == kFormDw ? 2 : 3) void k_lin
   }
   const T* x = (const T*)a.x;
   const T* w = (const T*)a.w + (int64_t)(FORM != kFormDw ? min(rows.g, a.groups - 1) : 0) * a.k * a.m;
+  const int64_t w_left = (int64_t)(a.groups - min(rows.g, a.groups - 1)) * a.k * a.m;       // elements from there on
   const T* dy = (const T*)a.dy;
   const T* act = (const T*)a.act;
 
@@ -252,15 +264,17 @@ __global__ __launch_bounds__(kLinearThreads, FORM == kFormDw ? 2 : 3) void k_lin
   Cols sc;
   auto load = [&](int t0) {
     if (FORM == kFormY) {
-      sr.load(x + (int64_t)r0 * a.x_stride, a.x_stride, nullptr, 0, n_rows, t0, depth);
-      sc.load(w + c0, a.m, nullptr, 0, width - c0, t0, depth);
+      sr.load(x + (int64_t)r0 * a.x_stride, a.x_stride, (int64_t)(a.n - 1 - r0) * a.x_stride + a.k, nullptr, 0, 0, n_rows, t0, depth);
+      sc.load(w + c0, a.m, w_left - c0, nullptr, 0, 0, width - c0, t0, depth);
     } else if (FORM == kFormDx) {
-      sr.load(dy + (int64_t)r0 * a.dy_stride, a.dy_stride, act + (int64_t)r0 * a.act_stride, a.act_stride, n_rows, t0, depth);
-      sc.load(w + (int64_t)c0 * a.m, a.m, nullptr, 0, width - c0, t0, depth);
+      sr.load(dy + (int64_t)r0 * a.dy_stride, a.dy_stride, (int64_t)(a.n - 1 - r0) * a.dy_stride + a.m, act + (int64_t)r0 * a.act_stride,
+              a.act_stride, (int64_t)(a.n - 1 - r0) * a.act_stride + a.m, n_rows, t0, depth);
+      sc.load(w + (int64_t)c0 * a.m, a.m, w_left - (int64_t)c0 * a.m, nullptr, 0, 0, width - c0, t0, depth);
     } else {
-      sr.load(x + (int64_t)rows.lo * a.x_stride + r0, a.x_stride, nullptr, 0, n_rows, t0, depth);
-      sc.load(dy + (int64_t)rows.lo * a.dy_stride + c0, a.dy_stride, act + (int64_t)rows.lo * a.act_stride + c0, a.act_stride, width - c0,
-              t0, depth);
+      const int64_t below = a.n - 1 - rows.lo;
+      sr.load(x + (int64_t)rows.lo * a.x_stride + r0, a.x_stride, below * a.x_stride + a.k - r0, nullptr, 0, 0, n_rows, t0, depth);
+      sc.load(dy + (int64_t)rows.lo * a.dy_stride + c0, a.dy_stride, below * a.dy_stride + a.m - c0,
+              act + (int64_t)rows.lo * a.act_stride + c0, a.act_stride, below * a.act_stride + a.m - c0, width - c0, t0, depth);
     }
   };
 
@@ -337,7 +351,7 @@ __global__ __launch_bounds__(kLinearThreads, FORM == kFormDw ? 2 : 3) void k_lin
         for (int e = 0; e < 4; ++e) v[4 * h + e] = f[e];
       }
       if (FORM == kFormDw) {
-        float* out = slot < 0 ? a.dw + (int64_t)rows.g * a.k * a.m : a.part + slot * ((int64_t)a.k * a.m + a.m);
+        float* out = slot < 0 ? a.dw + (int64_t)rows.g * a.k * a.m : a.part + slot * chunk_stride(a);
         store_some(out + row * a.m + c, left, v);
       } else if (FORM == kFormDx) {
         store_some((TO*)a.dx + row * a.dx_stride + c, left, v);
@@ -376,18 +390,23 @@ __global__ __launch_bounds__(kLinearThreads, FORM == kFormDw ? 2 : 3) void k_lin
     if (threadIdx.x < BN && c < a.m) {
       float v = 0.f;
       for (int u = 0; u < same; ++u) v += s[u * BN + threadIdx.x];
-      float* out = slot < 0 ? a.db + (int64_t)rows.g * a.m : a.part + slot * ((int64_t)a.k * a.m + a.m) + (int64_t)a.k * a.m;
+      float* out = slot < 0 ? a.db + (int64_t)rows.g * a.m : a.part + slot * chunk_stride(a) + (int64_t)a.k * a.m;
       out[c] = v;
     }
   }
 }
 
-// Adds up the chunks of the groups that have several, in their order, and clears the gradients of the empty groups.
+// Adds up the chunks of the groups that have several, and clears the gradients of the empty groups.  A workgroup takes 4 elements of
+// the gradient for each of its 256 / SLICES columns of threads; SLICES threads share out an element's chunks (many where there are many
+// chunks, so that their loads are under way together), and their sums meet in LDS, in a fixed order.
+template <int SLICES>
 __global__ __launch_bounds__(256) void k_join_chunks(LinearArgs a) {
+  constexpr int kAcross = 256 / SLICES;
+  __shared__ f32x4 sums[SLICES][kAcross];
   const int g = blockIdx.y;
-  const int64_t km = (int64_t)a.k * a.m, all = km + (a.db ? a.m : 0);
+  const int64_t km = (int64_t)a.k * a.m, stride = chunk_stride(a), all = km + (a.db ? a.m : 0);
   // the chunks of the groups before this one, and its own
-  int lo, hi, end = 0, before = 0;
+  int lo = 0, hi = 0, end = 0, before = 0;
   const int lane = threadIdx.x & 63;
   for (int base = 0; base <= g; base += 64) {
     const int q = base + lane;
@@ -410,10 +429,22 @@ __global__ __launch_bounds__(256) void k_join_chunks(LinearArgs a) {
     end = __shfl(e, 63);
   }
   if (hi - lo == 1) return;                                // written by the one chunk's workgroups
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-    float v = 0.f;
-    for (int s = lo; s < hi; ++s) v += a.part[s * (km + a.m) + i];
-    if (i < km) a.dw[g * km + i] = v; else a.db[(int64_t)g * a.m + i - km] = v;
+  const int col = threadIdx.x % kAcross, slice = threadIdx.x / kAcross;
+  const int64_t at = ((int64_t)blockIdx.x * kAcross + col) * 4;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (at < all) {                                          // (what lies behind the sums is never looked at)
+#pragma unroll 4
+    for (int s = lo + slice; s < hi; s += SLICES) v += *reinterpret_cast<const f32x4*>(a.part + s * stride + at);
+  }
+  sums[slice][col] = v;
+  __syncthreads();
+  if (slice > 0) return;
+  for (int s = 1; s < SLICES; ++s) v += sums[s][col];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int64_t i = at + e;
+    if (i >= all) break;
+    if (i < km) a.dw[g * km + i] = v[e]; else a.db[(int64_t)g * a.m + i - km] = v[e];
   }
 }
 

@@ -8,8 +8,11 @@
 
 namespace sp {
 
-constexpr int kNormDimMax = 16384;          // a workgroup of 1024 threads with 16 elements each
 constexpr int kNormBlocks = 2048;           // workgroups that share out the rows of a forward pass
+constexpr int kNormBackBlocks = 1024;       // and of a backward pass, each with a row of sums of its own to be added up
+
+// Elements from one row of partial sums to the next: whole 16-byte pieces.
+__host__ __device__ __forceinline__ int64_t norm_part_stride(int d) { return (2 * (int64_t)d + 3) / 4 * 4; }
 
 // A team's columns: piece c of lane t holds columns (c * TEAM + t) * V on.
 template <typename T, int TEAM, int C>
@@ -66,8 +69,9 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm(int n, int d, const
   }
 }
 
-// Every team walks its rows with dgamma's and dbeta's sums of its columns in registers; the workgroup's teams add theirs up in LDS,
-// one after the other, and write one row of partial sums: part[workgroup][2][d].
+// Every team walks its rows with dgamma's and dbeta's sums of its columns in registers; the workgroup's teams add theirs up,
+// those of a wavefront across lanes and the wavefronts one after the other in LDS, and write one row of partial sums:
+// part[workgroup][2][d], each row of them at a 16-byte piece.
 template <typename T, int TEAM, int C>
 __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, const T* dy, int64_t dy_stride,
                                                                   const T* x, int64_t x_stride,
@@ -76,7 +80,7 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, 
                                                                   float* __restrict__ part) {
   constexpr int V = kPiece<T>, ROWS = kTeamThreads<TEAM> / TEAM;
   __shared__ float red[2][TEAM > 64 ? TEAM / 64 : 1];
-  __shared__ float sums[ROWS > 1 ? TEAM * C * V : 1][2];
+  __shared__ float sums[TEAM <= 64 ? TEAM * C * V : 1][2];
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   float ga[C][V], dg[C][V], db[C][V];
 #pragma unroll
@@ -91,12 +95,15 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, 
   for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS) {
     float g[C][V], xh[C][V];
     const float mu = mean[row], rs = rstd[row];
-    float sq = 0.f, sqx = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = (c * TEAM + t) * V;
       load_some(dy + row * dy_stride + col, d - col, 0.f, g[c]);
-      load_some(x + row * x_stride + col, d - col, mu, xh[c]);     // (columns beyond the row: xh = 0, dy = 0)
+      load_some(x + row * x_stride + col, d - col, mu, xh[c]);       // (columns beyond the row: xh = 0, dy = 0)
+    }
+    float sq = 0.f, sqx = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         xh[c][i] = (xh[c][i] - mu) * rs;
@@ -106,7 +113,6 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, 
         sq += g[c][i];
         sqx += g[c][i] * xh[c][i];
       }
-    }
     if (!dx) continue;
     const float mq = team_sum<TEAM>(sq, red[0]) / fd, mqx = team_sum<TEAM>(sqx, red[1]) / fd;
 #pragma unroll
@@ -118,23 +124,34 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, 
     }
   }
   if (!part) return;
-  if (ROWS > 1) {
-    for (int turn = 0; turn < ROWS; ++turn) {
-      if (turn == team) {
+  if (TEAM <= 64) {
+    constexpr int WAVES = kTeamThreads<TEAM> / 64;
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int s = TEAM; s < 64; s *= 2) {
+          dg[c][i] += __shfl_xor(dg[c][i], s);
+          db[c][i] += __shfl_xor(db[c][i], s);
+        }
+    for (int turn = 0; turn < WAVES; ++turn) {
+      if (turn == wave && (threadIdx.x & 63) < TEAM) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             float* at = sums[(c * V + i) * TEAM + t];
             if (turn > 0) { dg[c][i] += at[0]; db[c][i] += at[1]; }
-            if (turn < ROWS - 1) { at[0] = dg[c][i]; at[1] = db[c][i]; }
+            if (turn < WAVES - 1) { at[0] = dg[c][i]; at[1] = db[c][i]; }
           }
       }
       __syncthreads();
     }
-    if (team != ROWS - 1) return;
+    if (wave != WAVES - 1 || (threadIdx.x & 63) >= TEAM) return;
   }
-  float* out = part + (int64_t)blockIdx.x * 2 * d;
+  float* out = part + blockIdx.x * norm_part_stride(d);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int col = (c * TEAM + t) * V;
@@ -143,21 +160,27 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, 
   }
 }
 
-// Sums of the workgroups' rows of partial sums: 32 columns to a workgroup of 256, eight threads to a column.
+// Sums of the workgroups' rows of partial sums: 32 columns to a workgroup of 256, 32 threads to 4 columns, their loads under way
+// together (one thread that adds 128 rows one after the other takes 30 us).
 __global__ __launch_bounds__(256) void k_norm_join(int parts, int d, const float* __restrict__ part, float* __restrict__ dgamma,
                                                    float* __restrict__ dbeta) {
-  __shared__ float sums[8][33];
-  const int lane = threadIdx.x % 32, slice = threadIdx.x / 32;
-  const int col = blockIdx.x * 32 + lane;              // of 2 d
-  float s = 0.f;
-  if (col < 2 * d)
-    for (int p = slice; p < parts; p += 8) s += part[(int64_t)p * 2 * d + col];
+  __shared__ f32x4 sums[32][8];
+  const int lane = threadIdx.x % 8, slice = threadIdx.x / 8;
+  const int64_t cols = 2 * (int64_t)d, stride = norm_part_stride(d), col = (int64_t)blockIdx.x * 32 + lane * 4;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (col < cols) {
+#pragma unroll 8
+    for (int p = slice; p < parts; p += 32) s += *reinterpret_cast<const f32x4*>(part + p * stride + col);
+  }
   sums[slice][lane] = s;
   __syncthreads();
-  if (slice == 0 && col < 2 * d) {
-    for (int j = 1; j < 8; ++j) s += sums[j][lane];
-    float* out = col < d ? dgamma : dbeta;
-    if (out) out[col < d ? col : col - d] = s;
+  if (slice > 0) return;
+  for (int j = 1; j < 32; ++j) s += sums[j][lane];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int64_t c = col + e;
+    float* out = c < d ? dgamma : dbeta;
+    if (c < cols && out) out[c < d ? c : c - d] = s[e];
   }
 }
 
