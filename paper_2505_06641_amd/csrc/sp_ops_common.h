@@ -163,16 +163,16 @@ __device__ __forceinline__ bool find_row_tile(const int32_t* offsets, int n_grou
     const int upto = before + (int)wave_scan_incl((uint32_t)tiles);
     const unsigned long long has = __ballot(upto > tile);
     if (has) {
-      const int l = __ffsll(has) - 1;
-      const int first = __shfl(s0 + (tile - (upto - tiles)) * tile_rows, l), last = __shfl(e, l);
+      const int l = __ffsll(has) - 1;            // (scalars from here on: the same on every lane, and known to be)
+      const int first = __builtin_amdgcn_readlane(s0 + (tile - (upto - tiles)) * tile_rows, l), last = __builtin_amdgcn_readlane(e, l);
       out->g = base + l;
       out->lo = first;
       out->hi = last - first < tile_rows ? last : first + tile_rows;
-      out->whole = __shfl(tiles, l) == 1;
+      out->whole = __builtin_amdgcn_readlane(tiles, l) == 1;
       return true;
     }
-    before = __shfl(upto, 63);
-    end = __shfl(e, 63);
+    before = __builtin_amdgcn_readlane(upto, 63);
+    end = __builtin_amdgcn_readlane(e, 63);
   }
   return false;
 }

@@ -64,23 +64,19 @@ template <typename T> constexpr int kDepth = sizeof(T) == 4 ? 32 : 64; // depth 
 // Where NaN has to stay NaN: only what is below 0 becomes 0.
 __device__ __forceinline__ float relu_of(float z) { return z < 0.f ? 0.f : z; }
 
-__device__ __forceinline__ u32x4 load_raw(const void* p) {
-  const u32x4_any q = *reinterpret_cast<const u32x4_any*>(p);
-  return u32x4{q[0], q[1], q[2], q[3]};
-}
+// The first `count` elements of a piece, one by one (at the very end of an array; few registers matter more here than time).
 __device__ __forceinline__ u32x4 load_raw_some(const float* p, int count) {
   u32x4 q = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < count) q[i] = __float_as_uint(p[i]);
+#pragma unroll 1
+  for (int i = count - 1; i >= 0; --i) q = u32x4{__float_as_uint(p[i]), q[0], q[1], q[2]};
   return q;
 }
 __device__ __forceinline__ u32x4 load_raw_some(const bf16* p, int count) {
   const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
   u32x4 q = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < count) q[i / 2] |= (uint32_t)h[i] << (16 * (i % 2));
+#pragma unroll 1
+  for (int i = count - 1; i >= 0; --i)
+    q = u32x4{q[0] << 16 | h[i], q[1] << 16 | q[0] >> 16, q[2] << 16 | q[1] >> 16, q[3] << 16 | q[2] >> 16};
   return q;
 }
 // dz: dy where act is not <= 0 (as the comparison has it, NaN passes).
@@ -117,44 +113,58 @@ struct Side {
   u32x4 raw[kPieces];
   u32x4 act[MASK ? kPieces : 1];
 
-  // base: element (first row, depth 0) of a contiguous side, (depth 0, first column) of a strided one; limit: elements from base to the
-  // end of the array.  A piece that reaches beyond the tile or the depth is read as far as the array goes and cut to what it may hold.
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t limit, const T* act_base, int64_t act_stride, int64_t act_limit,
-                                       int valid, int t0, int depth) {
-    if (valid >= W && t0 + D <= depth) {
+  uint32_t off, act_off;                                            // bytes from the piece of the depth's first element
+  int64_t step, act_step;                                           // elements from one of a thread's pieces to the next
+  static constexpr int kStep = kLinearThreads / kAcross;            // the same in rows
+
+  __device__ __forceinline__ void init(int64_t stride, int64_t act_stride) {
+    const uint32_t major = threadIdx.x / kAcross, minor = (threadIdx.x % kAcross) * V;
+    off = (major * (uint32_t)stride + minor) * (uint32_t)sizeof(T);
+    act_off = (major * (uint32_t)act_stride + minor) * (uint32_t)sizeof(T);
+    step = kStep * stride;
+    act_step = kStep * act_stride;
+  }
+  // at: that element.  Where everything lies inside the tile and the depth:
+  __device__ __forceinline__ void load(const T* at, const T* act_at) {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int p = threadIdx.x + i * kLinearThreads, major = p / kAcross, minor = (p % kAcross) * V;
-        const int64_t row = STRIDED ? t0 + major : major;
-        const int col = STRIDED ? minor : t0 + minor;
-        raw[i] = load_raw(base + row * stride + col);
-        if (MASK) act[i] = load_raw(act_base + row * act_stride + col);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int p = threadIdx.x + i * kLinearThreads, major = p / kAcross, minor = (p % kAcross) * V;
-        const int64_t row = STRIDED ? t0 + major : major;
-        const int col = STRIDED ? minor : t0 + minor;
-        const bool in = STRIDED ? t0 + major < depth : major < valid;
-        const int count = in ? (STRIDED ? valid : depth) - col : 0;
-        raw[i] = load_cut(base, row * stride + col, limit, count);
-        if (MASK) act[i] = load_cut(act_base, row * act_stride + col, act_limit, count);
-      }
+    for (int i = 0; i < kPieces; ++i) {
+      raw[i] = load_raw(at + i * step, off);
+      if (MASK) act[i] = load_raw(act_at + i * act_step, act_off);
     }
   }
-  __device__ __forceinline__ static u32x4 load_cut(const T* base, int64_t at, int64_t limit, int count) {
-    u32x4 q = {0, 0, 0, 0};
-    if (count <= 0) return q;
-    if (count < V && at + V > limit) return load_raw_some(base + at, count);
-    q = load_raw(base + at);
+  // ... and where it does not.  limit: elements from `at` to the array's end (where its last row ends); valid rows (columns) and depth
+  // are what is left of them.  A piece that reaches beyond what is left is read as far as the array goes, and cut later.
+  __device__ __forceinline__ void load_edge(const T* at, int64_t limit, const T* act_at, int64_t act_limit, int valid, int depth) {
+    const int major = threadIdx.x / kAcross, minor = (threadIdx.x % kAcross) * V;
+    const int rows = STRIDED ? depth : valid, cols = STRIDED ? valid : depth;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int left = count - i * (V / 4);
-      if constexpr (V == 4) q[i] = left > 0 ? q[i] : 0u;
-      else q[i] &= left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
+    for (int i = 0; i < kPieces; ++i) {
+      const int count = major + i * kStep < rows ? cols - minor : 0;
+      raw[i] = load_cut(at + i * step, off, limit - i * step, count);
+      if (MASK) act[i] = load_cut(act_at + i * act_step, act_off, act_limit - i * act_step, count);
     }
-    return q;
+  }
+  __device__ __forceinline__ static u32x4 load_raw(const T* base, uint32_t off) {
+    const u32x4_any q = *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const char*>(base) + off);
+    return u32x4{q[0], q[1], q[2], q[3]};
+  }
+  __device__ __forceinline__ static u32x4 load_cut(const T* base, uint32_t off, int64_t limit, int count) {
+    if (count <= 0) return u32x4{0, 0, 0, 0};
+    if (count < V && (int64_t)off + 16 > limit * (int64_t)sizeof(T))
+      return load_raw_some(reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + off), count);
+    return load_raw(base, off);
+  }
+  // (Apart from the load, so that no piece's load is waited for before the next one's is under way.)
+  __device__ __forceinline__ void cut(int valid, int depth) {
+    const int minor = (threadIdx.x % kAcross) * V, cols = STRIDED ? valid : depth;
+    if (valid >= W && depth >= D) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int left = cols - minor - j * (V / 4);                  // (pieces of rows beyond the last are 0 already)
+      const uint32_t keep = V == 4 ? (left > 0 ? 0xffffffffu : 0u) : left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) raw[i][j] &= keep;
+    }
   }
 
   __device__ __forceinline__ static int place(int major, int minor) {     // element of a plane, minor a multiple of 4
@@ -218,7 +228,7 @@ struct Side {
 
 // Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, two by two: 64 rows and BN / 2 columns each.
 template <typename T, typename TO, int FORM, int BN, bool MASK>
-__global__ __launch_bounds__(kLinearThreads, BN == 128 ? 2 : 3) void k_linear(LinearArgs a) {
+__global__ __launch_bounds__(kLinearThreads, MASK ? 2 : 3) void k_linear(LinearArgs a) {
   constexpr int BM = kLinearRows, D = kDepth<T>, P = kPlanes<T>, FR = 2, FC = BN / 64, V = kPiece<T>;
   typedef Side<T, BM, FORM == kFormDw, FORM == kFormDx && MASK> Rows;
   typedef Side<T, BN, FORM != kFormDx, FORM == kFormDw && MASK> Cols;
@@ -262,19 +272,50 @@ __global__ __launch_bounds__(kLinearThreads, BN == 128 ? 2 : 3) void k_linear(Li
 
   Rows sr;
   Cols sc;
-  auto load = [&](int t0) {
+  if (FORM == kFormY) {
+    sr.init(a.x_stride, 0);
+    sc.init(a.m, 0);
+  } else if (FORM == kFormDx) {
+    sr.init(a.dy_stride, a.act_stride);
+    sc.init(a.m, 0);
+  } else {
+    sr.init(a.x_stride, 0);
+    sc.init(a.dy_stride, a.act_stride);
+  }
+  const bool inside = n_rows >= BM && width - c0 >= BN;
+  auto load = [&](int t0, bool edge) {
+    const T *pr, *pc, *qr = nullptr, *qc = nullptr;
+    int64_t end_r, end_c, qend_r = 0, qend_c = 0;
     if (FORM == kFormY) {
-      sr.load(x + (int64_t)r0 * a.x_stride, a.x_stride, (int64_t)(a.n - 1 - r0) * a.x_stride + a.k, nullptr, 0, 0, n_rows, t0, depth);
-      sc.load(w + c0, a.m, w_left - c0, nullptr, 0, 0, width - c0, t0, depth);
+      pr = x + (int64_t)r0 * a.x_stride + t0;
+      end_r = (int64_t)(a.n - 1 - r0) * a.x_stride + a.k - t0;
+      const int64_t skip = (int64_t)t0 * a.m + c0;
+      pc = w + skip;
+      end_c = w_left - skip;
     } else if (FORM == kFormDx) {
-      sr.load(dy + (int64_t)r0 * a.dy_stride, a.dy_stride, (int64_t)(a.n - 1 - r0) * a.dy_stride + a.m, act + (int64_t)r0 * a.act_stride,
-              a.act_stride, (int64_t)(a.n - 1 - r0) * a.act_stride + a.m, n_rows, t0, depth);
-      sc.load(w + (int64_t)c0 * a.m, a.m, w_left - (int64_t)c0 * a.m, nullptr, 0, 0, width - c0, t0, depth);
+      const int64_t below = a.n - 1 - r0;
+      pr = dy + (int64_t)r0 * a.dy_stride + t0;
+      end_r = below * a.dy_stride + a.m - t0;
+      qr = act + (int64_t)r0 * a.act_stride + t0;
+      qend_r = below * a.act_stride + a.m - t0;
+      const int64_t skip = (int64_t)c0 * a.m + t0;
+      pc = w + skip;
+      end_c = w_left - skip;
     } else {
-      const int64_t below = a.n - 1 - rows.lo;
-      sr.load(x + (int64_t)rows.lo * a.x_stride + r0, a.x_stride, below * a.x_stride + a.k - r0, nullptr, 0, 0, n_rows, t0, depth);
-      sc.load(dy + (int64_t)rows.lo * a.dy_stride + c0, a.dy_stride, below * a.dy_stride + a.m - c0,
-              act + (int64_t)rows.lo * a.act_stride + c0, a.act_stride, below * a.act_stride + a.m - c0, width - c0, t0, depth);
+      const int64_t row = rows.lo + t0, below = a.n - 1 - row;
+      pr = x + row * a.x_stride + r0;
+      end_r = below * a.x_stride + a.k - r0;
+      pc = dy + row * a.dy_stride + c0;
+      end_c = below * a.dy_stride + a.m - c0;
+      qc = act + row * a.act_stride + c0;
+      qend_c = below * a.act_stride + a.m - c0;
+    }
+    if (edge) {
+      sr.load_edge(pr, end_r, qr, qend_r, n_rows, depth - t0);
+      sc.load_edge(pc, end_c, qc, qend_c, width - c0, depth - t0);
+    } else {
+      sr.load(pr, qr);
+      sc.load(pc, qc);
     }
   };
 
@@ -290,13 +331,13 @@ __global__ __launch_bounds__(kLinearThreads, BN == 128 ? 2 : 3) void k_linear(Li
   const bool sum_columns = FORM == kFormDw && a.db && r0 == 0;
   float sums[V] = {};
 
-  if (depth > 0) load(0);
-  for (int t0 = 0; t0 < depth; t0 += D) {
+  auto store = [&]() {
     sr.store(lds_rows);
     sc.store(lds_cols);
     if (FORM == kFormDw && sum_columns) sc.add_columns(sums);
     __syncthreads();
-    if (t0 + D < depth) load(t0 + D);
+  };
+  auto multiply = [&]() {
 #pragma unroll
     for (int step = 0; step < D / 16; ++step) {
       bf16x8 fr[FR][P], fc[FC][P];
@@ -317,6 +358,25 @@ __global__ __launch_bounds__(kLinearThreads, BN == 128 ? 2 : 3) void k_linear(Li
             for (int j = 0; j < FC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fc[j][q], fr[i][p], acc[i][j], 0, 0, 0);
     }
     __syncthreads();
+  };
+  // Inside the tile and the depth no piece is cut; the loop for the others has branches and registers that would slow this one down.
+  int t0 = 0;
+  if (inside && depth >= D) {
+    load(0, false);
+    for (; t0 + 2 * D <= depth; t0 += D) {
+      store();
+      load(t0 + D, false);
+      multiply();
+    }
+  } else if (depth > 0) {
+    load(0, true);
+  }
+  for (; t0 < depth; t0 += D) {
+    sr.cut(n_rows, depth - t0);
+    sc.cut(width - c0, depth - t0);
+    store();
+    if (t0 + D < depth) load(t0 + D, true);
+    multiply();
   }
 
   // Sums to memory by way of LDS, 64 rows at a time, so that whole lines are read and written: lane l has row l % 32 of a 32 x 32
