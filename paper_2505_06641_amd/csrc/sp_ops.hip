@@ -12,6 +12,7 @@
 #include "sp_ops_clip.h"
 #include "sp_ops_common.h"
 #include "sp_ops_linear.h"
+#include "sp_ops_linear_few.h"
 #include "sp_ops_loss.h"
 #include "sp_ops_norm.h"
 
@@ -274,8 +275,27 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
 
 namespace {
 
-constexpr int kDwWorkgroups = 1024;        // four to a compute unit
-constexpr int kDwMinRows = 256;
+// Whether a layer is better off in pieces of 16 rows than in tiles of 128: as long as the device holds about all of the small pieces'
+// workgroups at once, their shorter way through the depth wins (bfloat16 1024 -> 1024: 512 rows 15 us against 17, 1024 rows 24 against 17;
+// float32: 1024 rows 52 against 66, 2048 rows 93 against 67; 512 -> 256 of one request: 5 against 14).
+bool few_rows(int64_t n, int64_t width, int cols, int64_t groups, int32_t dtype) {
+  const int64_t workgroups = ((n + kFewRows - 1) / kFewRows + std::min(n, groups)) * ((width + cols - 1) / cols);
+  return workgroups <= (dtype == SP_F32 ? 2560 : 1280);
+}
+
+// Rows of a group that one workgroup adds up for dW (0: all).  A workgroup takes about 19 ns a row (float32 55 ns), and every chunk's
+// sums are written and read again at about 4 TB/s: the number of rows at which both cost the same, but not so many that the device runs
+// empty, nor so few that the workgroups wait in line.
+int dw_chunk(const sp_ops* o, const LinearArgs& a, int64_t tiles, int32_t dtype) {
+  const double n = a.n, sums = 8.0 * (double)chunk_stride(a) / 4e12, row = dtype == SP_F32 ? 55e-9 : 19e-9;
+  int64_t chunk = (int64_t)std::sqrt(n * sums / row);
+  chunk = std::clamp<int64_t>(chunk, a.n * tiles / 2048, std::max<int64_t>(a.n * tiles / 2048, a.n * tiles / 256));
+  chunk = (std::max<int64_t>(chunk, 64) + 63) / 64 * 64;
+  const int64_t most = o->ws_bytes / (chunk_stride(a) * (int64_t)sizeof(float)) - a.groups;    // chunks: at most n / chunk + groups
+  if (most <= 0) return 0;
+  chunk = std::max(chunk, ((int64_t)a.n + most - 1) / most);
+  return chunk < a.n ? (int)chunk : 0;
+}
 
 // The launch's tiles; false where there are more than a launch holds.
 bool linear_grid(LinearArgs* a, int64_t row_tiles, int64_t col_tiles) {
@@ -284,9 +304,9 @@ bool linear_grid(LinearArgs* a, int64_t row_tiles, int64_t col_tiles) {
   a->col_tiles = (int)col_tiles;
   return true;
 }
-void launch_linear(void (*kernel)(LinearArgs), const LinearArgs& a, void* stream) {
+void launch_linear(void (*kernel)(LinearArgs), int threads, const LinearArgs& a, void* stream) {
   const int tiles = a.row_tiles * a.col_tiles;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(kLinearThreads), 0, (hipStream_t)stream, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(threads), 0, (hipStream_t)stream, a);
 }
 
 // Shared checks of the grouped linear layers.
@@ -320,11 +340,18 @@ sp_status sp_grouped_linear(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t 
   a.n = n; a.k = k; a.m = m; a.groups = groups; a.x = x; a.x_stride = x_stride; a.offsets = offsets; a.w = w; a.bias = bias;
   a.relu = activation == SP_ACT_RELU; a.residual = residual; a.residual_stride = residual_stride; a.y = y; a.y_stride = y_stride;
   a.act = act_out; a.act_stride = act_stride; a.err = o->err;
+  if (few_rows(n, m, kFewCols, groups, dtype)) {
+    if (!linear_grid(&a, ((int64_t)n + kFewRows - 1) / kFewRows + groups, (m + kFewCols - 1) / kFewCols)) return SP_ECAPACITY;
+    if (dtype == SP_F32) launch_linear(k_linear_few<float, float>, kFewThreads, a, stream);
+    else if (out_dtype == SP_F32) launch_linear(k_linear_few<bf16, float>, kFewThreads, a, stream);
+    else launch_linear(k_linear_few<bf16, bf16>, kFewThreads, a, stream);
+    return launched(o);
+  }
   const bool narrow = m <= 64;
   if (!linear_grid(&a, (int64_t)(n + kLinearRows - 1) / kLinearRows + groups, (m + (narrow ? 63 : 127)) / (narrow ? 64 : 128))) return SP_ECAPACITY;
   auto run = [&]<typename T, typename TO>() {
-    if (narrow) launch_linear(k_linear<T, TO, kFormY, 64, false>, a, stream);
-    else launch_linear(k_linear<T, TO, kFormY, 128, false>, a, stream);
+    if (narrow) launch_linear(k_linear<T, TO, kFormY, 64, false>, kLinearThreads, a, stream);
+    else launch_linear(k_linear<T, TO, kFormY, 128, false>, kLinearThreads, a, stream);
   };
   if (dtype == SP_F32) run.template operator()<float, float>();
   else if (out_dtype == SP_F32) run.template operator()<bf16, float>();
@@ -353,35 +380,37 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
   hipStream_t s = (hipStream_t)stream;
   sp_status rc = SP_OK;
   auto run = [&]<typename T, bool MASK>() {
-    if (dx && n > 0) {
+    if (dx && n > 0 && few_rows(n, k, kFewDxCols, groups, dtype)) {
+      if (!linear_grid(&a, ((int64_t)n + kFewRows - 1) / kFewRows + groups, (k + kFewDxCols - 1) / kFewDxCols)) {
+        rc = SP_ECAPACITY;
+        return;
+      }
+      launch_linear(k_linear_few_dx<T>, kFewDxThreads, a, stream);
+    } else if (dx && n > 0) {
       const bool narrow = k <= 64;
       if (!linear_grid(&a, (int64_t)(n + kLinearRows - 1) / kLinearRows + groups, (k + (narrow ? 63 : 127)) / (narrow ? 64 : 128))) {
         rc = SP_ECAPACITY;
         return;
       }
-      if (narrow) launch_linear(k_linear<T, T, kFormDx, 64, MASK>, a, stream);
-      else launch_linear(k_linear<T, T, kFormDx, 128, MASK>, a, stream);
+      if (narrow) launch_linear(k_linear<T, T, kFormDx, 64, MASK>, kLinearThreads, a, stream);
+      else launch_linear(k_linear<T, T, kFormDx, 128, MASK>, kLinearThreads, a, stream);
     }
     if (dw) {
       const bool narrow = m <= 64;
       const int64_t k_tiles = (k + kLinearRows - 1) / kLinearRows, m_tiles = (m + (narrow ? 63 : 127)) / (narrow ? 64 : 128);
-      // Rows to a workgroup: so many that about kDwWorkgroups share the work, however the rows are spread over the groups; fewer
-      // chunks where the workspace does not hold their sums.
-      int64_t chunk = std::max<int64_t>(kDwMinRows, ((int64_t)n * k_tiles * m_tiles + kDwWorkgroups - 1) / kDwWorkgroups);
-      const int64_t most = o->ws_bytes / (chunk_stride(a) * (int64_t)sizeof(float)) - groups;   // chunks: at most n / chunk + groups
-      if (most > 0) chunk = std::max(chunk, (n + most - 1) / most);
-      a.chunk = most > 0 && chunk < n ? (int)((chunk + 63) / 64 * 64) : 0;
+      a.chunk = dw_chunk(o, a, k_tiles * m_tiles, dtype);
       a.part = (float*)o->ws;
       const int64_t items = a.chunk ? (n + a.chunk - 1) / a.chunk + groups : groups;
       if (!linear_grid(&a, items * k_tiles, m_tiles)) {
         rc = SP_ECAPACITY;
         return;
       }
-      if (narrow) launch_linear(k_linear<T, float, kFormDw, 64, MASK>, a, stream);
-      else launch_linear(k_linear<T, float, kFormDw, 128, MASK>, a, stream);
+      if (narrow) launch_linear(k_linear<T, float, kFormDw, 64, MASK>, kLinearThreads, a, stream);
+      else launch_linear(k_linear<T, float, kFormDw, 128, MASK>, kLinearThreads, a, stream);
       if (a.chunk) {
         const int64_t elems = (int64_t)k * m + (db ? m : 0);
-        if ((n + a.chunk - 1) / a.chunk >= 24 * (int64_t)groups)
+        // few elements: what fills the device is that many threads share an element's chunks
+        if (elems * groups < 512 * 256 && (n + a.chunk - 1) / a.chunk >= 8 * (int64_t)groups)
           hipLaunchKernelGGL(k_join_chunks<32>, dim3((unsigned)((elems + 31) / 32), groups), dim3(256), 0, s, a);
         else
           hipLaunchKernelGGL(k_join_chunks<4>, dim3((unsigned)((elems + 255) / 256), groups), dim3(256), 0, s, a);
