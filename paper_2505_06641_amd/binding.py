@@ -412,48 +412,22 @@ def sp_debug_copy_rate(n_bytes: int = 1 << 28, device: int = 0, stream=None):
     return gbs.value
 
 
-def _refuse(where, detail):
-    raise SneakPeekError(SP_EINVAL, where, detail)
+_native = None
 
 
-class _Checked:
-    """Checks of one call's tensors before their addresses go to the library (which cannot see shapes)."""
-
-    def __init__(self, where, device):
-        import torch
-        self.where, self.device = where, torch.device("cuda", device)
-        self.f32, self.bf16, self.i32 = torch.float32, torch.bfloat16, torch.int32
-
-    def dtype(self, t, name):
-        if t.dtype not in (self.f32, self.bf16):
-            _refuse(self.where, f"{name} is {t.dtype}, not float32 or bfloat16")
-        return F32 if t.dtype == self.f32 else BF16
-
-    def tensor(self, t, name, shape, dtype):
-        """Address of a contiguous tensor; None stays None."""
-        if t is None:
-            return None
-        if t.dtype != dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
-            self._say(t, name, shape, dtype)
-        return t.data_ptr()
-
-    def rows(self, t, name, shape, dtype):
-        """Address and row stride of a matrix with contiguous rows."""
-        if t is None:
-            return None, 0
-        if t.dtype != dtype or t.shape != shape or t.device != self.device:
-            self._say(t, name, shape, dtype)
-        stride, step = t.stride()
-        if (step != 1 and shape[1] > 1) or (stride < shape[1] and shape[0] > 1):
-            self._say(t, name, shape, dtype)
-        return t.data_ptr(), stride if stride > shape[1] else shape[1]
-
-    def _say(self, t, name, shape, dtype):
-        _refuse(self.where, f"{name}: {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}, where {dtype} "
-                            f"{tuple(shape)} with contiguous rows on {self.device} is asked for")
-
-
-F32, BF16 = 0, 1          # sp_dtype
+def load_native():
+    """The extension that checks the operators' tensors and calls the library (which is loaded first)."""
+    global _native
+    if _native is None:
+        load_library()
+        try:
+            from . import _ops_native
+        except ImportError as e:
+            raise RuntimeError(f"the extension _ops_native is missing or does not load ({e}): build it first "
+                               "(python -m paper_2505_06641_amd.build)") from e
+        _ops_native.set_error(SneakPeekError)
+        _native = _ops_native
+    return _native
 
 
 class TensorList:
@@ -461,152 +435,67 @@ class TensorList:
     where they are makes the list once.  Holds the tensors."""
 
     def __init__(self, grads, out=None):
-        import torch
         self.grads, self.out = list(grads), None if out is None else list(out)
-        n = len(self.grads)
-        if self.out is not None and len(self.out) != n:
-            _refuse("TensorList", f"{n} gradients, {len(self.out)} outputs")
-        self.device = self.grads[0].device if n else None
-        self.torch_dtype = self.grads[0].dtype if n else torch.float32
-        if self.torch_dtype not in (torch.float32, torch.bfloat16):
-            _refuse("TensorList", f"{self.torch_dtype}, not float32 or bfloat16")
-        self.dtype = F32 if self.torch_dtype == torch.float32 else BF16
-        for t in self.grads + (self.out or []):
-            if t.device != self.device or t.dtype != self.torch_dtype or not t.is_contiguous():
-                _refuse("TensorList", "tensors of one type on one device, each contiguous, are asked for")
-        for g, o in zip(self.grads, self.out or []):
-            if g.numel() != o.numel():
-                _refuse("TensorList", f"a gradient of {g.numel()} elements, an output of {o.numel()}")
-        self.n = n
-        self.ptrs = (C.c_void_p * max(1, n))(*[t.data_ptr() for t in self.grads])
-        self.sizes = (C.c_int64 * max(1, n))(*[t.numel() for t in self.grads])
-        self.outs = None if self.out is None else (C.c_void_p * max(1, n))(*[t.data_ptr() for t in self.out])
+        self.packed = load_native().pack_tensors(self.grads, self.out)
 
 
-class Ops:
-    """One sp_ops: the operators that train the heads.  Methods carry the names of the C entry points; tensors live on the ops'
-    device, matrices have contiguous rows.  What does not fit together raises before anything is launched."""
+def Ops(device: int = 0, workspace_bytes: int = 64 << 20):
+    """One sp_ops: the operators that train the heads.  Its methods carry the names of the C entry points; tensors live on the
+    ops' device, matrices have contiguous rows.  What does not fit together raises before anything is launched."""
+    return _ops_class()(device, workspace_bytes)
 
-    def __init__(self, device: int = 0, workspace_bytes: int = 64 << 20):
-        self.lib = load_library()
-        self.device = int(device)
-        h = C.c_void_p()
-        rc = self.lib.sp_ops_create(self.device, int(workspace_bytes), C.byref(h))
-        if rc != SP_OK:
-            raise SneakPeekError(rc, "sp_ops_create", self.lib.sp_strerror(rc).decode())
-        self.h = h
-        self._checked = {name: _Checked(name, self.device) for name in EXPORTS}
 
-    def close(self):
-        if getattr(self, "h", None):
-            self.lib.sp_ops_destroy(self.h)
-            self.h = None
+_Ops = None
 
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
 
-    def _check(self, rc, where):
-        if rc != SP_OK:
-            raise SneakPeekError(rc, where, self.lib.sp_strerror(rc).decode() + " " +
-                                 self.lib.sp_ops_last_hip_error(self.h).decode())
-        return rc
+def _ops_class():
+    """The class behind Ops(): its base comes from the extension, which is not loaded before it is needed."""
+    global _Ops
+    if _Ops is not None:
+        return _Ops
 
-    def sp_ops_check(self, stream=None):
-        """Waits for the stream; raises if a call since the last check met bad offsets, application ids, class counts or labels."""
-        return self._check(self.lib.sp_ops_check(self.h, _stream_ptr(stream)), "sp_ops_check")
+    class Ops(load_native().OpsBase):
+        def __init__(self, device, workspace_bytes):
+            self.lib = load_library()
+            self.device = int(device)
+            h = C.c_void_p()
+            rc = self.lib.sp_ops_create(self.device, int(workspace_bytes), C.byref(h))
+            if rc != SP_OK:
+                raise SneakPeekError(rc, "sp_ops_create", self.lib.sp_strerror(rc).decode())
+            self.h = h
+            self.set_handle(h.value, self.device)
 
-    def sp_layer_norm(self, x, y, gamma=None, beta=None, eps=1e-5, mean=None, rstd=None, stream=None):
-        """y = layer norm of x's rows; mean and rstd (float32 [n]) receive the statistics."""
-        c = self._checked["sp_layer_norm"]
-        n, d = x.shape
-        dt = c.dtype(x, "x")
-        px, sx = c.rows(x, "x", x.shape, x.dtype)
-        py, sy = c.rows(y, "y", x.shape, x.dtype)
-        rc = self.lib.sp_layer_norm(self.h, n, d, dt, px, sx, c.tensor(gamma, "gamma", (d,), c.f32), c.tensor(beta, "beta", (d,), c.f32),
-                                    eps, py, sy, c.tensor(mean, "mean", (n,), c.f32), c.tensor(rstd, "rstd", (n,), c.f32),
-                                    _stream_ptr(stream))
-        return self._check(rc, "sp_layer_norm")
+        def close(self):
+            if getattr(self, "h", None):
+                self.set_handle(0, self.device)
+                self.lib.sp_ops_destroy(self.h)
+                self.h = None
 
-    def sp_layer_norm_backward(self, dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, stream=None):
-        """Gradients of sp_layer_norm with the statistics that it handed out; dgamma and dbeta are float32 [d]."""
-        c = self._checked["sp_layer_norm_backward"]
-        n, d = x.shape
-        dt = c.dtype(x, "x")
-        px, sx = c.rows(x, "x", x.shape, x.dtype)
-        pdy, sdy = c.rows(dy, "dy", x.shape, x.dtype)
-        pdx, sdx = c.rows(dx, "dx", x.shape, x.dtype)
-        rc = self.lib.sp_layer_norm_backward(self.h, n, d, dt, pdy, sdy, px, sx, c.tensor(gamma, "gamma", (d,), c.f32),
-                                             c.tensor(mean, "mean", (n,), c.f32), c.tensor(rstd, "rstd", (n,), c.f32), pdx, sdx,
-                                             c.tensor(dgamma, "dgamma", (d,), c.f32), c.tensor(dbeta, "dbeta", (d,), c.f32),
-                                             _stream_ptr(stream))
-        return self._check(rc, "sp_layer_norm_backward")
+        def __del__(self):
+            try:
+                self.close()
+            except Exception:
+                pass
 
-    def sp_grouped_linear(self, x, offsets, w, y, bias=None, relu=False, residual=None, act_out=None, stream=None):
-        """y = act(x W_g + b_g) + residual; x [n, k], offsets int32 [groups + 1], w [groups, k, m], bias float32 [groups, m]."""
-        c = self._checked["sp_grouped_linear"]
-        n, k = x.shape
-        groups, m = w.shape[0], w.shape[-1]
-        dt = c.dtype(x, "x")
-        px, sx = c.rows(x, "x", x.shape, x.dtype)
-        py, sy = c.rows(y, "y", (n, m), y.dtype)
-        pr, sr = c.rows(residual, "residual", (n, m), y.dtype)
-        pa, sa = c.rows(act_out, "act_out", (n, m), y.dtype)
-        rc = self.lib.sp_grouped_linear(self.h, n, k, m, groups, dt, px, sx, c.tensor(offsets, "offsets", (groups + 1,), c.i32),
-                                        c.tensor(w, "w", (groups, k, m), x.dtype), c.tensor(bias, "bias", (groups, m), c.f32),
-                                        1 if relu else 0, c.dtype(y, "y"), pr, sr, py, sy, pa, sa, _stream_ptr(stream))
-        return self._check(rc, "sp_grouped_linear")
+        def sp_ops_check(self, stream=None):
+            """Waits for the stream; raises if a call since the last check met bad offsets, application ids, class counts or labels."""
+            rc = self.lib.sp_ops_check(self.h, _stream_ptr(stream))
+            if rc != SP_OK:
+                raise SneakPeekError(rc, "sp_ops_check", self.lib.sp_strerror(rc).decode() + " " +
+                                     self.lib.sp_ops_last_hip_error(self.h).decode())
+            return rc
 
-    def sp_grouped_linear_backward(self, dy, x, offsets, w, act=None, dx=None, dw=None, db=None, stream=None):
-        """Gradients of sp_grouped_linear; act: its y (act_out, if it had a residual) where it had relu=True.  dw, db: float32."""
-        c = self._checked["sp_grouped_linear_backward"]
-        n, k = x.shape
-        groups, m = w.shape[0], w.shape[-1]
-        dt = c.dtype(x, "x")
-        px, sx = c.rows(x, "x", x.shape, x.dtype)
-        pdy, sdy = c.rows(dy, "dy", (n, m), x.dtype)
-        pa, sa = c.rows(act, "act", (n, m), x.dtype)
-        pdx, sdx = c.rows(dx, "dx", x.shape, x.dtype)
-        rc = self.lib.sp_grouped_linear_backward(self.h, n, k, m, groups, dt, pdy, sdy, pa, sa, px, sx,
-                                                 c.tensor(offsets, "offsets", (groups + 1,), c.i32),
-                                                 c.tensor(w, "w", (groups, k, m), x.dtype), pdx, sdx,
-                                                 c.tensor(dw, "dw", (groups, k, m), c.f32), c.tensor(db, "db", (groups, m), c.f32),
-                                                 _stream_ptr(stream))
-        return self._check(rc, "sp_grouped_linear_backward")
+        def sp_clip_grad_norm(self, grads, max_norm, norm, out=None, stream=None):
+            """norm (float32 [1]) of all gradients together, and the gradients scaled to at most max_norm, in place or into `out`.
+            grads: a TensorList (which says where the outputs go), or a sequence of tensors."""
+            if not isinstance(grads, TensorList):
+                grads = TensorList(grads, out=out)
+            elif out is not None:
+                raise SneakPeekError(SP_EINVAL, "sp_clip_grad_norm", "a TensorList holds its outputs")
+            return self.clip_packed(grads.packed, max_norm, norm, stream)
 
-    def sp_cross_entropy(self, logits, label, loss, app=None, n_classes=None, weight=None, scale=1.0, dlogits=None, stream=None):
-        """loss [n] and dlogits of softmax cross entropy over the first n_classes[app[i]] columns (all of them without app)."""
-        c = self._checked["sp_cross_entropy"]
-        n, width = logits.shape
-        dt = c.dtype(logits, "logits")
-        pz, sz = c.rows(logits, "logits", logits.shape, logits.dtype)
-        gt = dt
-        pd, sd = None, 0
-        if dlogits is not None:
-            gt = c.dtype(dlogits, "dlogits")
-            pd, sd = c.rows(dlogits, "dlogits", logits.shape, dlogits.dtype)
-        apps = 0 if n_classes is None else n_classes.numel()
-        rc = self.lib.sp_cross_entropy(self.h, n, width, dt, pz, sz, apps, c.tensor(app, "app", (n,), c.i32),
-                                       c.tensor(n_classes, "n_classes", (apps,), c.i32), c.tensor(label, "label", (n,), c.i32),
-                                       c.tensor(weight, "weight", (n,), c.f32), scale, c.tensor(loss, "loss", (n,), c.f32), gt, pd, sd,
-                                       _stream_ptr(stream))
-        return self._check(rc, "sp_cross_entropy")
-
-    def sp_clip_grad_norm(self, grads, max_norm, norm, out=None, stream=None):
-        """norm (float32 [1]) of all gradients together, and the gradients scaled to at most max_norm, in place or into `out`.
-        grads: a TensorList (which says where the outputs go), or a sequence of tensors."""
-        c = self._checked["sp_clip_grad_norm"]
-        if not isinstance(grads, TensorList):
-            grads = TensorList(grads, out=out)
-        elif out is not None:
-            _refuse("sp_clip_grad_norm", "a TensorList holds its outputs")
-        if grads.n and grads.device != c.device:
-            _refuse("sp_clip_grad_norm", f"tensors on {grads.device}, operators on {c.device}")
-        rc = self.lib.sp_clip_grad_norm(self.h, grads.n, grads.dtype, grads.ptrs, grads.sizes, max_norm, grads.outs,
-                                        c.tensor(norm, "norm", (1,), c.f32), _stream_ptr(stream))
-        return self._check(rc, "sp_clip_grad_norm")
+    _Ops = Ops
+    return _Ops
 
 
 def to_device(requests, device="cuda:0"):
