@@ -229,9 +229,12 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
     if (total > ((int64_t)1 << 46)) return SP_ECAPACITY;
   }
   // some 2,000 workgroups share the elements, but none gets less than is worth a workgroup
-  const int piece = (int)std::clamp<int64_t>((total / 2048 + 4095) / 4096 * 4096, kClipPieceMin, kClipPieceMax);
+  int piece = (int)std::clamp<int64_t>((total / 2048 + 4095) / 4096 * 4096, kClipPieceMin, kClipPieceMax);
   for (int i = 0; i < n_tensors; ++i) pieces += (sizes[i] + piece - 1) / piece;
   if (pieces > INT_MAX || pieces * (int64_t)sizeof(double) > o->ws_bytes) return SP_ECAPACITY;
+  const int vec = (int)(16 / elem_bytes(dtype));
+  const bool few = n_tensors <= kClipTensors && total / vec + n_tensors <= kClipFewThreads * kClipFewEach;
+  if (few) piece = vec;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
   hipStream_t s = (hipStream_t)stream;
@@ -240,7 +243,7 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
     hipLaunchKernelGGL(k_clip_none, dim3(1), dim3(1), 0, s, norm_out);
     return launched(o);
   }
-  for (int pass = 0; pass < 2; ++pass) {
+  for (int pass = few ? 1 : 0; pass < 2; ++pass) {
     int64_t done = 0;
     for (int at = 0; at < n_tensors;) {
       ClipTable tb;
@@ -258,7 +261,9 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
       if (tb.count == 0) continue;
       tb.first[tb.count] = (int32_t)k;
       float* first_norm = done == 0 ? norm_out : nullptr;
-      if (pass == 0 && dtype == SP_F32) hipLaunchKernelGGL(k_clip_sum<float>, dim3((unsigned)k), dim3(256), 0, s, tb, part + done);
+      if (few && dtype == SP_F32) hipLaunchKernelGGL(k_clip_few<float>, dim3(1), dim3(kClipFewThreads), 0, s, tb, max_norm, norm_out);
+      else if (few) hipLaunchKernelGGL(k_clip_few<bf16>, dim3(1), dim3(kClipFewThreads), 0, s, tb, max_norm, norm_out);
+      else if (pass == 0 && dtype == SP_F32) hipLaunchKernelGGL(k_clip_sum<float>, dim3((unsigned)k), dim3(256), 0, s, tb, part + done);
       else if (pass == 0) hipLaunchKernelGGL(k_clip_sum<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, part + done);
       else if (dtype == SP_F32)
         hipLaunchKernelGGL(k_clip_scale<float>, dim3((unsigned)k), dim3(256), 0, s, tb, (int)pieces, part, max_norm, first_norm);
