@@ -139,7 +139,7 @@ sp_status sp_layer_norm(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const vo
       if constexpr (TEAM * C * kPiece<T> <= SP_MAX_NORM_DIM) {
         constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
         const int blocks = std::min((n + rows - 1) / rows, kNormBlocks);
-        hipLaunchKernelGGL((k_norm<T, TEAM, C>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)x, x_stride, gamma,
+        hipLaunchKernelGGL((d % kPiece<T> ? k_norm<T, TEAM, C, false> : k_norm<T, TEAM, C, true>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)x, x_stride, gamma,
                            beta, eps, (T*)y, y_stride, mean_out, rstd_out);
       }
     });
@@ -169,7 +169,7 @@ sp_status sp_layer_norm_backward(sp_ops* o, int32_t n, int32_t d, int32_t dtype,
         if constexpr (TEAM * C * kPiece<T> <= SP_MAX_NORM_DIM) {
           constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
           parts = (int)std::min<int64_t>({((int64_t)n + rows - 1) / rows, kNormBackBlocks, sums ? most : kNormBackBlocks});
-          hipLaunchKernelGGL((k_norm_back<T, TEAM, C>), dim3(parts), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)dy, dy_stride,
+          hipLaunchKernelGGL((d % kPiece<T> ? k_norm_back<T, TEAM, C, false> : k_norm_back<T, TEAM, C, true>), dim3(parts), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)dy, dy_stride,
                              (const T*)x, x_stride, gamma, mean, rstd, (T*)dx, dx_stride, sums ? (float*)o->ws : nullptr);
         }
       });
@@ -233,7 +233,7 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
   for (int i = 0; i < n_tensors; ++i) pieces += (sizes[i] + piece - 1) / piece;
   if (pieces > INT_MAX || pieces * (int64_t)sizeof(double) > o->ws_bytes) return SP_ECAPACITY;
   const int vec = (int)(16 / elem_bytes(dtype));
-  const bool few = n_tensors <= kClipTensors && total / vec + n_tensors <= kClipFewThreads * kClipFewEach;
+  const bool few = n_tensors <= kClipTensors && total / vec + n_tensors <= kClipThreads * kClipFewEach;
   if (few) piece = vec;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
@@ -243,35 +243,43 @@ sp_status sp_clip_grad_norm(sp_ops* o, int32_t n_tensors, int32_t dtype, const v
     hipLaunchKernelGGL(k_clip_none, dim3(1), dim3(1), 0, s, norm_out);
     return launched(o);
   }
-  for (int pass = few ? 1 : 0; pass < 2; ++pass) {
-    int64_t done = 0;
-    for (int at = 0; at < n_tensors;) {
-      ClipTable tb;
-      tb.count = 0;
-      tb.piece = piece;
-      int64_t k = 0;
-      for (; at < n_tensors && tb.count < kClipTensors; ++at) {
-        if (sizes[at] == 0) continue;
-        tb.src[tb.count] = grads[at];
-        tb.dst[tb.count] = out ? out[at] : const_cast<void*>(grads[at]);
-        tb.size[tb.count] = sizes[at];
-        tb.first[tb.count++] = (int32_t)k;
-        k += (sizes[at] + piece - 1) / piece;
-      }
-      if (tb.count == 0) continue;
-      tb.first[tb.count] = (int32_t)k;
-      float* first_norm = done == 0 ? norm_out : nullptr;
-      if (few && dtype == SP_F32) hipLaunchKernelGGL(k_clip_few<float>, dim3(1), dim3(kClipFewThreads), 0, s, tb, max_norm, norm_out);
-      else if (few) hipLaunchKernelGGL(k_clip_few<bf16>, dim3(1), dim3(kClipFewThreads), 0, s, tb, max_norm, norm_out);
-      else if (pass == 0 && dtype == SP_F32) hipLaunchKernelGGL(k_clip_sum<float>, dim3((unsigned)k), dim3(256), 0, s, tb, part + done);
-      else if (pass == 0) hipLaunchKernelGGL(k_clip_sum<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, part + done);
-      else if (dtype == SP_F32)
-        hipLaunchKernelGGL(k_clip_scale<float>, dim3((unsigned)k), dim3(256), 0, s, tb, (int)pieces, part, max_norm, first_norm);
-      else
-        hipLaunchKernelGGL(k_clip_scale<bf16>, dim3((unsigned)k), dim3(256), 0, s, tb, (int)pieces, part, max_norm, first_norm);
-      SP_HIP(o, hipGetLastError());
-      done += k;
+  // Tables from the first tensor on for the sums; back again for the scaling, whose first reads the last-level cache then still holds.
+  auto fill = [&](ClipTable* tb, int* from, int dir) {
+    int64_t k = 0;
+    tb->count = 0;
+    tb->piece = piece;
+    for (; *from >= 0 && *from < n_tensors && tb->count < kClipTensors; *from += dir) {
+      const int i = *from;
+      if (sizes[i] == 0) continue;
+      tb->src[tb->count] = grads[i];
+      tb->dst[tb->count] = out ? out[i] : const_cast<void*>(grads[i]);
+      tb->size[tb->count] = sizes[i];
+      tb->first[tb->count++] = (int32_t)k;
+      k += (sizes[i] + piece - 1) / piece;
     }
+    tb->first[tb->count] = (int32_t)k;
+    return (unsigned)k;
+  };
+  int64_t done = 0;
+  ClipTable tb;
+  for (int at = 0; at < n_tensors && !few;) {
+    const unsigned k = fill(&tb, &at, 1);
+    if (k == 0) continue;
+    if (dtype == SP_F32) hipLaunchKernelGGL(k_clip_sum<float>, dim3(k), dim3(kClipThreads), 0, s, tb, part + done);
+    else hipLaunchKernelGGL(k_clip_sum<bf16>, dim3(k), dim3(kClipThreads), 0, s, tb, part + done);
+    SP_HIP(o, hipGetLastError());
+    done += k;
+  }
+  float* norm = norm_out;                // written by the first of the launches
+  for (int at = n_tensors - 1; at >= 0;) {
+    const unsigned k = fill(&tb, &at, -1);
+    if (k == 0) continue;
+    if (few && dtype == SP_F32) hipLaunchKernelGGL(k_clip_few<float>, dim3(1), dim3(kClipThreads), 0, s, tb, max_norm, norm);
+    else if (few) hipLaunchKernelGGL(k_clip_few<bf16>, dim3(1), dim3(kClipThreads), 0, s, tb, max_norm, norm);
+    else if (dtype == SP_F32) hipLaunchKernelGGL(k_clip_scale<float>, dim3(k), dim3(kClipThreads), 0, s, tb, (int)pieces, part, max_norm, norm);
+    else hipLaunchKernelGGL(k_clip_scale<bf16>, dim3(k), dim3(kClipThreads), 0, s, tb, (int)pieces, part, max_norm, norm);
+    SP_HIP(o, hipGetLastError());
+    norm = nullptr;
   }
   return SP_OK;
 }

@@ -11,6 +11,7 @@
 namespace sp {
 
 constexpr int kClipTensors = 128;          // to a launch: the table has to fit the kernel's arguments
+constexpr int kClipThreads = 1024;          // few pieces fill the device: 65536 elements each at 1.2e8
 constexpr int kClipPieceMin = 8192, kClipPieceMax = 65536;       // elements; see clip_piece
 
 struct ClipTable {
@@ -36,6 +37,17 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
   return v;
 }
 
+// Sum of a value over the workgroup's wavefronts, on every thread.
+__device__ __forceinline__ double block_sum_f64(double v, double* waves) {
+  v = wave_sum_f64(v);
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double all = 0.0;
+#pragma unroll
+  for (int w = 0; w < kClipThreads / 64; ++w) all += waves[w];
+  return all;
+}
+
 // What a gradient is multiplied by.  A norm that is no number leaves none behind either.
 __device__ __forceinline__ float clip_coefficient(double norm, float max_norm) {
   const double ratio = (double)max_norm / (norm + 1e-6);
@@ -45,12 +57,12 @@ __device__ __forceinline__ float clip_coefficient(double norm, float max_norm) {
 // Few elements: one workgroup does both passes with everything in registers between them, and the call is one launch (the second one
 // costs the host 3 us and the device a start: 28000 elements in 14 tensors take the device 8 us either way, the host 3 us instead of 6).  Pieces are of 16 bytes;
 // a thread takes every 1024th, and has all of its loads under way together.
-constexpr int kClipFewThreads = 1024, kClipFewEach = 8;
+constexpr int kClipFewEach = 8;
 
 template <typename T>
-__global__ __launch_bounds__(kClipFewThreads) void k_clip_few(ClipTable tb, float max_norm, float* __restrict__ norm_out) {
-  constexpr int V = kPiece<T>, WAVES = kClipFewThreads / 64;
-  __shared__ double waves[WAVES];
+__global__ __launch_bounds__(kClipThreads) void k_clip_few(ClipTable tb, float max_norm, float* __restrict__ norm_out) {
+  constexpr int V = kPiece<T>;
+  __shared__ double waves[kClipThreads / 64];
   __shared__ const T* src[kClipTensors];
   __shared__ T* dst[kClipTensors];
   __shared__ int32_t size[kClipTensors], first[kClipTensors + 1];
@@ -72,28 +84,23 @@ __global__ __launch_bounds__(kClipFewThreads) void k_clip_few(ClipTable tb, floa
 #pragma unroll
     for (int u = 0; u < kClipFewEach; ++u) {
       const int k = tensor[u] + step;
-      if (k < tb.count && first[k] <= (int)threadIdx.x + u * kClipFewThreads) tensor[u] = k;
+      if (k < tb.count && first[k] <= (int)threadIdx.x + u * kClipThreads) tensor[u] = k;
     }
 #pragma unroll
   for (int u = 0; u < kClipFewEach; ++u) {
-    const int piece = threadIdx.x + u * kClipFewThreads, k = tensor[u], at = (piece - first[k]) * V;
+    const int piece = threadIdx.x + u * kClipThreads, k = tensor[u], at = (piece - first[k]) * V;
     load_some(src[k] + at, piece < pieces ? size[k] - at : 0, 0.f, v[u]);
   }
 #pragma unroll
   for (int u = 0; u < kClipFewEach; ++u)
 #pragma unroll
     for (int j = 0; j < V; ++j) s += (double)v[u][j] * (double)v[u][j];
-  s = wave_sum_f64(s);
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
-  __syncthreads();
-  double all = 0.0;
-  for (int w = 0; w < WAVES; ++w) all += waves[w];
-  const double norm = sqrt(all);
+  const double norm = sqrt(block_sum_f64(s, waves));
   if (threadIdx.x == 0) *norm_out = (float)norm;
   const float c = clip_coefficient(norm, max_norm);
 #pragma unroll
   for (int u = 0; u < kClipFewEach; ++u) {
-    const int piece = threadIdx.x + u * kClipFewThreads, k = tensor[u], at = (piece - first[k]) * V;
+    const int piece = threadIdx.x + u * kClipThreads, k = tensor[u], at = (piece - first[k]) * V;
     if (piece >= pieces || (c == 1.f && src[k] == dst[k])) continue;
 #pragma unroll
     for (int j = 0; j < V; ++j) v[u][j] *= c;
@@ -103,41 +110,34 @@ __global__ __launch_bounds__(kClipFewThreads) void k_clip_few(ClipTable tb, floa
 
 // The elements of a workgroup's piece.
 template <typename T>
-__device__ __forceinline__ int clip_piece_of(const ClipTable& tb, const T** src, T** dst) {
-  const int k = clip_tensor(tb, (int)blockIdx.x);
-  const int64_t at = (int64_t)((int)blockIdx.x - tb.first[k]) * tb.piece;
+__device__ __forceinline__ int clip_piece_of(const ClipTable& tb, int block, const T** src, T** dst) {
+  const int k = clip_tensor(tb, block);
+  const int64_t at = (int64_t)(block - tb.first[k]) * tb.piece;
   *src = (const T*)tb.src[k] + at;
   *dst = (T*)tb.dst[k] + at;
   return (int)min((int64_t)tb.piece, tb.size[k] - at);
 }
 
-// Sum of a value over the workgroup's four wavefronts, on every thread.
-__device__ __forceinline__ double block_sum_f64(double v, double* waves) {
-  v = wave_sum_f64(v);
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (waves[0] + waves[1]) + (waves[2] + waves[3]);
-}
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_clip_sum(ClipTable tb, double* __restrict__ part) {
+__global__ __launch_bounds__(kClipThreads) void k_clip_sum(ClipTable tb, double* __restrict__ part) {
   constexpr int V = kPiece<T>;
-  __shared__ double waves[4];
+  __shared__ double waves[kClipThreads / 64];
   const T* src;
   T* dst;
-  const int count = clip_piece_of(tb, &src, &dst);
+  const int count = clip_piece_of(tb, (int)blockIdx.x, &src, &dst);
   double s = 0.0;
   int i = threadIdx.x * V;
-  for (; i + 3 * 256 * V + V <= count; i += 4 * 256 * V) {           // four loads under way
+  for (; i + 3 * kClipThreads * V + V <= count; i += 4 * kClipThreads * V) {           // four loads under way
     float v[4][V];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load_piece(src + i + u * 256 * V, v[u]);
+    for (int u = 0; u < 4; ++u) load_piece(src + i + u * kClipThreads * V, v[u]);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int j = 0; j < V; ++j) s += (double)v[u][j] * (double)v[u][j];
   }
-  for (; i < count; i += 256 * V) {
+  for (; i < count; i += kClipThreads * V) {
     float v[V];
     load_some(src + i, count - i, 0.f, v);
 #pragma unroll
@@ -148,32 +148,32 @@ __global__ __launch_bounds__(256) void k_clip_sum(ClipTable tb, double* __restri
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_clip_scale(ClipTable tb, int pieces, const double* __restrict__ part, float max_norm,
+__global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipTable tb, int pieces, const double* __restrict__ part, float max_norm,
                                                     float* __restrict__ norm_out) {
   constexpr int V = kPiece<T>;
-  __shared__ double waves[4];
+  __shared__ double waves[kClipThreads / 64];
   double all = 0.0;
-  for (int i = threadIdx.x; i < pieces; i += 256) all += part[i];
+  for (int i = threadIdx.x; i < pieces; i += kClipThreads) all += part[i];
   const double norm = sqrt(block_sum_f64(all, waves));
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   const float c = clip_coefficient(norm, max_norm);
   const T* src;
   T* dst;
-  const int count = clip_piece_of(tb, &src, &dst);
+  const int count = clip_piece_of(tb, (int)(gridDim.x - 1 - blockIdx.x), &src, &dst);       // the last ones read are still in the cache
   if (c == 1.f && src == dst) return;                      // stays as it is
   int i = threadIdx.x * V;
-  for (; i + 3 * 256 * V + V <= count; i += 4 * 256 * V) {
+  for (; i + 3 * kClipThreads * V + V <= count; i += 4 * kClipThreads * V) {
     float v[4][V];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load_piece(src + i + u * 256 * V, v[u]);
+    for (int u = 0; u < 4; ++u) load_piece(src + i + u * kClipThreads * V, v[u]);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
 #pragma unroll
       for (int j = 0; j < V; ++j) v[u][j] *= c;
-      store_piece(dst + i + u * 256 * V, v[u]);
+      store_piece(dst + i + u * kClipThreads * V, v[u]);
     }
   }
-  for (; i < count; i += 256 * V) {
+  for (; i < count; i += kClipThreads * V) {
     float v[V];
     load_some(src + i, count - i, 0.f, v);
 #pragma unroll
