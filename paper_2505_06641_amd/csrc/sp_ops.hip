@@ -322,6 +322,20 @@ void launch_linear(void (*kernel)(LinearArgs), int threads, const LinearArgs& a,
   hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(threads), 0, (hipStream_t)stream, a);
 }
 
+// Tiles of 64 or 128 columns; those of 128 with eight wavefronts where the device holds all of them at once, or where there is a mask.
+template <typename T, typename TO, int FORM, bool MASK>
+void launch_tiles(bool narrow, const LinearArgs& a, void* stream) {
+  if (narrow) {
+    launch_linear(k_linear<T, TO, FORM, 64, MASK, 256>, 256, a, stream);
+  } else if constexpr (MASK) {
+    launch_linear(k_linear<T, TO, FORM, 128, MASK, 512>, 512, a, stream);
+  } else if ((int64_t)a.row_tiles * a.col_tiles <= 768) {
+    launch_linear(k_linear<T, TO, FORM, 128, MASK, 512>, 512, a, stream);
+  } else {
+    launch_linear(k_linear<T, TO, FORM, 128, MASK, 256>, 256, a, stream);
+  }
+}
+
 // Shared checks of the grouped linear layers.
 sp_status linear_sizes(const sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype) {
   if (!o || n < 0 || k < 1 || m < 1 || groups < 1 || !dtype_ok(dtype)) return SP_EINVAL;
@@ -363,8 +377,7 @@ sp_status sp_grouped_linear(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t 
   const bool narrow = m <= 64;
   if (!linear_grid(&a, (int64_t)(n + kLinearRows - 1) / kLinearRows + groups, (m + (narrow ? 63 : 127)) / (narrow ? 64 : 128))) return SP_ECAPACITY;
   auto run = [&]<typename T, typename TO>() {
-    if (narrow) launch_linear(k_linear<T, TO, kFormY, 64, false>, kLinearThreads, a, stream);
-    else launch_linear(k_linear<T, TO, kFormY, 128, false>, kLinearThreads, a, stream);
+    launch_tiles<T, TO, kFormY, false>(narrow, a, stream);
   };
   if (dtype == SP_F32) run.template operator()<float, float>();
   else if (out_dtype == SP_F32) run.template operator()<bf16, float>();
@@ -405,8 +418,7 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
         rc = SP_ECAPACITY;
         return;
       }
-      if (narrow) launch_linear(k_linear<T, T, kFormDx, 64, MASK>, kLinearThreads, a, stream);
-      else launch_linear(k_linear<T, T, kFormDx, 128, MASK>, kLinearThreads, a, stream);
+      launch_tiles<T, T, kFormDx, MASK>(narrow, a, stream);
     }
     if (dw) {
       const bool narrow = m <= 64;
@@ -418,8 +430,7 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
         rc = SP_ECAPACITY;
         return;
       }
-      if (narrow) launch_linear(k_linear<T, float, kFormDw, 64, MASK>, kLinearThreads, a, stream);
-      else launch_linear(k_linear<T, float, kFormDw, 128, MASK>, kLinearThreads, a, stream);
+      launch_tiles<T, float, kFormDw, MASK>(narrow, a, stream);
       if (a.chunk) {
         const int64_t elems = (int64_t)k * m + (db ? m : 0);
         // few elements: what fills the device is that many threads share an element's chunks

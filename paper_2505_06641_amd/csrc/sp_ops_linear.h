@@ -56,7 +56,6 @@ __host__ __device__ __forceinline__ int64_t chunk_stride(const LinearArgs& a) { 
 
 enum LinearForm { kFormY = 0, kFormDx = 1, kFormDw = 2 };
 
-constexpr int kLinearThreads = 256;
 constexpr int kLinearRows = 128;                                      // rows of a tile
 template <typename T> constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1; // bfloat16 numbers that make up a value
 template <typename T> constexpr int kDepth = sizeof(T) == 4 ? 32 : 64; // depth of a piece: 48 KB of LDS with 128 columns, 32 KB
@@ -104,10 +103,10 @@ __device__ __forceinline__ float high_bf16(uint32_t v) { return __uint_as_float(
 // One side of a tile: W rows (or columns) by kDepth<T> of the depth.
 // LDS, per plane: contiguous depth [W][depth], the 16-byte pieces of a row permuted by the row, so that the eight rows that are
 // read together lie in different banks; strided depth [depth][W], the 64-byte pieces permuted likewise by the depth.
-template <typename T, int W, bool STRIDED, bool MASK>
+template <typename T, int W, bool STRIDED, bool MASK, int THREADS>
 struct Side {
   static constexpr int V = kPiece<T>, D = kDepth<T>, P = kPlanes<T>;
-  static constexpr int kPieces = W * D / V / kLinearThreads;        // of 16 bytes, each thread's
+  static constexpr int kPieces = W * D / V / THREADS;        // of 16 bytes, each thread's
   static constexpr int kAcross = (STRIDED ? W : D) / V;             // pieces of a contiguous run in memory
   static constexpr int kElems = W * D;
   u32x4 raw[kPieces];
@@ -115,7 +114,7 @@ struct Side {
 
   uint32_t off, act_off;                                            // bytes from the piece of the depth's first element
   int64_t step, act_step;                                           // elements from one of a thread's pieces to the next
-  static constexpr int kStep = kLinearThreads / kAcross;            // the same in rows
+  static constexpr int kStep = THREADS / kAcross;            // the same in rows
 
   __device__ __forceinline__ void init(int64_t stride, int64_t act_stride) {
     const uint32_t major = threadIdx.x / kAcross, minor = (threadIdx.x % kAcross) * V;
@@ -179,7 +178,7 @@ struct Side {
   __device__ __forceinline__ void store(uint16_t* lds) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int p = threadIdx.x + i * kLinearThreads, major = p / kAcross, minor = (p % kAcross) * V;
+      const int p = threadIdx.x + i * THREADS, major = p / kAcross, minor = (p % kAcross) * V;
       if (MASK) raw[i] = masked((const T*)nullptr, raw[i], act[i]);
       uint16_t* at = lds + place(major, minor);
       if constexpr (P == 1) {
@@ -226,12 +225,16 @@ struct Side {
   }
 };
 
-// Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, two by two: 64 rows and BN / 2 columns each.
-template <typename T, typename TO, int FORM, int BN, bool MASK>
-__global__ __launch_bounds__(kLinearThreads, MASK ? 2 : 3) void k_linear(LinearArgs a) {
-  constexpr int BM = kLinearRows, D = kDepth<T>, P = kPlanes<T>, FR = 2, FC = BN / 64, V = kPiece<T>;
-  typedef Side<T, BM, FORM == kFormDw, FORM == kFormDx && MASK> Rows;
-  typedef Side<T, BN, FORM != kFormDx, FORM == kFormDw && MASK> Cols;
+// Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, 64 rows and BN / 2 columns each, or eight of 64 by 32: a wavefront
+// of 64 by 64 reads a third less from LDS for its products (65536 x 1024 -> 512 bfloat16 99 us against 109, the LDS being what is busiest),
+// eight are quicker through a tile where the device is not full (6170 x 256 -> 862 21 us against 24) and where the mask's registers leave
+// room for two workgroups of four only.
+template <typename T, typename TO, int FORM, int BN, bool MASK, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_linear(LinearArgs a) {
+  constexpr int BM = kLinearRows, D = kDepth<T>, P = kPlanes<T>, FR = 2, FC = BN * 2 / (THREADS / 2), V = kPiece<T>;
+  constexpr int WN = FC * 32, WAVE_COLS = BN / WN;          // columns of a wavefront, wavefronts side by side
+  typedef Side<T, BM, FORM == kFormDw, FORM == kFormDx && MASK, THREADS> Rows;
+  typedef Side<T, BN, FORM != kFormDx, FORM == kFormDw && MASK, THREADS> Cols;
   __shared__ __align__(16) uint16_t lds[P * (Rows::kElems + Cols::kElems)];
   uint16_t* lds_rows = lds;
   uint16_t* lds_cols = lds + P * Rows::kElems;
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(kLinearThreads, MASK ? 2 : 3) void k_linear(LinearA
   };
 
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int wr = (wave >> 1) * 64, wc = (wave & 1) * (BN / 2);
+  const int wr = wave / WAVE_COLS * 64, wc = wave % WAVE_COLS * WN;
   f32x16 acc[FR][FC];
 #pragma unroll
   for (int i = 0; i < FR; ++i)
@@ -366,6 +369,7 @@ __global__ __launch_bounds__(kLinearThreads, MASK ? 2 : 3) void k_linear(LinearA
     for (; t0 + 2 * D <= depth; t0 += D) {
       store();
       load(t0 + D, false);
+      __builtin_amdgcn_sched_barrier(0);                   // the loads go out before the products, not between the last of them
       multiply();
     }
   } else if (depth > 0) {
@@ -376,6 +380,7 @@ __global__ __launch_bounds__(kLinearThreads, MASK ? 2 : 3) void k_linear(LinearA
     sc.cut(width - c0, depth - t0);
     store();
     if (t0 + D < depth) load(t0 + D, true);
+    __builtin_amdgcn_sched_barrier(0);
     multiply();
   }
 
@@ -386,7 +391,7 @@ __global__ __launch_bounds__(kLinearThreads, MASK ? 2 : 3) void k_linear(LinearA
   constexpr int VO = kPiece<TO>, kAcross = BN / VO;        // 16 bytes of output a time
 #pragma unroll
   for (int i = 0; i < FR; ++i) {
-    const int mine = (wave >> 1) * 32 + (lane & 31);
+    const int mine = wr / 2 + (lane & 31);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < FC; ++j)
@@ -398,8 +403,8 @@ __global__ __launch_bounds__(kLinearThreads, MASK ? 2 : 3) void k_linear(LinearA
       }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < 64 * kAcross / kLinearThreads; ++u) {
-      const int p = threadIdx.x + u * kLinearThreads, sr_ = p / kAcross, sc_ = (p % kAcross) * VO;
+    for (int u = 0; u < 64 * kAcross / THREADS; ++u) {
+      const int p = threadIdx.x + u * THREADS, sr_ = p / kAcross, sc_ = (p % kAcross) * VO;
       const int r = (sr_ >> 5) * 64 + i * 32 + (sr_ & 31), c = c0 + sc_, left = width - c;
       if (r >= n_rows || left <= 0) continue;
       const int64_t row = r0 + r;
@@ -439,7 +444,7 @@ __global__ __launch_bounds__(kLinearThreads, MASK ? 2 : 3) void k_linear(LinearA
     }
   }
   if (FORM == kFormDw && sum_columns) {                    // the threads that have loaded the same columns: their sums through LDS
-    constexpr int across = Cols::kAcross, same = kLinearThreads / across;
+    constexpr int across = Cols::kAcross, same = THREADS / across;
     float* s = stage;                                      // [same][BN]
     static_assert(same <= 64, "sums of columns fit");
     __syncthreads();
