@@ -143,6 +143,7 @@ __device__ __forceinline__ void group_rows(const int32_t* offsets, int n, int g,
 // 64 groups at a time, each lane one of them.  Returns false where there are fewer tiles than `tile` + 1.
 struct RowTile {
   int g, lo, hi;      // rows lo .. hi of group g
+  int start;          // the group's first row
   bool whole;         // they are all of the group's rows
 };
 __device__ __forceinline__ bool find_row_tile(const int32_t* offsets, int n_groups, int n, int tile_rows, int tile, RowTile* out) {
@@ -167,6 +168,7 @@ __device__ __forceinline__ bool find_row_tile(const int32_t* offsets, int n_grou
       const int first = __builtin_amdgcn_readlane(s0 + (tile - (upto - tiles)) * tile_rows, l), last = __builtin_amdgcn_readlane(e, l);
       out->g = base + l;
       out->lo = first;
+      out->start = __builtin_amdgcn_readlane(s0, l);
       out->hi = last - first < tile_rows ? last : first + tile_rows;
       out->whole = __builtin_amdgcn_readlane(tiles, l) == 1;
       return true;

@@ -31,6 +31,18 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
+// A piece's elements from `first` on, as far as there are any.
+template <typename T, int V>
+__device__ __forceinline__ void store_part(T* p, int first, int count, const float (&v)[V]) {
+  if (first == 0) {
+    store_some(p, count, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i >= first && i < count) p[i] = from_float<T>(v[i]);
+  }
+}
+
 struct LinearArgs {
   int n, k, m, groups;
   const void* x;  int64_t x_stride;      // [n, k]
@@ -225,7 +237,9 @@ struct Side {
   }
 };
 
-// Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, 64 rows and BN / 2 columns each, or eight of 64 by 32: a wavefront
+// The last tile of a group's rows, and the last one of the columns, starts early enough to be a whole one where there is enough before it:
+// it computes again what the tile before it has, and leaves the writing to that one (float32 256 -> 1000: 921 -> 861 us; pieces that are cut take
+// twice as long).  Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, 64 rows and BN / 2 columns each, or eight of 64 by 32: a wavefront
 // of 64 by 64 reads a third less from LDS for its products (65536 x 1024 -> 512 bfloat16 99 us against 109, the LDS being what is busiest),
 // eight are quicker through a tile where the device is not full (6170 x 256 -> 862 21 us against 24) and where the mask's registers leave
 // room for two workgroups of four only.
@@ -244,11 +258,13 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
   // the tile: consecutive ones share rows, and go to one die as far as that is possible
   const int tile = xcd_tile(blockIdx.x, a.row_tiles * a.col_tiles);
   if (tile < 0) return;
-  const int rt = tile / a.col_tiles, ct = tile % a.col_tiles, c0 = ct * BN;
   RowTile rows;
+  const int rt = tile / a.col_tiles, ct = tile % a.col_tiles;
   int r0, n_rows, depth;
+  int skip_r = 0;                                          // rows (columns) of the tile that are another one's to write
   int64_t slot = -1;                                       // dW: where a chunk's sums go
   const int width = FORM == kFormDx ? a.k : a.m;
+  const int c0 = max(min(ct * BN, width - BN), 0), skip_c = ct * BN - c0;
   if (FORM == kFormDw) {
     const int k_tiles = (a.k + BM - 1) / BM, kt = rt % k_tiles, item = rt / k_tiles;
     if (a.chunk == 0) {
@@ -258,13 +274,15 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
       if (!find_row_tile(a.offsets, a.groups, a.n, a.chunk, item, &rows) || rows.g >= a.groups) return;
       if (!rows.whole) slot = item;
     }
-    r0 = kt * BM;
+    r0 = max(min(kt * BM, a.k - BM), 0);
+    skip_r = kt * BM - r0;
     n_rows = a.k - r0;
     depth = rows.hi - rows.lo;
   } else {
     if (!find_row_tile(a.offsets, a.groups, a.n, BM, rt, &rows)) return;
-    r0 = rows.lo;
-    n_rows = rows.hi - rows.lo;
+    r0 = max(min(rows.lo, rows.hi - BM), rows.start);
+    skip_r = rows.lo - r0;
+    n_rows = rows.hi - r0;
     depth = rows.g < a.groups ? (FORM == kFormY ? a.k : a.m) : 0;
   }
   const T* x = (const T*)a.x;
@@ -331,7 +349,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
     for (int j = 0; j < FC; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-  const bool sum_columns = FORM == kFormDw && a.db && r0 == 0;
+  const bool sum_columns = FORM == kFormDw && a.db && r0 == 0 && skip_r == 0;
   float sums[V] = {};
 
   auto store = [&]() {
@@ -406,8 +424,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
     for (int u = 0; u < 64 * kAcross / THREADS; ++u) {
       const int p = threadIdx.x + u * THREADS, sr_ = p / kAcross, sc_ = (p % kAcross) * VO;
       const int r = (sr_ >> 5) * 64 + i * 32 + (sr_ & 31), c = c0 + sc_, left = width - c;
-      if (r >= n_rows || left <= 0) continue;
+      if (r < skip_r || r >= n_rows || left <= 0 || sc_ + VO <= skip_c) continue;
       const int64_t row = r0 + r;
+      const int first = max(skip_c - sc_, 0);              // of the piece's elements
       float v[VO];
 #pragma unroll
       for (int h = 0; h < VO / 4; ++h) {
@@ -417,9 +436,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
       }
       if (FORM == kFormDw) {
         float* out = slot < 0 ? a.dw + (int64_t)rows.g * a.k * a.m : a.part + slot * chunk_stride(a);
-        store_some(out + row * a.m + c, left, v);
+        store_part(out + row * a.m + c, first, left, v);
       } else if (FORM == kFormDx) {
-        store_some((TO*)a.dx + row * a.dx_stride + c, left, v);
+        store_part((TO*)a.dx + row * a.dx_stride + c, first, left, v);
       } else {
         const bool in = rows.g < a.groups;
         if (in && a.bias) {
@@ -432,14 +451,14 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
 #pragma unroll
           for (int e = 0; e < VO; ++e) v[e] = relu_of(v[e]);
         }
-        if (a.act) store_some((TO*)a.act + row * a.act_stride + c, left, v);
+        if (a.act) store_part((TO*)a.act + row * a.act_stride + c, first, left, v);
         if (in && a.residual) {
           float b[VO];
           load_some((const TO*)a.residual + row * a.residual_stride + c, left, 0.f, b);
 #pragma unroll
           for (int e = 0; e < VO; ++e) v[e] += b[e];
         }
-        store_some((TO*)a.y + row * a.y_stride + c, left, v);
+        store_part((TO*)a.y + row * a.y_stride + c, first, left, v);
       }
     }
   }
@@ -452,7 +471,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
     for (int j = 0; j < V; ++j) s[(threadIdx.x / across) * BN + (threadIdx.x % across) * V + j] = sums[j];
     __syncthreads();
     const int c = c0 + threadIdx.x;
-    if (threadIdx.x < BN && c < a.m) {
+    if (threadIdx.x < BN && threadIdx.x >= skip_c && c < a.m) {
       float v = 0.f;
       for (int u = 0; u < same; ++u) v += s[u * BN + threadIdx.x];
       float* out = slot < 0 ? a.db + (int64_t)rows.g * a.m : a.part + slot * chunk_stride(a) + (int64_t)a.k * a.m;
