@@ -410,6 +410,20 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
 #pragma unroll
   for (int i = 0; i < FR; ++i) {
     const int mine = wr / 2 + (lane & 31);
+    // the residual is on its way while the sums go through LDS
+    constexpr int kEach = 64 * kAcross / THREADS;
+    u32x4 res[FORM == kFormY ? kEach : 1];                 // (as it is in memory: what turns it into floats would wait for it)
+    if (FORM == kFormY && a.residual && rows.g < a.groups) {
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const int p = threadIdx.x + u * THREADS, sr_ = p / kAcross, sc_ = (p % kAcross) * VO;
+        const int r = (sr_ >> 5) * 64 + i * 32 + (sr_ & 31), c = c0 + sc_;
+        const TO* from = (const TO*)a.residual + (int64_t)(r0 + r) * a.residual_stride + c;
+        const int count = r >= skip_r && r < n_rows ? width - c : 0;
+        if (count >= VO) res[u] = __builtin_bit_cast(u32x4, *reinterpret_cast<const u32x4_any*>(from));
+        else res[u] = load_raw_some(from, count);
+      }
+    }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < FC; ++j)
@@ -421,7 +435,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
       }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < 64 * kAcross / THREADS; ++u) {
+    for (int u = 0; u < kEach; ++u) {
       const int p = threadIdx.x + u * THREADS, sr_ = p / kAcross, sc_ = (p % kAcross) * VO;
       const int r = (sr_ >> 5) * 64 + i * 32 + (sr_ & 31), c = c0 + sc_, left = width - c;
       if (r < skip_r || r >= n_rows || left <= 0 || sc_ + VO <= skip_c) continue;
@@ -453,10 +467,11 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
         }
         if (a.act) store_part((TO*)a.act + row * a.act_stride + c, first, left, v);
         if (in && a.residual) {
-          float b[VO];
-          load_some((const TO*)a.residual + row * a.residual_stride + c, left, 0.f, b);
 #pragma unroll
-          for (int e = 0; e < VO; ++e) v[e] += b[e];
+          for (int e = 0; e < VO; ++e) {
+            if constexpr (VO == 4) v[e] += __uint_as_float(res[u][e]);
+            else v[e] += e % 2 ? high_bf16(res[u][e / 2]) : low_bf16(res[u][e / 2]);
+          }
         }
         store_part((TO*)a.y + row * a.y_stride + c, first, left, v);
       }
