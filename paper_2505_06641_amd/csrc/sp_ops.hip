@@ -20,20 +20,15 @@ using namespace sp;
 
 struct sp_ops {
   int device = 0;
-  char* ws = nullptr;              // the caller's share of the device memory: partial sums
+  char* ws = nullptr;              // partial sums
   int64_t ws_bytes = 0;
-  uint32_t* err = nullptr;         // device: kErr* bits since the last sp_ops_check
-  uint32_t* err_host = nullptr;    // pinned
+  uint32_t* err = nullptr;         // behind them: kErr* bits since the last sp_ops_check; those of the last one
   std::string hip_err;
 };
 
 namespace {
 
-__global__ void k_ops_clear(uint32_t* err) { *err = 0u; }
-__global__ void k_ops_report(uint32_t* err, uint32_t* host) {
-  *host = atomicExch(err, 0u);
-  __threadfence_system();
-}
+__global__ void k_ops_report(uint32_t* err) { err[1] = atomicExch(err, 0u); }
 __global__ void k_clip_none(float* norm_out) { *norm_out = 0.f; }
 
 bool dtype_ok(int32_t t) { return t == SP_F32 || t == SP_BF16; }
@@ -84,14 +79,13 @@ sp_status sp_ops_create(int device_id, int64_t workspace_bytes, sp_ops** out) {
   DeviceGuard g(device_id);
   sp_status rc = g.ok ? SP_OK : SP_EDEVICE;
   auto need = [&](hipError_t e) { if (rc == SP_OK && e != hipSuccess) rc = e == hipErrorOutOfMemory ? SP_ENOMEM : SP_EDEVICE; };
-  if (rc == SP_OK) need(hipMalloc((void**)&o->ws, (size_t)workspace_bytes));
-  if (rc == SP_OK) need(hipMalloc((void**)&o->err, 256));
-  if (rc == SP_OK) need(hipHostMalloc((void**)&o->err_host, sizeof(uint32_t), hipHostMallocDefault));
+  const int64_t bytes = (workspace_bytes + 255) / 256 * 256;
+  const uint32_t none[2] = {0u, 0u};
+  if (rc == SP_OK) need(hipMalloc((void**)&o->ws, (size_t)bytes + sizeof(none)));
   if (rc == SP_OK) {
     o->ws_bytes = workspace_bytes;
-    hipLaunchKernelGGL(k_ops_clear, dim3(1), dim3(1), 0, nullptr, o->err);
-    need(hipGetLastError());
-    need(hipDeviceSynchronize());
+    o->err = reinterpret_cast<uint32_t*>(o->ws + bytes);
+    need(hipMemcpy(o->err, none, sizeof(none), hipMemcpyHostToDevice));
   }
   if (rc != SP_OK) {
     sp_ops_destroy(o);
@@ -106,8 +100,6 @@ void sp_ops_destroy(sp_ops* o) {
   DeviceGuard g(o->device);
   (void)hipDeviceSynchronize();
   if (o->ws) (void)hipFree(o->ws);
-  if (o->err) (void)hipFree(o->err);
-  if (o->err_host) (void)hipHostFree(o->err_host);
   delete o;
 }
 
@@ -118,10 +110,12 @@ sp_status sp_ops_check(sp_ops* o, void* stream) {
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
   hipStream_t s = (hipStream_t)stream;
-  hipLaunchKernelGGL(k_ops_report, dim3(1), dim3(1), 0, s, o->err, o->err_host);
+  uint32_t seen = 0u;
+  hipLaunchKernelGGL(k_ops_report, dim3(1), dim3(1), 0, s, o->err);
   SP_HIP(o, hipGetLastError());
+  SP_HIP(o, hipMemcpyAsync(&seen, o->err + 1, sizeof(seen), hipMemcpyDeviceToHost, s));
   SP_HIP(o, hipStreamSynchronize(s));
-  return *o->err_host ? SP_EINVAL : SP_OK;
+  return seen ? SP_EINVAL : SP_OK;
 }
 
 sp_status sp_layer_norm(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const void* x, int64_t x_stride, const float* gamma,
@@ -169,14 +163,16 @@ sp_status sp_layer_norm_backward(sp_ops* o, int32_t n, int32_t d, int32_t dtype,
         if constexpr (TEAM * C * kPiece<T> <= SP_MAX_NORM_DIM) {
           constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
           parts = (int)std::min<int64_t>({((int64_t)n + rows - 1) / rows, kNormBackBlocks, sums ? most : kNormBackBlocks});
+          if (parts <= 4) parts = 1;           // one workgroup in up to four turns: no sums to be joined by a second launch
           hipLaunchKernelGGL((d % kPiece<T> ? k_norm_back<T, TEAM, C, false> : k_norm_back<T, TEAM, C, true>), dim3(parts), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)dy, dy_stride,
-                             (const T*)x, x_stride, gamma, mean, rstd, (T*)dx, dx_stride, sums ? (float*)o->ws : nullptr);
+                             (const T*)x, x_stride, gamma, mean, rstd, (T*)dx, dx_stride, sums && parts > 1 ? (float*)o->ws : nullptr,
+                             parts > 1 ? nullptr : dgamma, parts > 1 ? nullptr : dbeta);
         }
       });
     };
     if (dtype == SP_F32) run.template operator()<float>(); else run.template operator()<bf16>();
   }
-  if (sums)
+  if (sums && parts != 1)                      // (without rows: zeros)
     hipLaunchKernelGGL(k_norm_join, dim3((2 * d + 31) / 32), dim3(256), 0, (hipStream_t)stream, parts, d, (const float*)o->ws, dgamma,
                        dbeta);
   return launched(o);

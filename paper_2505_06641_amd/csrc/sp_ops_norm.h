@@ -103,12 +103,13 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm(int n, int d, const
 
 // Every team walks its rows with dgamma's and dbeta's sums of its columns in registers; the workgroup's teams add theirs up,
 // those of a wavefront across lanes and the wavefronts one after the other in LDS, and write one row of partial sums:
-// part[workgroup][2][d], each row of them at a 16-byte piece.
+// part[workgroup][2][d], each row of them at a 16-byte piece.  A single workgroup writes dgamma and dbeta.
 template <typename T, int TEAM, int C, bool WHOLE>
 __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, const T* dy, int64_t dy_stride, const T* x,
                                                                   int64_t x_stride, const float* __restrict__ gamma,
                                                                   const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
-                                                                  int64_t dx_stride, float* __restrict__ part) {
+                                                                  int64_t dx_stride, float* __restrict__ part,
+                                                                  float* __restrict__ dgamma, float* __restrict__ dbeta) {
   constexpr int V = kPiece<T>, ROWS = kTeamThreads<TEAM> / TEAM;
   typedef NormPiece<T, TEAM, WHOLE> Piece;
   __shared__ float red[2][TEAM > 64 ? TEAM / 64 : 1];
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, 
       Piece(d, c, t).store(dx + row * dx_stride, d, g[c]);
     }
   }
-  if (!part) return;
+  if (!part && !dgamma && !dbeta) return;
   if (TEAM <= 64) {
     constexpr int WAVES = kTeamThreads<TEAM> / 64;
     const int wave = threadIdx.x >> 6;
@@ -187,20 +188,21 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_norm_back(int n, int d, 
     }
     if (wave != WAVES - 1 || (threadIdx.x & 63) >= TEAM) return;
   }
-  float* out = part + blockIdx.x * norm_part_stride(d);
+  float* to_gamma = part ? part + blockIdx.x * norm_part_stride(d) : dgamma;
+  float* to_beta = part ? to_gamma + d : dbeta;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const Piece p(d, c, t);
     if (!p.any()) continue;
     if (WHOLE) {
-      store_piece(out + p.col, dg[c]);
-      store_piece(out + d + p.col, db[c]);
+      if (to_gamma) store_piece(to_gamma + p.col, dg[c]);
+      if (to_beta) store_piece(to_beta + p.col, db[c]);
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (p.own(i, d)) {
-          out[p.col + i] = dg[c][i];
-          out[d + p.col + i] = db[c][i];
+          if (to_gamma) to_gamma[p.col + i] = dg[c][i];
+          if (to_beta) to_beta[p.col + i] = db[c][i];
         }
     }
   }
