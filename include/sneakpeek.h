@@ -437,7 +437,7 @@ typedef enum { SP_ACT_NONE = 0, SP_ACT_RELU = 1 } sp_activation;
 #define SP_MAX_LINEAR_DIM 1048576         /* inputs and outputs of a layer        */
 
 /* workspace_bytes >= SP_OPS_MIN_WORKSPACE: more of it lets long sums (weight gradients of many rows) be split over more of the
- * device; 64 MiB serve every size that was measured.  SP_EINVAL: less, or out NULL. */
+ * device; 32 MiB serve every size that was measured (and are quick to come by).  SP_EINVAL: less, or out NULL. */
 sp_status sp_ops_create(int device_id, int64_t workspace_bytes, sp_ops** out);
 void sp_ops_destroy(sp_ops* ops);
 /* Waits for the stream.  SP_EINVAL if a call on these ops since the last check (or since sp_ops_create) met bad data:

@@ -439,7 +439,7 @@ class TensorList:
         self.packed = load_native().pack_tensors(self.grads, self.out)
 
 
-def Ops(device: int = 0, workspace_bytes: int = 64 << 20):
+def Ops(device: int = 0, workspace_bytes: int = 32 << 20):
     """One sp_ops: the operators that train the heads.  Its methods carry the names of the C entry points; tensors live on the
     ops' device, matrices have contiguous rows.  What does not fit together raises before anything is launched."""
     return _ops_class()(device, workspace_bytes)

@@ -724,3 +724,16 @@ def test_what_does_not_fit_together_is_refused(gpu, ops):
         with pytest.raises(binding.SneakPeekError) as e:
             call()
         assert e.value.status == binding.SP_EINVAL, k
+
+
+@pytest.mark.parametrize("args", [[], ["--bf16"]])
+def test_the_example_learns_and_serves(gpu, args):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_heads.py")
+    spec = importlib.util.spec_from_file_location("train_heads", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    losses, trained, seen, summary = module.main(args + ["--steps", "120"])
+    assert losses[-1] < 0.5 * losses[0] and trained > 0.8 and seen > 0.7
+    assert summary["done"] == 1 and summary["n_scheduled"] > 0
