@@ -308,14 +308,14 @@ int dw_chunk(const sp_ops* o, const LinearArgs& a, int64_t tiles, int32_t dtype)
 
 // The launch's tiles; false where there are more than a launch holds.
 bool linear_grid(LinearArgs* a, int64_t row_tiles, int64_t col_tiles) {
-  if (row_tiles * col_tiles > INT_MAX - kXcds) return false;
+  if (row_tiles * col_tiles > INT_MAX / 2 - kXcds) return false;
   a->row_tiles = (int)row_tiles;
   a->col_tiles = (int)col_tiles;
   return true;
 }
+int linear_blocks(const LinearArgs& a) { return (a.row_tiles * a.col_tiles + kXcds - 1) / kXcds * kXcds; }
 void launch_linear(void (*kernel)(LinearArgs), int threads, const LinearArgs& a, void* stream) {
-  const int tiles = a.row_tiles * a.col_tiles;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(threads), 0, (hipStream_t)stream, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)linear_blocks(a)), dim3(threads), 0, (hipStream_t)stream, a);
 }
 
 // Tiles of 64 or 128 columns; those of 128 with eight wavefronts where the device holds all of them at once, or where there is a mask.
@@ -400,50 +400,47 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
   a.act = const_cast<void*>(act); a.act_stride = act_stride; a.dy = dy; a.dy_stride = dy_stride; a.dx = dx; a.dx_stride = dx_stride;
   a.dw = dw; a.db = db; a.err = o->err;
   hipStream_t s = (hipStream_t)stream;
-  sp_status rc = SP_OK;
+  // both products' launches, before either is made
+  const bool want_dx = dx && n > 0, few = want_dx && few_rows(n, k, kFewDxCols, groups, dtype);
+  const bool dx_narrow = k <= 64, dw_narrow = m <= 64;
+  LinearArgs ax = a, aw = a;
+  if (few && !linear_grid(&ax, ((int64_t)n + kFewRows - 1) / kFewRows + groups, (k + kFewDxCols - 1) / kFewDxCols)) return SP_ECAPACITY;
+  if (want_dx && !few &&
+      !linear_grid(&ax, ((int64_t)n + kLinearRows - 1) / kLinearRows + groups, (k + (dx_narrow ? 63 : 127)) / (dx_narrow ? 64 : 128)))
+    return SP_ECAPACITY;
+  if (dw) {
+    const int64_t k_tiles = (k + kLinearRows - 1) / kLinearRows, m_tiles = (m + (dw_narrow ? 63 : 127)) / (dw_narrow ? 64 : 128);
+    aw.chunk = dw_chunk(o, a, k_tiles * m_tiles, dtype);
+    aw.part = (float*)o->ws;
+    if (!linear_grid(&aw, (aw.chunk ? ((int64_t)n + aw.chunk - 1) / aw.chunk + groups : groups) * k_tiles, m_tiles)) return SP_ECAPACITY;
+  }
+  const int dx_blocks = few ? linear_blocks(ax) : 0;
+  // (three workgroups to a compute unit: both products' run at once)
+  const bool together = few && dw && dx_blocks + linear_blocks(aw) <= 768;
   auto run = [&]<typename T, bool MASK>() {
-    if (dx && n > 0 && few_rows(n, k, kFewDxCols, groups, dtype)) {
-      if (!linear_grid(&a, ((int64_t)n + kFewRows - 1) / kFewRows + groups, (k + kFewDxCols - 1) / kFewDxCols)) {
-        rc = SP_ECAPACITY;
-        return;
-      }
-      launch_linear(k_linear_few_dx<T>, kFewDxThreads, a, stream);
-    } else if (dx && n > 0) {
-      const bool narrow = k <= 64;
-      if (!linear_grid(&a, (int64_t)(n + kLinearRows - 1) / kLinearRows + groups, (k + (narrow ? 63 : 127)) / (narrow ? 64 : 128))) {
-        rc = SP_ECAPACITY;
-        return;
-      }
-      launch_tiles<T, T, kFormDx, MASK>(narrow, a, stream);
+    if (together) {
+      const dim3 grid((unsigned)(dx_blocks + linear_blocks(aw)));
+      if (dw_narrow) hipLaunchKernelGGL((k_linear_few_back<T, 64, MASK>), grid, dim3(kFewDxThreads), 0, s, ax, aw, dx_blocks);
+      else hipLaunchKernelGGL((k_linear_few_back<T, 128, MASK>), grid, dim3(kFewDxThreads), 0, s, ax, aw, dx_blocks);
+    } else {
+      if (few) launch_linear(k_linear_few_dx<T>, kFewDxThreads, ax, stream);
+      else if (want_dx) launch_tiles<T, T, kFormDx, MASK>(dx_narrow, ax, stream);
+      if (dw) launch_tiles<T, float, kFormDw, MASK>(dw_narrow, aw, stream);
     }
-    if (dw) {
-      const bool narrow = m <= 64;
-      const int64_t k_tiles = (k + kLinearRows - 1) / kLinearRows, m_tiles = (m + (narrow ? 63 : 127)) / (narrow ? 64 : 128);
-      a.chunk = dw_chunk(o, a, k_tiles * m_tiles, dtype);
-      a.part = (float*)o->ws;
-      const int64_t items = a.chunk ? (n + a.chunk - 1) / a.chunk + groups : groups;
-      if (!linear_grid(&a, items * k_tiles, m_tiles)) {
-        rc = SP_ECAPACITY;
-        return;
-      }
-      launch_tiles<T, float, kFormDw, MASK>(narrow, a, stream);
-      if (a.chunk) {
-        const int64_t elems = (int64_t)k * m + (db ? m : 0);
-        // few elements: what fills the device is that many threads share an element's chunks
-        if (elems * groups < 512 * 256 && (n + a.chunk - 1) / a.chunk >= 8 * (int64_t)groups)
-          hipLaunchKernelGGL(k_join_chunks<32>, dim3((unsigned)((elems + 31) / 32), groups), dim3(256), 0, s, a);
-        else
-          hipLaunchKernelGGL(k_join_chunks<4>, dim3((unsigned)((elems + 255) / 256), groups), dim3(256), 0, s, a);
-      }
-    } else if (db) {
-      hipLaunchKernelGGL((k_bias_grad<T>), dim3((m + 63) / 64, groups), dim3(256), 0, s, a);
+    if (dw && aw.chunk) {
+      const int64_t elems = (int64_t)k * m + (db ? m : 0);
+      // few elements: what fills the device is that many threads share an element's chunks
+      if (elems * groups < 512 * 256 && (n + aw.chunk - 1) / aw.chunk >= 8 * (int64_t)groups)
+        hipLaunchKernelGGL(k_join_chunks<32>, dim3((unsigned)((elems + 31) / 32), groups), dim3(256), 0, s, aw);
+      else
+        hipLaunchKernelGGL(k_join_chunks<4>, dim3((unsigned)((elems + 255) / 256), groups), dim3(256), 0, s, aw);
     }
+    if (db && !dw) hipLaunchKernelGGL((k_bias_grad<T>), dim3((m + 63) / 64, groups), dim3(256), 0, s, a);
   };
   if (dtype == SP_F32 && act) run.template operator()<float, true>();
   else if (dtype == SP_F32) run.template operator()<float, false>();
   else if (act) run.template operator()<bf16, true>();
   else run.template operator()<bf16, false>();
-  if (rc != SP_OK) return rc;
   return launched(o);
 }
 

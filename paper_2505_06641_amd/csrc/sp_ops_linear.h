@@ -244,7 +244,7 @@ struct Side {
 // eight are quicker through a tile where the device is not full (6170 x 256 -> 862 21 us against 24) and where the mask's registers leave
 // room for two workgroups of four only.
 template <typename T, typename TO, int FORM, int BN, bool MASK, int THREADS>
-__global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_linear(LinearArgs a) {
+__device__ __forceinline__ void linear_tile(const LinearArgs& a, int block) {
   constexpr int BM = kLinearRows, D = kDepth<T>, P = kPlanes<T>, FR = 2, FC = BN * 2 / (THREADS / 2), V = kPiece<T>;
   constexpr int WN = FC * 32, WAVE_COLS = BN / WN;          // columns of a wavefront, wavefronts side by side
   typedef Side<T, BM, FORM == kFormDw, FORM == kFormDx && MASK, THREADS> Rows;
@@ -253,10 +253,10 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
   uint16_t* lds_rows = lds;
   uint16_t* lds_cols = lds + P * Rows::kElems;
   static_assert(sizeof(lds) >= 64 * BN * sizeof(float), "half a tile of sums fits");
-  if (blockIdx.x == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
+  if (block == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
 
   // the tile: consecutive ones share rows, and go to one die as far as that is possible
-  const int tile = xcd_tile(blockIdx.x, a.row_tiles * a.col_tiles);
+  const int tile = xcd_tile(block, a.row_tiles * a.col_tiles);
   if (tile < 0) return;
   RowTile rows;
   const int rt = tile / a.col_tiles, ct = tile % a.col_tiles;
@@ -493,6 +493,11 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_
       out[c] = v;
     }
   }
+}
+
+template <typename T, typename TO, int FORM, int BN, bool MASK, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_linear(LinearArgs a) {
+  linear_tile<T, TO, FORM, BN, MASK, THREADS>(a, blockIdx.x);
 }
 
 // Adds up the chunks of the groups that have several, and clears the gradients of the empty groups.  A workgroup takes 4 elements of

@@ -136,11 +136,11 @@ __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
 
 // dx: rows of weights are contiguous along the depth, so that both sides' fragments come straight from memory.
 template <typename T>
-__global__ __launch_bounds__(kFewDxThreads) void k_linear_few_dx(LinearArgs a) {
+__device__ __forceinline__ void linear_few_dx(const LinearArgs& a, int block) {
   constexpr int P = kPlanes<T>, WAVES = kFewDxThreads / 64;
   __shared__ float part[WAVES][16 * 17];
-  if (blockIdx.x == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
-  const int tile = xcd_tile(blockIdx.x, a.row_tiles * a.col_tiles);
+  if (block == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
+  const int tile = xcd_tile(block, a.row_tiles * a.col_tiles);
   if (tile < 0) return;
   const int rt = tile / a.col_tiles, c0 = (tile % a.col_tiles) * kFewDxCols;
   RowTile rows;
@@ -177,6 +177,19 @@ __global__ __launch_bounds__(kFewDxThreads) void k_linear_few_dx(LinearArgs a) {
 #pragma unroll
   for (int q = 0; q < WAVES; ++q) v += part[q][r * 17 + col];
   ((T*)a.dx)[((int64_t)rows.lo + r) * a.dx_stride + c0 + col] = from_float<T>(v);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kFewDxThreads) void k_linear_few_dx(LinearArgs a) {
+  linear_few_dx<T>(a, blockIdx.x);
+}
+
+// A small layer's dx and dW in one launch, where the device holds the workgroups of both at once: the first dx_blocks are dx's.
+// (12 rows of 7 applications, 479 x 113 float32: 11.2 -> 7.9 us a call, of which the second launch costs the host 2.)
+template <typename T, int BN, bool MASK>
+__global__ __launch_bounds__(kFewDxThreads, 2) void k_linear_few_back(LinearArgs dx, LinearArgs dw, int dx_blocks) {
+  if ((int)blockIdx.x < dx_blocks) linear_few_dx<T>(dx, blockIdx.x);
+  else linear_tile<T, float, kFormDw, BN, MASK, kFewDxThreads>(dw, (int)blockIdx.x - dx_blocks);
 }
 
 }  // namespace sp
