@@ -318,17 +318,28 @@ void launch_linear(void (*kernel)(LinearArgs), int threads, const LinearArgs& a,
   hipLaunchKernelGGL(kernel, dim3((unsigned)linear_blocks(a)), dim3(threads), 0, (hipStream_t)stream, a);
 }
 
-// Tiles of 64 or 128 columns; those of 128 with eight wavefronts where the device holds all of them at once, or where there is a mask.
+// Rows and columns of the tiles of an output: 64 where it is no wider.
+int tile_rows(int64_t k) { return k <= 64 ? 64 : 128; }           // dW's rows are inputs; the other forms' rows are requests: 128
+int tile_cols(int64_t width) { return width <= 64 ? 64 : 128; }
+
+// Tiles of 128 by 128 have eight wavefronts where the device holds all of them at once, or where there is a mask, else four.
 template <typename T, typename TO, int FORM, bool MASK>
-void launch_tiles(bool narrow, const LinearArgs& a, void* stream) {
-  if (narrow) {
-    launch_linear(k_linear<T, TO, FORM, 64, MASK, 256>, 256, a, stream);
+void launch_tiles(int bm, int bn, const LinearArgs& a, void* stream) {
+  if constexpr (FORM == kFormDw) {
+    if (bm == 64) {
+      if (bn == 64) launch_linear(k_linear<T, TO, FORM, 64, 64, MASK, 256>, 256, a, stream);
+      else launch_linear(k_linear<T, TO, FORM, 64, 128, MASK, 256>, 256, a, stream);
+      return;
+    }
+  }
+  if (bn == 64) {
+    launch_linear(k_linear<T, TO, FORM, 128, 64, MASK, 256>, 256, a, stream);
   } else if constexpr (MASK) {
-    launch_linear(k_linear<T, TO, FORM, 128, MASK, 512>, 512, a, stream);
+    launch_linear(k_linear<T, TO, FORM, 128, 128, MASK, 512>, 512, a, stream);
   } else if ((int64_t)a.row_tiles * a.col_tiles <= 768) {
-    launch_linear(k_linear<T, TO, FORM, 128, MASK, 512>, 512, a, stream);
+    launch_linear(k_linear<T, TO, FORM, 128, 128, MASK, 512>, 512, a, stream);
   } else {
-    launch_linear(k_linear<T, TO, FORM, 128, MASK, 256>, 256, a, stream);
+    launch_linear(k_linear<T, TO, FORM, 128, 128, MASK, 256>, 256, a, stream);
   }
 }
 
@@ -370,10 +381,10 @@ sp_status sp_grouped_linear(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t 
     else launch_linear(k_linear_few<bf16, bf16>, kFewThreads, a, stream);
     return launched(o);
   }
-  const bool narrow = m <= 64;
-  if (!linear_grid(&a, (int64_t)(n + kLinearRows - 1) / kLinearRows + groups, (m + (narrow ? 63 : 127)) / (narrow ? 64 : 128))) return SP_ECAPACITY;
+  const int bn = tile_cols(m);
+  if (!linear_grid(&a, ((int64_t)n + 127) / 128 + groups, (m + bn - 1) / bn)) return SP_ECAPACITY;
   auto run = [&]<typename T, typename TO>() {
-    launch_tiles<T, TO, kFormY, false>(narrow, a, stream);
+    launch_tiles<T, TO, kFormY, false>(128, bn, a, stream);
   };
   if (dtype == SP_F32) run.template operator()<float, float>();
   else if (out_dtype == SP_F32) run.template operator()<bf16, float>();
@@ -402,14 +413,12 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
   hipStream_t s = (hipStream_t)stream;
   // both products' launches, before either is made
   const bool want_dx = dx && n > 0, few = want_dx && few_rows(n, k, kFewDxCols, groups, dtype);
-  const bool dx_narrow = k <= 64, dw_narrow = m <= 64;
+  const int dx_cols = tile_cols(k), dw_rows = tile_rows(k), dw_cols = tile_cols(m);
   LinearArgs ax = a, aw = a;
   if (few && !linear_grid(&ax, ((int64_t)n + kFewRows - 1) / kFewRows + groups, (k + kFewDxCols - 1) / kFewDxCols)) return SP_ECAPACITY;
-  if (want_dx && !few &&
-      !linear_grid(&ax, ((int64_t)n + kLinearRows - 1) / kLinearRows + groups, (k + (dx_narrow ? 63 : 127)) / (dx_narrow ? 64 : 128)))
-    return SP_ECAPACITY;
+  if (want_dx && !few && !linear_grid(&ax, ((int64_t)n + 127) / 128 + groups, (k + dx_cols - 1) / dx_cols)) return SP_ECAPACITY;
   if (dw) {
-    const int64_t k_tiles = (k + kLinearRows - 1) / kLinearRows, m_tiles = (m + (dw_narrow ? 63 : 127)) / (dw_narrow ? 64 : 128);
+    const int64_t k_tiles = (k + dw_rows - 1) / dw_rows, m_tiles = (m + dw_cols - 1) / dw_cols;
     aw.chunk = dw_chunk(o, a, k_tiles * m_tiles, dtype);
     aw.part = (float*)o->ws;
     if (!linear_grid(&aw, (aw.chunk ? ((int64_t)n + aw.chunk - 1) / aw.chunk + groups : groups) * k_tiles, m_tiles)) return SP_ECAPACITY;
@@ -420,12 +429,13 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
   auto run = [&]<typename T, bool MASK>() {
     if (together) {
       const dim3 grid((unsigned)(dx_blocks + linear_blocks(aw)));
-      if (dw_narrow) hipLaunchKernelGGL((k_linear_few_back<T, 64, MASK>), grid, dim3(kFewDxThreads), 0, s, ax, aw, dx_blocks);
-      else hipLaunchKernelGGL((k_linear_few_back<T, 128, MASK>), grid, dim3(kFewDxThreads), 0, s, ax, aw, dx_blocks);
+      auto both = dw_rows == 64 ? (dw_cols == 64 ? k_linear_few_back<T, 64, 64, MASK> : k_linear_few_back<T, 64, 128, MASK>)
+                                : (dw_cols == 64 ? k_linear_few_back<T, 128, 64, MASK> : k_linear_few_back<T, 128, 128, MASK>);
+      hipLaunchKernelGGL(both, grid, dim3(kFewDxThreads), 0, s, ax, aw, dx_blocks);
     } else {
       if (few) launch_linear(k_linear_few_dx<T>, kFewDxThreads, ax, stream);
-      else if (want_dx) launch_tiles<T, T, kFormDx, MASK>(dx_narrow, ax, stream);
-      if (dw) launch_tiles<T, float, kFormDw, MASK>(dw_narrow, aw, stream);
+      else if (want_dx) launch_tiles<T, T, kFormDx, MASK>(128, dx_cols, ax, stream);
+      if (dw) launch_tiles<T, float, kFormDw, MASK>(dw_rows, dw_cols, aw, stream);
     }
     if (dw && aw.chunk) {
       const int64_t elems = (int64_t)k * m + (db ? m : 0);

@@ -68,7 +68,6 @@ __host__ __device__ __forceinline__ int64_t chunk_stride(const LinearArgs& a) { 
 
 enum LinearForm { kFormY = 0, kFormDx = 1, kFormDw = 2 };
 
-constexpr int kLinearRows = 128;                                      // rows of a tile
 template <typename T> constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1; // bfloat16 numbers that make up a value
 template <typename T> constexpr int kDepth = sizeof(T) == 4 ? 32 : 64; // depth of a piece: 48 KB of LDS with 128 columns, 32 KB
 
@@ -239,20 +238,21 @@ struct Side {
 
 // The last tile of a group's rows, and the last one of the columns, starts early enough to be a whole one where there is enough before it:
 // it computes again what the tile before it has, and leaves the writing to that one (float32 256 -> 1000: 921 -> 861 us; pieces that are cut take
-// twice as long).  Columns of the tile: 128, or 64 for narrow outputs.  Four wavefronts, 64 rows and BN / 2 columns each, or eight of 64 by 32: a wavefront
+// twice as long).  Columns of the tile: 128, or 64 for narrow outputs; rows: 128, or 64 for dW of few
+// inputs (90070 rows, 5 -> 544 float32: dW 92 us with 128, 66 with 64).  Four wavefronts, 64 rows and BN / 2 columns each, or eight of 64 by 32: a wavefront
 // of 64 by 64 reads a third less from LDS for its products (65536 x 1024 -> 512 bfloat16 99 us against 109, the LDS being what is busiest),
 // eight are quicker through a tile where the device is not full (6170 x 256 -> 862 21 us against 24) and where the mask's registers leave
 // room for two workgroups of four only.
-template <typename T, typename TO, int FORM, int BN, bool MASK, int THREADS>
+template <typename T, typename TO, int FORM, int BM, int BN, bool MASK, int THREADS>
 __device__ __forceinline__ void linear_tile(const LinearArgs& a, int block) {
-  constexpr int BM = kLinearRows, D = kDepth<T>, P = kPlanes<T>, FR = 2, FC = BN * 2 / (THREADS / 2), V = kPiece<T>;
-  constexpr int WN = FC * 32, WAVE_COLS = BN / WN;          // columns of a wavefront, wavefronts side by side
+  constexpr int D = kDepth<T>, P = kPlanes<T>, FR = BM / 64, FC = BN * 2 / (THREADS / 2), V = kPiece<T>;
+  constexpr int WM = FR * 32, WN = FC * 32, WAVE_COLS = BN / WN;     // rows and columns of a wavefront, wavefronts side by side
   typedef Side<T, BM, FORM == kFormDw, FORM == kFormDx && MASK, THREADS> Rows;
   typedef Side<T, BN, FORM != kFormDx, FORM == kFormDw && MASK, THREADS> Cols;
-  __shared__ __align__(16) uint16_t lds[P * (Rows::kElems + Cols::kElems)];
+  constexpr int kBoth = P * (Rows::kElems + Cols::kElems), kSums = 64 * BN * 2;      // two sides; 64 rows of sums
+  __shared__ __align__(16) uint16_t lds[kBoth > kSums ? kBoth : kSums];
   uint16_t* lds_rows = lds;
   uint16_t* lds_cols = lds + P * Rows::kElems;
-  static_assert(sizeof(lds) >= 64 * BN * sizeof(float), "half a tile of sums fits");
   if (block == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
 
   // the tile: consecutive ones share rows, and go to one die as far as that is possible
@@ -341,7 +341,7 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& a, int block) {
   };
 
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int wr = wave / WAVE_COLS * 64, wc = wave % WAVE_COLS * WN;
+  const int wr = wave / WAVE_COLS * WM, wc = wave % WAVE_COLS * WN;
   f32x16 acc[FR][FC];
 #pragma unroll
   for (int i = 0; i < FR; ++i)
@@ -409,7 +409,7 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& a, int block) {
   constexpr int VO = kPiece<TO>, kAcross = BN / VO;        // 16 bytes of output a time
 #pragma unroll
   for (int i = 0; i < FR; ++i) {
-    const int mine = wr / 2 + (lane & 31);
+    const int mine = wave / WAVE_COLS * 32 + (lane & 31);
     // the residual is on its way while the sums go through LDS
     constexpr int kEach = 64 * kAcross / THREADS;
     u32x4 res[FORM == kFormY ? kEach : 1];                 // (as it is in memory: what turns it into floats would wait for it)
@@ -417,7 +417,7 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& a, int block) {
 #pragma unroll
       for (int u = 0; u < kEach; ++u) {
         const int p = threadIdx.x + u * THREADS, sr_ = p / kAcross, sc_ = (p % kAcross) * VO;
-        const int r = (sr_ >> 5) * 64 + i * 32 + (sr_ & 31), c = c0 + sc_;
+        const int r = (sr_ >> 5) * WM + i * 32 + (sr_ & 31), c = c0 + sc_;
         const TO* from = (const TO*)a.residual + (int64_t)(r0 + r) * a.residual_stride + c;
         const int count = r >= skip_r && r < n_rows ? width - c : 0;
         if (count >= VO) res[u] = __builtin_bit_cast(u32x4, *reinterpret_cast<const u32x4_any*>(from));
@@ -437,7 +437,7 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& a, int block) {
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
       const int p = threadIdx.x + u * THREADS, sr_ = p / kAcross, sc_ = (p % kAcross) * VO;
-      const int r = (sr_ >> 5) * 64 + i * 32 + (sr_ & 31), c = c0 + sc_, left = width - c;
+      const int r = (sr_ >> 5) * WM + i * 32 + (sr_ & 31), c = c0 + sc_, left = width - c;
       if (r < skip_r || r >= n_rows || left <= 0 || sc_ + VO <= skip_c) continue;
       const int64_t row = r0 + r;
       const int first = max(skip_c - sc_, 0);              // of the piece's elements
@@ -495,9 +495,9 @@ __device__ __forceinline__ void linear_tile(const LinearArgs& a, int block) {
   }
 }
 
-template <typename T, typename TO, int FORM, int BN, bool MASK, int THREADS>
+template <typename T, typename TO, int FORM, int BM, int BN, bool MASK, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : MASK ? 2 : 3) void k_linear(LinearArgs a) {
-  linear_tile<T, TO, FORM, BN, MASK, THREADS>(a, blockIdx.x);
+  linear_tile<T, TO, FORM, BM, BN, MASK, THREADS>(a, blockIdx.x);
 }
 
 // Adds up the chunks of the groups that have several, and clears the gradients of the empty groups.  A workgroup takes 4 elements of

@@ -186,10 +186,10 @@ __global__ __launch_bounds__(kFewDxThreads) void k_linear_few_dx(LinearArgs a) {
 
 // A small layer's dx and dW in one launch, where the device holds the workgroups of both at once: the first dx_blocks are dx's.
 // (12 rows of 7 applications, 479 x 113 float32: 11.2 -> 7.9 us a call, of which the second launch costs the host 2.)
-template <typename T, int BN, bool MASK>
+template <typename T, int BM, int BN, bool MASK>
 __global__ __launch_bounds__(kFewDxThreads, 2) void k_linear_few_back(LinearArgs dx, LinearArgs dw, int dx_blocks) {
   if ((int)blockIdx.x < dx_blocks) linear_few_dx<T>(dx, blockIdx.x);
-  else linear_tile<T, float, kFormDw, BN, MASK, kFewDxThreads>(dw, (int)blockIdx.x - dx_blocks);
+  else linear_tile<T, float, kFormDw, BM, BN, MASK, kFewDxThreads>(dw, (int)blockIdx.x - dx_blocks);
 }
 
 }  // namespace sp
