@@ -435,6 +435,7 @@ typedef enum { SP_ACT_NONE = 0, SP_ACT_RELU = 1 } sp_activation;
 #define SP_OPS_MIN_WORKSPACE 1048576      /* bytes                                */
 #define SP_MAX_NORM_DIM 16384             /* columns of a normalised row          */
 #define SP_MAX_LINEAR_DIM 1048576         /* inputs and outputs of a layer        */
+#define SP_MAX_LINEAR_STRIDE 8388608      /* row strides of x, dy and act, in elements */
 
 /* workspace_bytes >= SP_OPS_MIN_WORKSPACE: more of it lets long sums (weight gradients of many rows) be split over more of the
  * device; 32 MiB serve every size that was measured (and are quick to come by).  SP_EINVAL: less, or out NULL. */
@@ -462,7 +463,10 @@ sp_status sp_layer_norm_backward(sp_ops* ops, int32_t n, int32_t d, int32_t dtyp
  *     on belong to no group and get y = 0
  *   y [n, m] out_dtype (dtype, or SP_F32 from SP_BF16); residual [n, m] out_dtype or NULL (may be y)
  *   act_out [n, m] out_dtype or NULL: act(x_i W_g + b_g) without the residual, which the backward pass of a layer with both an
- *     activation and a residual asks for */
+ *     activation and a residual asks for
+ * bfloat16 products are exact, sums are float32.  Float32 factors are taken by the matrix cores as three bfloat16 numbers each, with the
+ * six products that count: within 2^-24 of the sum of the products' magnitudes.  An infinite float32 factor makes the results that it
+ * enters NaN, NaN stays NaN; neither reaches another row's, group's or column's results.  */
 sp_status sp_grouped_linear(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype, const void* x, int64_t x_stride,
                             const int32_t* offsets, const void* w, const float* bias, int32_t activation, int32_t out_dtype,
                             const void* residual, int64_t residual_stride, void* y, int64_t y_stride, void* act_out, int64_t act_stride,
@@ -471,7 +475,8 @@ sp_status sp_grouped_linear(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_
  *   dx_i = dz_i W_g^T      dw_g = sum over the group's rows of x_i^T dz_i      db_g = sum of dz_i
  *   dy [n, m] dtype; act [n, m] dtype or NULL: the layer's y (or act_out, if it has a residual), for SP_ACT_RELU
  *   dx [n, k] dtype or NULL (0 for rows of no group); dw [groups, k, m] float or NULL; db [groups, m] float or NULL (0 for empty
- *     groups).  x is read for dw only, w for dx only (either may be NULL otherwise).  The residual's gradient is dy itself. */
+ *     groups).  x is read for dw only, w for dx only (either may be NULL otherwise).  The residual's gradient is dy itself.  dw and
+ *     db are sums over the rows in float32; long groups are summed in parts that are then added in their order. */
 sp_status sp_grouped_linear_backward(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype, const void* dy,
                                      int64_t dy_stride, const void* act, int64_t act_stride, const void* x, int64_t x_stride,
                                      const int32_t* offsets, const void* w, void* dx, int64_t dx_stride, float* dw, float* db,

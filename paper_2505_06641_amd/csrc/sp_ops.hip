@@ -132,7 +132,7 @@ sp_status sp_layer_norm(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const vo
     with_team((d + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
       if constexpr (TEAM * C * kPiece<T> <= SP_MAX_NORM_DIM) {
         constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
-        const int blocks = std::min((n + rows - 1) / rows, kNormBlocks);
+        const int blocks = (int)std::min<int64_t>(((int64_t)n + rows - 1) / rows, kNormBlocks);
         hipLaunchKernelGGL((d % kPiece<T> ? k_norm<T, TEAM, C, false> : k_norm<T, TEAM, C, true>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)x, x_stride, gamma,
                            beta, eps, (T*)y, y_stride, mean_out, rstd_out);
       }
@@ -194,7 +194,7 @@ sp_status sp_cross_entropy(sp_ops* o, int32_t n, int32_t c_max, int32_t dtype, c
   auto run = [&]<typename T, typename TO>() {
     const bool fits = with_team(((int64_t)c_max + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
       constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
-      const int blocks = std::min((n + rows - 1) / rows, kLossBlocks);
+      const int blocks = (int)std::min<int64_t>(((int64_t)n + rows - 1) / rows, kLossBlocks);
       hipLaunchKernelGGL((k_loss<T, TO, TEAM, C>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, c_max, (const T*)logits,
                          logits_stride, n_apps, app, n_classes, label, weight, scale, loss, (TO*)dlogits, dlogits_stride, o->err);
     });
@@ -367,6 +367,7 @@ sp_status sp_grouped_linear(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t 
   if (!aligned(x, dtype) || !aligned(w, dtype) || !aligned(y, out_dtype) || !aligned(residual, out_dtype) || !aligned(act_out, out_dtype) ||
       !aligned4(offsets) || !aligned4(bias))
     return SP_EINVAL;
+  if (x_stride > SP_MAX_LINEAR_STRIDE) return SP_ECAPACITY;
   if (n == 0) return SP_OK;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
@@ -403,6 +404,8 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
   if (!aligned(dy, dtype) || !aligned(act, dtype) || !aligned(x, dtype) || !aligned(w, dtype) || !aligned(dx, dtype) || !aligned4(offsets) ||
       !aligned4(dw) || !aligned4(db))
     return SP_EINVAL;
+  if (dy_stride > SP_MAX_LINEAR_STRIDE || (act && act_stride > SP_MAX_LINEAR_STRIDE) || (dw && x_stride > SP_MAX_LINEAR_STRIDE))
+    return SP_ECAPACITY;
   if ((n == 0 || !dx) && !dw && !db) return SP_OK;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;

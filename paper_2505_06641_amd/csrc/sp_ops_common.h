@@ -160,7 +160,7 @@ __device__ __forceinline__ bool find_row_tile(const int32_t* offsets, int n_grou
     }
     int s0 = __shfl_up(e, 1);
     if (lane == 0) s0 = end;
-    const int tiles = g <= n_groups ? (e - s0 + tile_rows - 1) / tile_rows : 0;
+    const int tiles = g <= n_groups ? (int)(((uint32_t)(e - s0) + (uint32_t)tile_rows - 1u) / (uint32_t)tile_rows) : 0;
     const int upto = before + (int)wave_scan_incl((uint32_t)tiles);
     const unsigned long long has = __ballot(upto > tile);
     if (has) {

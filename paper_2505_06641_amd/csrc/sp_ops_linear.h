@@ -15,7 +15,8 @@
 // Float32: a value is the sum of three bfloat16 numbers, each the rounded rest of the ones before it (8 + 8 + 8 significant bits: what
 // is left is below 2^-27 of the value).  Of the nine products of two such sums the six largest are taken, each exact in the float32
 // sum; the three others are below 2^-25 of the product together.  Six instructions of the bfloat16 rate are 2.6 times the float32
-// instruction's rate.  An infinite factor (or one that rounds to one in bfloat16, from 3.39e38 on) gives NaN.
+// instruction's rate.  An infinite factor (or one that rounds to one in bfloat16, from 3.39e38 on) makes its results NaN: its rest is
+// one.
 #pragma once
 #include "sp_common.h"
 #include "sp_ops_common.h"
@@ -523,7 +524,7 @@ __global__ __launch_bounds__(256) void k_join_chunks(LinearArgs a) {
     }
     int s0 = __shfl_up(e, 1);
     if (lane == 0) s0 = end;
-    const int chunks = q <= g ? (e - s0 + a.chunk - 1) / a.chunk : 0;
+    const int chunks = q <= g ? (int)(((uint32_t)(e - s0) + (uint32_t)a.chunk - 1u) / (uint32_t)a.chunk) : 0;
     const int upto = before + (int)wave_scan_incl((uint32_t)chunks);
     if (g - base < 64) {
       lo = __shfl(upto - chunks, g - base);

@@ -117,3 +117,13 @@ def test_clip_refuses(lib, handle):
     # the handle's workspace (0 bytes here) is too small for any tensor's sums
     assert lib.sp_clip_grad_norm(*base.values()) == ECAPACITY
     assert lib.sp_clip_grad_norm(*dict(base, sizes=size(1 << 45, 4)).values()) == ECAPACITY
+
+
+def test_row_strides_beyond_what_a_tile_reaches_are_refused(lib, handle):
+    forward = dict(ops=handle, n=4, k=8, m=16, groups=2, dtype=0, x=P, xs=1 << 24, offsets=P, w=P, bias=P, act=1, out=0, r=P, rs=16, y=P, ys=16,
+                   act_out=P, acts=16, stream=None)
+    assert lib.sp_grouped_linear(*forward.values()) == ECAPACITY
+    back = dict(ops=handle, n=4, k=8, m=16, groups=2, dtype=1, dy=P, dys=16, act=P, acts=16, x=P, xs=8, offsets=P, w=P, dx=P, dxs=8, dw=P,
+                db=P, stream=None)
+    for key in ("dys", "acts", "xs"):
+        assert lib.sp_grouped_linear_backward(*dict(back, **{key: 1 << 24}).values()) == ECAPACITY, key
