@@ -130,6 +130,18 @@ __device__ __forceinline__ float team_max(float v, float* lds) {
 // The threads of a workgroup whose teams take one row each at a time.
 template <int TEAM> constexpr int kTeamThreads = TEAM > 256 ? TEAM : 256;
 
+// Inclusive prefix maximum across a wavefront of values that are not negative, as wave_scan_incl adds them up: a lane that a step does
+// not write sees 0.
+__device__ __forceinline__ int wave_scan_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));   // row_shr:1
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));   // row_shr:2
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));   // row_shr:4
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));   // row_shr:8
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));   // row_bcast:15 into rows 1 and 3
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));   // row_bcast:31 into rows 2 and 3
+  return x;
+}
+
 // The rows of group g.  Offsets that are not 0 <= ... <= n in order are reported by whoever walks them all; here they are
 // only kept inside the arrays.
 __device__ __forceinline__ void group_rows(const int32_t* offsets, int n, int g, int* lo, int* hi) {
@@ -153,11 +165,7 @@ __device__ __forceinline__ bool find_row_tile(const int32_t* offsets, int n_grou
     const int g = base + lane;
     int e = g < n_groups ? min(max(offsets[g + 1], 0), n) : n;
     e = max(e, end);
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {            // ends in order, whatever the offsets say
-      const int o = __shfl_up(e, s);
-      if (lane >= s) e = max(e, o);
-    }
+    e = wave_scan_max(e);                        // ends in order, whatever the offsets say
     int s0 = __shfl_up(e, 1);
     if (lane == 0) s0 = end;
     const int tiles = g <= n_groups ? (int)(((uint32_t)(e - s0) + (uint32_t)tile_rows - 1u) / (uint32_t)tile_rows) : 0;

@@ -517,11 +517,7 @@ __global__ __launch_bounds__(256) void k_join_chunks(LinearArgs a) {
     const int q = base + lane;
     int e = q <= g ? min(max(a.offsets[q + 1], 0), a.n) : 0;
     e = max(e, end);
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-      const int o = __shfl_up(e, s);
-      if (lane >= s) e = max(e, o);
-    }
+    e = wave_scan_max(e);
     int s0 = __shfl_up(e, 1);
     if (lane == 0) s0 = end;
     const int chunks = q <= g ? (int)(((uint32_t)(e - s0) + (uint32_t)a.chunk - 1u) / (uint32_t)a.chunk) : 0;
