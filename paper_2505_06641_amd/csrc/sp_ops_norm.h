@@ -17,7 +17,7 @@ __host__ __device__ __forceinline__ int64_t norm_part_stride(int d) { return (2 
 // A team's columns: piece c of lane t holds columns (c * TEAM + t) * V on.  Where a row is no whole number of pieces (not WHOLE), its
 // last piece starts V columns before the row's end instead and holds `skip` columns that are another lane's as well: read whole like any
 // other, counted from `skip` on, and written with the values that the other lane writes there too.  (Element by element that piece
-// costs more than all others of the row: 665558 bfloat16 rows of 111 columns 145 us, so XX us, of 112 columns 67 us.)  Rows shorter than
+// costs more than all others of the row: 665558 bfloat16 rows of 111 columns 145 us, so 72 us, of 112 columns 67 us.)  Rows shorter than
 // a piece are read and written element by element.
 template <typename T, int TEAM, bool WHOLE>
 struct NormPiece {
