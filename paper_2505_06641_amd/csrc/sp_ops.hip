@@ -426,15 +426,15 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
     aw.part = (float*)o->ws;
     if (!linear_grid(&aw, (aw.chunk ? ((int64_t)n + aw.chunk - 1) / aw.chunk + groups : groups) * k_tiles, m_tiles)) return SP_ECAPACITY;
   }
-  const int dx_blocks = few ? linear_blocks(ax) : 0;
-  // (three workgroups to a compute unit: both products' run at once)
-  const bool together = few && dw && dx_blocks + linear_blocks(aw) <= 768;
+  const int dx_blocks = few ? linear_blocks(ax) : 0, dw_blocks = dw ? linear_blocks(aw) : 0;
+  // (three workgroups to a compute unit: all of dW's run at once)
+  const bool together = few && dw && dw_blocks <= 768;
   auto run = [&]<typename T, bool MASK>() {
     if (together) {
-      const dim3 grid((unsigned)(dx_blocks + linear_blocks(aw)));
+      const dim3 grid((unsigned)(dx_blocks + dw_blocks));
       auto both = dw_rows == 64 ? (dw_cols == 64 ? k_linear_few_back<T, 64, 64, MASK> : k_linear_few_back<T, 64, 128, MASK>)
                                 : (dw_cols == 64 ? k_linear_few_back<T, 128, 64, MASK> : k_linear_few_back<T, 128, 128, MASK>);
-      hipLaunchKernelGGL(both, grid, dim3(kFewDxThreads), 0, s, ax, aw, dx_blocks);
+      hipLaunchKernelGGL(both, grid, dim3(kFewDxThreads), 0, s, ax, aw, dw_blocks);
     } else {
       if (few) launch_linear(k_linear_few_dx<T>, kFewDxThreads, ax, stream);
       else if (want_dx) launch_tiles<T, T, kFormDx, MASK>(128, dx_cols, ax, stream);
