@@ -286,10 +286,12 @@ namespace {
 
 // Whether a layer is better off in pieces of 16 rows than in tiles of 128: as long as the device holds about all of the small pieces'
 // workgroups at once, their shorter way through the depth wins (bfloat16 1024 -> 1024: 512 rows 15 us against 17, 1024 rows 24 against 17;
-// float32: 1024 rows 52 against 66, 2048 rows 93 against 67; 512 -> 256 of one request: 5 against 14).
-bool few_rows(int64_t n, int64_t width, int cols, int64_t groups, int32_t dtype) {
+// float32: 1024 rows 52 against 66, 2048 rows 93 against 67; 512 -> 256 of one request: 5 against 14).  bfloat16's smaller bound is that of
+// float32 where one turn of dx's wavefronts covers the depth (gradients of 4096 rows, 128 -> 64 with a mask 12.9 us against 15.9, 2048 rows,
+// 256 -> 64 11.8 against 14.8; but of 600 rows, 1024 -> 256 25 against 23).
+bool few_rows(int64_t n, int64_t width, int cols, int64_t groups, int32_t dtype, int64_t depth) {
   const int64_t workgroups = ((n + kFewRows - 1) / kFewRows + std::min(n, groups)) * ((width + cols - 1) / cols);
-  return workgroups <= (dtype == SP_F32 ? 2560 : 1280);
+  return workgroups <= (dtype == SP_F32 || (cols == kFewDxCols && depth <= kFewDxThreads / 64 * 32) ? 2560 : 1280);
 }
 
 // Rows of a group that one workgroup adds up for dW (0: all).  A workgroup takes about 19 ns a row (float32 55 ns), and every chunk's
@@ -375,7 +377,7 @@ sp_status sp_grouped_linear(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t 
   a.n = n; a.k = k; a.m = m; a.groups = groups; a.x = x; a.x_stride = x_stride; a.offsets = offsets; a.w = w; a.bias = bias;
   a.relu = activation == SP_ACT_RELU; a.residual = residual; a.residual_stride = residual_stride; a.y = y; a.y_stride = y_stride;
   a.act = act_out; a.act_stride = act_stride; a.err = o->err;
-  if (few_rows(n, m, kFewCols, groups, dtype)) {
+  if (few_rows(n, m, kFewCols, groups, dtype, k)) {
     if (!linear_grid(&a, ((int64_t)n + kFewRows - 1) / kFewRows + groups, (m + kFewCols - 1) / kFewCols)) return SP_ECAPACITY;
     if (dtype == SP_F32) launch_linear(k_linear_few<float, float>, kFewThreads, a, stream);
     else if (out_dtype == SP_F32) launch_linear(k_linear_few<bf16, float>, kFewThreads, a, stream);
@@ -415,7 +417,7 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
   a.dw = dw; a.db = db; a.err = o->err;
   hipStream_t s = (hipStream_t)stream;
   // both products' launches, before either is made
-  const bool want_dx = dx && n > 0, few = want_dx && few_rows(n, k, kFewDxCols, groups, dtype);
+  const bool want_dx = dx && n > 0, few = want_dx && few_rows(n, k, kFewDxCols, groups, dtype, m);
   const int dx_cols = tile_cols(k), dw_rows = tile_rows(k), dw_cols = tile_cols(m);
   LinearArgs ax = a, aw = a;
   if (few && !linear_grid(&ax, ((int64_t)n + kFewRows - 1) / kFewRows + groups, (k + kFewDxCols - 1) / kFewDxCols)) return SP_ECAPACITY;
