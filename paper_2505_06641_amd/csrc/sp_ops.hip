@@ -429,7 +429,7 @@ sp_status sp_grouped_linear_backward(sp_ops* o, int32_t n, int32_t k, int32_t m,
     if (!linear_grid(&aw, (aw.chunk ? ((int64_t)n + aw.chunk - 1) / aw.chunk + groups : groups) * k_tiles, m_tiles)) return SP_ECAPACITY;
   }
   const int dx_blocks = few ? linear_blocks(ax) : 0, dw_blocks = dw ? linear_blocks(aw) : 0;
-  // (three workgroups to a compute unit: all of dW's run at once)
+  // (two or three workgroups to a compute unit: all of dW's run at once, or nearly)
   const bool together = few && dw && dw_blocks <= 768;
   auto run = [&]<typename T, bool MASK>() {
     if (together) {

@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kFewDxThreads) void k_linear_few_dx(LinearArgs a) {
   linear_few_dx<T>(a, blockIdx.x);
 }
 
-// A small layer's dx and dW in one launch, where the device holds all of dW's workgroups at once: the first dw_blocks are dW's, whose way
+// A small layer's dx and dW in one launch, where the device holds about all of dW's workgroups at once: the first dw_blocks are dW's, whose way
 // through the rows is the longer one, and dx's run beside and behind them.
 // (12 rows of 7 applications, 479 x 113 float32: 11.2 -> 7.9 us a call, of which the second launch costs the host 2;
 // 3000 rows of 3, 64 x 64 bfloat16: 11.3 -> 8.6; 2048 rows of 8, 256 x 256 float32 with a mask: 34 -> 30.)
