@@ -109,7 +109,8 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_loss(int n, int c_max, c
   }
 }
 
-// Rows of any width: one workgroup to a row.
+// Rows of any width: one workgroup to a row.  Columns are counted without a sign: the last step of a row of close to 2^31 classes ends
+// behind 2^31 - 1.
 template <typename T, typename TO>
 __global__ __launch_bounds__(1024) void k_loss_wide(int n, int c_max, const T* z, int64_t z_stride, int n_apps,
                                                     const int32_t* __restrict__ app, const int32_t* __restrict__ n_classes,
@@ -126,9 +127,9 @@ __global__ __launch_bounds__(1024) void k_loss_wide(int n, int c_max, const T* z
     const float at_label = r.classes ? to_float(z[row * z_stride + r.y]) : 0.f;
     here(at_label);                               // before any lane writes a gradient into the logits' place
     float top = -INFINITY, s = 0.f;
-    for (int col = t * V; col < r.classes; col += TEAM * V) {
+    for (uint32_t col = t * V; col < (uint32_t)r.classes; col += TEAM * V) {
       float v[V];
-      load_some(z + row * z_stride + col, r.classes - col, -INFINITY, v);
+      load_some(z + row * z_stride + col, (int)(r.classes - col), -INFINITY, v);
       float m = top;
 #pragma unroll
       for (int i = 0; i < V; ++i) m = fmaxf(m, v[i]);
@@ -144,12 +145,12 @@ __global__ __launch_bounds__(1024) void k_loss_wide(int n, int c_max, const T* z
     if (t == 0) loss[row] = none ? 0.f : r.w * (logf(s) + (from - at_label));
     if (dz) {
       const float by = none ? 0.f : r.w * scale, per = none ? 0.f : by / s;
-      for (int col = t * V; col < c_max; col += TEAM * V) {
+      for (uint32_t col = t * V; col < (uint32_t)c_max; col += TEAM * V) {
         float v[V];
-        load_some(z + row * z_stride + col, r.classes - col, -INFINITY, v);
+        load_some(z + row * z_stride + col, (int)(r.classes - col), -INFINITY, v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = none ? 0.f : exp_of(v[i] - from) * per - (col + i == r.y ? by : 0.f);
-        store_some(dz + row * dz_stride + col, c_max - col, v);
+        for (int i = 0; i < V; ++i) v[i] = none ? 0.f : exp_of(v[i] - from) * per - (col + i == (uint32_t)r.y ? by : 0.f);
+        store_some(dz + row * dz_stride + col, (int)(c_max - col), v);
       }
     }
     __syncthreads();                              // red is free for the next row
