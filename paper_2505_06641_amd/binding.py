@@ -431,8 +431,8 @@ def load_native():
 
 
 class TensorList:
-    """Gradients (and, optionally, where the scaled ones go) as sp_clip_grad_norm takes them: a program whose gradients stay
-    where they are makes the list once.  Holds the tensors."""
+    """Gradients (and, optionally, where the scaled ones go) as sp_clip_grad_norm takes them: a program whose gradients stay the same
+    tensors makes the list once.  Holds the tensors; where their values lie is looked up in every call."""
 
     def __init__(self, grads, out=None):
         self.grads, self.out = list(grads), None if out is None else list(out)

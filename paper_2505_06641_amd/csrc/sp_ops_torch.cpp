@@ -8,6 +8,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <memory>
 #include <new>
 #include <sstream>
 #include <string>
@@ -312,14 +313,39 @@ PyObject* cross_entropy(OpsObject* self, PyObject* const* args, Py_ssize_t nargs
                                           (float*)weight, scale, (float*)po, gt, pd, ds, s));
 }
 
-// Addresses and sizes of a list of tensors, as sp_clip_grad_norm takes them.
+// A list of tensors as sp_clip_grad_norm takes them.  What is kept is the tensors: one that gets other storage (assignment to .data, set_,
+// resize_) is found where it is at the time of the call, and checked anew.
 struct Packed {
-  std::vector<const void*> grads;
+  std::vector<at::Tensor> tensors, outs;        // outs empty: in place
+  std::vector<const void*> grads;               // of the call that is being made
   std::vector<void*> out;
   std::vector<int64_t> sizes;
   bool in_place = true;
   int32_t dtype = SP_F32;
   int device = -1;                              // -1: no tensors
+
+  void collect(Call& c) {
+    grads.clear();
+    out.clear();
+    sizes.clear();
+    device = -1;
+    for (size_t i = 0; i < tensors.size(); ++i) {
+      const at::Tensor &g = tensors[i], &o = in_place ? g : outs[i];
+      if (i == 0) {
+        dtype = c.dtype(&g, "a gradient");
+        device = g.is_cuda() ? g.device().index() : -2;
+      }
+      for (const at::Tensor* t : {&g, &o})
+        if (t->layout() != at::kStrided || !t->is_contiguous() || !t->is_cuda() || t->device().index() != device ||
+            t->scalar_type() != tensors[0].scalar_type())
+          c.refuse("contiguous tensors of one type on one device are asked for");
+      if (!c.bad && g.numel() != o.numel()) c.refuse("a gradient and its output differ in size");
+      if (c.bad) return;
+      grads.push_back(g.data_ptr());
+      out.push_back(o.data_ptr());
+      sizes.push_back(g.numel());
+    }
+  }
 };
 constexpr const char* kPacked = "sneakpeek.packed_tensors";
 
@@ -337,38 +363,19 @@ PyObject* pack_tensors(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     c.refuse("as many outputs as gradients are asked for");
     return nullptr;
   }
-  Packed* p = new (std::nothrow) Packed;
-  if (!p) return PyErr_NoMemory();
-  try {
-    p->in_place = in_place;
-    for (Py_ssize_t i = 0; i < n && !c.bad; ++i) {
-      const at::Tensor* g = c.needed(PyList_GET_ITEM(args[0], i), "a gradient");
-      const at::Tensor* o = in_place ? g : c.needed(PyList_GET_ITEM(args[1], i), "an output");
-      if (c.bad) break;
-      if (i == 0) {
-        p->dtype = c.dtype(g, "a gradient");
-        p->device = g->is_cuda() ? g->device().index() : -2;
-      }
-      for (const at::Tensor* t : {g, o})
-        if (t->layout() != at::kStrided || !t->is_contiguous() || !t->is_cuda() || t->device().index() != p->device ||
-            t->scalar_type() != THPVariable_Unpack(PyList_GET_ITEM(args[0], 0)).scalar_type())
-          c.refuse("contiguous tensors of one type on one device are asked for");
-      if (g->numel() != o->numel()) c.refuse("a gradient and its output differ in size");
-      if (c.bad) break;
-      p->grads.push_back(g->data_ptr());
-      p->out.push_back(o->data_ptr());
-      p->sizes.push_back(g->numel());
-    }
-  } catch (const std::bad_alloc&) {
-    delete p;
-    return PyErr_NoMemory();
+  std::unique_ptr<Packed> p(new Packed);
+  p->in_place = in_place;
+  for (Py_ssize_t i = 0; i < n && !c.bad; ++i) {
+    const at::Tensor* g = c.needed(PyList_GET_ITEM(args[0], i), "a gradient");
+    const at::Tensor* o = in_place ? g : c.needed(PyList_GET_ITEM(args[1], i), "an output");
+    if (c.bad) break;
+    p->tensors.push_back(*g);
+    if (!in_place) p->outs.push_back(*o);
   }
-  if (c.bad) {
-    delete p;
-    return nullptr;
-  }
-  PyObject* capsule = PyCapsule_New(p, kPacked, free_packed);
-  if (!capsule) delete p;
+  if (!c.bad) p->collect(c);
+  if (c.bad) return nullptr;
+  PyObject* capsule = PyCapsule_New(p.get(), kPacked, free_packed);
+  if (capsule) p.release();
   return capsule;
 }
 
@@ -378,9 +385,11 @@ PyObject* clip_packed(OpsObject* self, PyObject* const* args, Py_ssize_t nargs) 
     PyErr_SetString(PyExc_TypeError, "clip_packed(packed, max_norm, norm, stream)");
     return nullptr;
   }
-  const Packed* p = (const Packed*)PyCapsule_GetPointer(args[0], kPacked);
+  Packed* p = (Packed*)PyCapsule_GetPointer(args[0], kPacked);
   if (!p) return nullptr;
-  if (p->device != -1 && p->device != self->device) c.refuse("the tensors are on another device than the operators");
+  p->collect(c);
+  if (!c.bad && p->device != -1 && p->device != self->device) c.refuse("the tensors are on another device than the operators");
+  if (c.bad) return nullptr;
   const float max_norm = (float)c.number(args[1], 0.0);
   void* norm = c.whole(c.bad ? nullptr : c.needed(args[2], "norm"), "norm", at::kFloat, {1});
   void* s = c.stream(args[3]);
@@ -407,6 +416,8 @@ template <auto F, typename S>
 PyObject* guarded(S* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
   try {
     return F(self, args, nargs, kw);
+  } catch (const std::bad_alloc&) {
+    PyErr_NoMemory();
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
   } catch (...) {
@@ -453,7 +464,7 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 PyMethodDef module_methods[] = {
     {"set_error", set_error, METH_O, "set_error(cls): refusals and failures raise cls(status, where, detail)"},
-    {"pack_tensors", positional<pack_tensors, PyObject>(), METH_FASTCALL, "pack_tensors(grads, out or None): their addresses and sizes"},
+    {"pack_tensors", positional<pack_tensors, PyObject>(), METH_FASTCALL, "pack_tensors(grads, out or None): the tensors, as clip_packed takes them"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_ops_native", "Checked calls of the operators that train the heads.", -1, module_methods,
                           nullptr, nullptr, nullptr, nullptr};

@@ -31,3 +31,45 @@ def test_loss_of_the_widest_row_stays_inside_it(gpu, ops):
     step = 1 << 28
     for lo in range(0, INT_MAX - 1, step):
         assert bool((row[0, lo:min(lo + step, INT_MAX - 1)] == first).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [True, False])
+def test_a_list_of_gradients_finds_them_where_they_are(gpu, ops, in_place):
+    """Tensors of a list that get other storage, another size or another type after it was made."""
+    torch, binding = gpu
+    grads = [torch.randn(1000, device=DEV), torch.randn(20, 3, device=DEV), torch.randn(0, device=DEV)]
+    outs = None if in_place else [torch.zeros_like(g) for g in grads]
+    made = binding.TensorList(grads, out=outs)
+    norm = torch.empty(1, device=DEV)
+    held = [t.data for t in grads + (outs or [])]            # the old values' memory lives on, and stays as it is
+    was = [t.clone() for t in held]
+
+    def clipped():
+        want = [g.double() for g in grads]
+        size = math.sqrt(sum(float((g * g).sum()) for g in want))
+        ops.sp_clip_grad_norm(made, 0.5, norm)
+        # the norm is rounded once; factor and product once each
+        assert abs(float(norm) - size) <= 2 * U * size
+        for got, g in zip(outs or grads, want):
+            bound = 4 * U * g.abs() + 1e-40
+            assert_within(torch, got, g * min(1.0, 0.5 / (size + 1e-6)), bound, "clipped")
+
+    for g in grads:
+        g.data = torch.randn_like(g)
+    for o in outs or []:
+        o.data = torch.full_like(o, math.nan)
+    clipped()
+    for old, values in zip(held, was):
+        assert torch.equal(old, values)
+    for t in [grads[0]] + (outs or [])[:1]:                   # longer than what was there
+        t.data = torch.randn(50_000, device=DEV)
+    clipped()
+    good = grads[1].data
+    for other in (good.bfloat16(), good.cpu(), torch.randn(6, 20, device=DEV).t()[:, ::2]) + (() if in_place else (torch.randn(5, device=DEV),)):
+        grads[1].data = other
+        with pytest.raises(binding.SneakPeekError) as e:
+            ops.sp_clip_grad_norm(made, 0.5, norm)
+        assert e.value.status == binding.SP_EINVAL
+    grads[1].data = good
+    clipped()
