@@ -471,7 +471,7 @@ sp_status sp_grouped_linear(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_
                             const int32_t* offsets, const void* w, const float* bias, int32_t activation, int32_t out_dtype,
                             const void* residual, int64_t residual_stride, void* y, int64_t y_stride, void* act_out, int64_t act_stride,
                             void* stream);
-/* With dz_i = dy_i where act_i > 0, else 0 (act NULL: dz = dy):
+/* With dz_i = dy_i where act_i > 0, else 0, also where act_i is NaN (act NULL: dz = dy):
  *   dx_i = dz_i W_g^T      dw_g = sum over the group's rows of x_i^T dz_i      db_g = sum of dz_i
  *   dy [n, m] dtype; act [n, m] dtype or NULL: the layer's y (or act_out, if it has a residual), for SP_ACT_RELU
  *   dx [n, k] dtype or NULL (0 for rows of no group); dw [groups, k, m] float or NULL; db [groups, m] float or NULL (0 for empty

@@ -90,17 +90,17 @@ __device__ __forceinline__ u32x4 load_raw_some(const bf16* p, int count) {
     q = u32x4{q[0] << 16 | h[i], q[1] << 16 | q[0] >> 16, q[2] << 16 | q[1] >> 16, q[3] << 16 | q[2] >> 16};
   return q;
 }
-// dz: dy where act is not <= 0 (as the comparison has it, NaN passes).
+// dz: dy where act > 0, 0 elsewhere (also where act is NaN).
 __device__ __forceinline__ u32x4 masked(const float*, u32x4 dy, u32x4 act) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) dy[i] = __uint_as_float(act[i]) <= 0.f ? 0u : dy[i];
+  for (int i = 0; i < 4; ++i) dy[i] = __uint_as_float(act[i]) > 0.f ? dy[i] : 0u;
   return dy;
 }
 __device__ __forceinline__ u32x4 masked(const bf16*, u32x4 dy, u32x4 act) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = __uint_as_float(act[i] << 16) <= 0.f ? 0u : 0xffffu;
-    const uint32_t hi = __uint_as_float(act[i] & 0xffff0000u) <= 0.f ? 0u : 0xffff0000u;
+    const uint32_t lo = __uint_as_float(act[i] << 16) > 0.f ? 0xffffu : 0u;
+    const uint32_t hi = __uint_as_float(act[i] & 0xffff0000u) > 0.f ? 0xffff0000u : 0u;
     dy[i] &= lo | hi;
   }
   return dy;
@@ -561,7 +561,7 @@ __global__ __launch_bounds__(256) void k_bias_grad(LinearArgs a) {
   if (col < a.m)
     for (int64_t row = lo + slice; row < hi; row += 4) {
       const float g = to_float(((const T*)a.dy)[row * a.dy_stride + col]);
-      s += a.act && to_float(((const T*)a.act)[row * a.act_stride + col]) <= 0.f ? 0.f : g;
+      s += !a.act || to_float(((const T*)a.act)[row * a.act_stride + col]) > 0.f ? g : 0.f;
     }
   sums[slice][lane] = s;
   __syncthreads();

@@ -160,7 +160,7 @@ __device__ __forceinline__ void linear_few_dx(const LinearArgs& a, int block) {
     if (act) {
       pa.load(act + t, has_row ? count : 0);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pr.v[i] = pa.v[i] <= 0.f ? 0.f : pr.v[i];
+      for (int i = 0; i < 8; ++i) pr.v[i] = pa.v[i] > 0.f ? pr.v[i] : 0.f;
     }
     bf16x8 fc[P], fr[P];
     pc.fragment(fc);

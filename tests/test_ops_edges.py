@@ -73,3 +73,35 @@ def test_a_list_of_gradients_finds_them_where_they_are(gpu, ops, in_place):
         assert e.value.status == binding.SP_EINVAL
     grads[1].data = good
     clipped()
+
+
+# rows of the groups, inputs, outputs: dx and dW in one launch, dx of few rows apart from dW, tiles of 128 rows, narrow tiles
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes,k,m", [((40, 60), 24, 20), ((3, 2) * 35, 200, 700), ((4100, 5000), 300, 260), ((9000, 3000), 64, 64)])
+def test_gradients_pass_where_the_activation_is_above_zero(gpu, ops, sizes, k, m, dtype):
+    """NaN, infinities and both zeros among the activations."""
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    n = sum(sizes)
+    x, dy, act = (torch.randn(n, w, device=DEV, generator=g).to(t) for w in (k, m, m))
+    a = len(sizes)
+    w = (torch.randn(a, k, m, device=DEV, generator=g) / math.sqrt(k)).to(t)
+    act[::3, ::2] = math.nan
+    act[1::7, 1] = math.inf
+    act[2::7, 1] = -math.inf
+    act[::5, 3] = 0.0
+    act[1::5, 3] = -0.0
+    dy[act.isnan() & (torch.rand(n, m, device=DEV, generator=g) < 0.5)] = math.nan       # nothing of these is left either
+    dx, dw, db = torch.empty_like(x), torch.empty(a, k, m, device=DEV), torch.empty(a, m, device=DEV)
+    offsets = offsets_of(torch, sizes)
+    ops.sp_grouped_linear_backward(dy, x, offsets, w, act=act, dx=dx, dw=dw, db=db)
+    wx, ww, wb, sx, sw, sb = plain_linear_backward(torch, dy, act, x, sizes, w)
+    bound = (m + 10) * U * sx
+    assert_within(torch, dx, wx, bound + half_step(torch, t) * (wx.abs() + bound), "dx")
+    rows = (max(sizes) + 10) * U
+    assert_within(torch, dw, ww, rows * sw, "dw")
+    assert_within(torch, db, wb, rows * sb, "db")
+    ops.sp_grouped_linear_backward(dy, x, offsets, w, act=act, db=db.fill_(math.nan))
+    assert_within(torch, db, wb, rows * sb, "db alone")
