@@ -485,7 +485,8 @@ sp_status sp_grouped_linear_backward(sp_ops* ops, int32_t n, int32_t k, int32_t 
 /* loss_i = weight_i (log sum_{c < C} exp z_ic - z_i,label), dlogits_ic = scale weight_i (softmax(z_i)_c - [c = label_i]), C the
  * number of classes of the row's application; dlogits are 0 from C on.
  *   logits [n, c_max] dtype, columns from C on are not read      label int32 [n]; -1: loss and gradient 0
- *   app int32 [n] in [0, n_apps) with n_classes int32 [n_apps], or both NULL (C = c_max)      weight [n] float or NULL (1)
+ *   app int32 [n] in [0, n_apps) with n_classes int32 [n_apps], or both NULL (C = c_max; app alone may be for n == 0)
+ *   weight [n] float or NULL (1)
  *   loss [n] float; dlogits [n, c_max] grad_dtype (dtype, or SP_BF16 from SP_F32) or NULL; may be logits if type and stride are
  * A logit of -inf is a class that cannot be; a row that has no other counts as one without a label. */
 sp_status sp_cross_entropy(sp_ops* ops, int32_t n, int32_t c_max, int32_t dtype, const void* logits, int64_t logits_stride, int32_t n_apps,

@@ -183,7 +183,7 @@ sp_status sp_cross_entropy(sp_ops* o, int32_t n, int32_t c_max, int32_t dtype, c
                            float* loss, int32_t grad_dtype, void* dlogits, int64_t dlogits_stride, void* stream) {
   if (!o || n < 0 || c_max < 1 || !dtype_ok(dtype) || logits_stride < c_max || !std::isfinite(scale)) return SP_EINVAL;
   if (dlogits && (!dtype_ok(grad_dtype) || dlogits_stride < c_max || (dtype == SP_BF16 && grad_dtype == SP_F32))) return SP_EINVAL;
-  if ((app != nullptr) != (n_classes != nullptr) || (app && n_apps < 1)) return SP_EINVAL;
+  if (app ? !n_classes || n_apps < 1 : n_classes && n > 0) return SP_EINVAL;       // (an array of no rows may have no address)
   if (n > 0 && (!logits || !label || !loss)) return SP_EINVAL;
   if (!aligned(logits, dtype) || (dlogits && !aligned(dlogits, grad_dtype)) || !aligned4(app) || !aligned4(n_classes) || !aligned4(label) ||
       !aligned4(weight) || !aligned4(loss))

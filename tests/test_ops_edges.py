@@ -5,7 +5,9 @@ import math
 import numpy as np
 import pytest
 
+from paper_2505_06641_amd import binding
 from tests.test_ops import DEV, U, assert_within, dtype_of, gpu, half_step, offsets_of, ops, plain_linear, plain_linear_backward
+from tests.test_ops_refusals import P, handle, lib
 
 INT_MAX = 2 ** 31 - 1
 
@@ -105,3 +107,22 @@ def test_gradients_pass_where_the_activation_is_above_zero(gpu, ops, sizes, k, m
     assert_within(torch, db, wb, rows * sb, "db")
     ops.sp_grouped_linear_backward(dy, x, offsets, w, act=act, db=db.fill_(math.nan))
     assert_within(torch, db, wb, rows * sb, "db alone")
+
+
+@pytest.mark.gpu
+def test_loss_without_rows(gpu, ops):
+    torch, _ = gpu
+    i = lambda n: torch.zeros(n, dtype=torch.int32, device=DEV)
+    z, none = torch.empty(0, 5, device=DEV), torch.empty(0, device=DEV)
+    ops.sp_cross_entropy(z, i(0), none, app=i(0), n_classes=i(3) + 5, weight=none.clone(), dlogits=z.clone())
+    ops.sp_cross_entropy(z, i(0), none)
+
+
+def test_loss_without_rows_takes_an_app_array_without_an_address(lib, handle):
+    base = dict(ops=handle, n=0, c=8, dtype=0, z=None, zs=8, apps=2, app=None, n_classes=P, label=None, weight=None, scale=1.0, loss=None, gt=0,
+                dz=None, dzs=8, stream=None)
+    assert lib.sp_cross_entropy(*base.values()) == binding.SP_OK
+    assert lib.sp_cross_entropy(*dict(base, app=P).values()) == binding.SP_OK
+    assert lib.sp_cross_entropy(*dict(base, app=P, n_classes=None).values()) == binding.SP_EINVAL
+    assert lib.sp_cross_entropy(*dict(base, app=P, apps=0).values()) == binding.SP_EINVAL
+    assert lib.sp_cross_entropy(*dict(base, n=1, z=P, label=P, loss=P, dz=P).values()) == binding.SP_EINVAL
