@@ -126,3 +126,24 @@ def test_loss_without_rows_takes_an_app_array_without_an_address(lib, handle):
     assert lib.sp_cross_entropy(*dict(base, app=P, n_classes=None).values()) == binding.SP_EINVAL
     assert lib.sp_cross_entropy(*dict(base, app=P, apps=0).values()) == binding.SP_EINVAL
     assert lib.sp_cross_entropy(*dict(base, n=1, z=P, label=P, loss=P, dz=P).values()) == binding.SP_EINVAL
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,m", [(262144, 64), (200003, 5), (1025, 70)])
+def test_bias_gradient_alone_of_long_groups(gpu, ops, n, m, dtype):
+    """Equal values, whose roundings in one long sum all go the same way, and random ones."""
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    g = torch.Generator(device=DEV).manual_seed(n + m)
+    x, w = torch.zeros(n, 1, dtype=t, device=DEV), torch.zeros(1, 1, m, dtype=t, device=DEV)
+    offsets = offsets_of(torch, (n,))
+    act = torch.randn(n, m, device=DEV, generator=g).to(t)
+    for dy in (torch.full((n, m), 0.1, dtype=t, device=DEV), torch.randn(n, m, device=DEV, generator=g).to(t)):
+        for mask in (None, act):
+            db = torch.full((1, m), math.nan, device=DEV)
+            ops.sp_grouped_linear_backward(dy, x, offsets, w, act=mask, db=db)
+            dz = dy.double() if mask is None else torch.where(mask > 0, dy.double(), 0.0)
+            # a thread's 256 rows, its n / 1024 parts, four threads
+            bound = (256 + math.ceil(n / 1024) + 4) * U * dz.abs().sum(0)[None]
+            assert_within(torch, db, dz.sum(0)[None], bound, "db")
