@@ -1,6 +1,8 @@
-"""Builds the HIP library for gfx950 with hipcc, and the Python extension that checks the operators' tensors; both in-tree."""
+"""Builds the HIP library for gfx950 with hipcc, and, where torch is installed, the Python extension that checks the operators' tensors;
+both in-tree."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -39,10 +41,17 @@ def native_command(hipcc: str):
 
 def build_library(verbose: bool = True) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    for cmd in ([hipcc] + HIPCC_FLAGS + sources() + ["-o", LIB], native_command(hipcc)):
+
+    def run(cmd):
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
+
+    run([hipcc] + HIPCC_FLAGS + sources() + ["-o", LIB])
+    if importlib.util.find_spec("torch") is not None:
+        run(native_command(hipcc))
+    elif verbose:
+        print("no torch here: the extension of binding.Ops is not built", flush=True)
     return LIB
 
 
