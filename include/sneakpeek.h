@@ -436,6 +436,8 @@ typedef enum { SP_ACT_NONE = 0, SP_ACT_RELU = 1 } sp_activation;
 #define SP_MAX_NORM_DIM 16384             /* columns of a normalised row          */
 #define SP_MAX_LINEAR_DIM 1048576         /* inputs and outputs of a layer        */
 #define SP_MAX_LINEAR_STRIDE 8388608      /* row strides of x, dy and act, in elements */
+/* The layers are computed in tiles of 128 rows by 64 or 128 columns with 256 threads each (dx with an activation: 512), and a launch holds
+ * fewer than 2^32 threads: SP_ECAPACITY beyond that, from about 2^31 rows on (2^30). */
 
 /* workspace_bytes >= SP_OPS_MIN_WORKSPACE: more of it lets long sums (weight gradients of many rows) be split over more of the
  * device; 32 MiB serve every size that was measured (and are quick to come by).  SP_EINVAL: less, or out NULL. */

@@ -147,3 +147,44 @@ def test_bias_gradient_alone_of_long_groups(gpu, ops, n, m, dtype):
             # a thread's 256 rows, its n / 1024 parts, four threads
             bound = (256 + math.ceil(n / 1024) + 4) * U * dz.abs().sum(0)[None]
             assert_within(torch, db, dz.sum(0)[None], bound, "db")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_rows_of_the_most_applications(gpu, ops, dtype):
+    """Five rows of 65535 applications with wide layers: no more workgroups than rows can fill."""
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    apps, k, m = 65535, 1, 4096
+    w = torch.randn(apps, k, m, device=DEV, generator=g).to(t)
+    x = torch.randn(6, k, device=DEV, generator=g).to(t)
+    owner = [0, 3, 3, 40000, 65534]                           # the sixth row is of no application
+    counts = torch.bincount(torch.tensor(owner), minlength=apps)
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), counts.cumsum(0)]).int().to(DEV)
+    y = torch.full((6, m), math.nan, dtype=t, device=DEV)
+    ops.sp_grouped_linear(x, offsets, w, y)
+    want = x[:5].double() * w[owner, 0].double()
+    bound = (k + 10) * U * want.abs()
+    assert_within(torch, y[:5], want, bound + half_step(torch, t) * (want.abs() + bound), "y")
+    assert not y[5].any()
+    dy = torch.randn(6, m, device=DEV, generator=g).to(t)
+    dx = torch.full((6, k), math.nan, dtype=t, device=DEV)
+    ops.sp_grouped_linear_backward(dy, x, offsets, w, dx=dx)
+    terms = dy[:5].double() * w[owner, 0].double()
+    bound = (m + 10) * U * terms.abs().sum(1, keepdim=True)
+    want = terms.sum(1, keepdim=True)
+    assert_within(torch, dx[:5], want, bound + half_step(torch, t) * (want.abs() + bound), "dx")
+    assert not dx[5].any()
+
+
+def test_launches_beyond_32_bits_of_threads_are_refused(lib, handle):
+    """2^24 tiles of 256 threads, 2^23 of 512 (a mask): more than a launch counts."""
+    forward = dict(ops=handle, n=INT_MAX, k=1, m=1, groups=1, dtype=1, x=P, xs=1, offsets=P, w=P, bias=None, act=0, out=1, r=None, rs=1, y=P, ys=1,
+                   act_out=None, acts=1, stream=None)
+    assert lib.sp_grouped_linear(*forward.values()) == binding.SP_ECAPACITY
+    back = dict(ops=handle, n=INT_MAX, k=1, m=1, groups=1, dtype=1, dy=P, dys=1, act=None, acts=1, x=P, xs=1, offsets=P, w=P, dx=P, dxs=1, dw=None,
+                db=None, stream=None)
+    assert lib.sp_grouped_linear_backward(*back.values()) == binding.SP_ECAPACITY
+    masked = dict(back, n=1 << 30, k=65, xs=65, dxs=65, act=P)
+    assert lib.sp_grouped_linear_backward(*masked.values()) == binding.SP_ECAPACITY
