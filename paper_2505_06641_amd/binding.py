@@ -478,8 +478,12 @@ def _ops_class():
                 pass
 
         def sp_ops_check(self, stream=None):
-            """Waits for the stream; raises if a call since the last check met bad offsets, application ids, class counts or labels."""
-            rc = self.lib.sp_ops_check(self.h, _stream_ptr(stream))
+            """Waits for the stream (by default the current one of the ops' device); raises if a call since the last check met bad offsets,
+            application ids, class counts or labels."""
+            if stream is None:
+                import torch
+                stream = torch.cuda.current_stream(self.device)
+            rc = self.lib.sp_ops_check(self.h, stream.cuda_stream)
             if rc != SP_OK:
                 raise SneakPeekError(rc, "sp_ops_check", self.lib.sp_strerror(rc).decode() + " " +
                                      self.lib.sp_ops_last_hip_error(self.h).decode())

@@ -188,3 +188,20 @@ def test_launches_beyond_32_bits_of_threads_are_refused(lib, handle):
     assert lib.sp_grouped_linear_backward(*back.values()) == binding.SP_ECAPACITY
     masked = dict(back, n=1 << 30, k=65, xs=65, dxs=65, act=P)
     assert lib.sp_grouped_linear_backward(*masked.values()) == binding.SP_ECAPACITY
+
+
+def test_the_check_waits_for_the_current_stream_of_the_operators_device(lib, monkeypatch):
+    """As the other calls do; the device of the program may be another one."""
+    import types
+
+    import torch
+    kind = binding._ops_class()
+    o = kind.__new__(kind)
+    o.device, o.h, seen = 1, None, []
+    o.lib = types.SimpleNamespace(sp_ops_check=lambda h, stream: seen.append(stream) or binding.SP_OK)
+    stream_of = {None: 10, 0: 10, 1: 11}
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=stream_of[device]))
+    monkeypatch.setattr(binding, "_current_stream", lambda: 10)
+    o.sp_ops_check()
+    o.sp_ops_check(stream=types.SimpleNamespace(cuda_stream=12))
+    assert seen == [11, 12]
