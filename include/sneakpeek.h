@@ -466,8 +466,9 @@ sp_status sp_layer_norm_backward(sp_ops* ops, int32_t n, int32_t d, int32_t dtyp
  *   y [n, m] out_dtype (dtype, or SP_F32 from SP_BF16); residual [n, m] out_dtype or NULL (may be y)
  *   act_out [n, m] out_dtype or NULL: act(x_i W_g + b_g) without the residual, which the backward pass of a layer with both an
  *     activation and a residual asks for
- * bfloat16 products are exact, sums are float32.  Float32 factors are taken by the matrix cores as three bfloat16 numbers each, with the
- * six products that count: within 2^-24 of the sum of the products' magnitudes.  An infinite float32 factor makes the results that it
+ * bfloat16 products are exact, sums are float32.  A float32 factor is taken by the matrix cores as three bfloat16 numbers (exactly from
+ * magnitudes of 2^-110 on, to within 2^-134 below), and of the nine products of two factors the three smallest are left out: at most
+ * 2^-24 (1 + 2^-10) of the factors' product.  That holds for the gradients too.  An infinite float32 factor makes the results that it
  * enters NaN, NaN stays NaN; neither reaches another row's, group's or column's results.  */
 sp_status sp_grouped_linear(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype, const void* x, int64_t x_stride,
                             const int32_t* offsets, const void* w, const float* bias, int32_t activation, int32_t out_dtype,

@@ -12,9 +12,11 @@
 // A side whose depth is the contiguous one in memory lies in LDS as it came and is read 8 elements of the depth at a time; one
 // whose depth is strided is read by the LDS's transposing loads.
 //
-// Float32: a value is the sum of three bfloat16 numbers, each the rounded rest of the ones before it (8 + 8 + 8 significant bits: what
-// is left is below 2^-27 of the value).  Of the nine products of two such sums the six largest are taken, each exact in the float32
-// sum; the three others are below 2^-25 of the product together.  Six instructions of the bfloat16 rate are 2.6 times the float32
+// Float32: a value is the sum of three bfloat16 numbers, each the rounded rest of the ones before it.  bfloat16 has 8 significant bits, so the
+// second number is at most 2^-8 of the value and the third 2^-17, which leaves nothing over: 8 + 8 + 8 bits are float32's 24.  Where
+// the last of them would be below bfloat16's smallest subnormal, 2^-133 (values below 2^-110), up to 2^-134 is left over; the matrix cores
+// take subnormals as they are.  Of the nine products of two such sums the six largest are taken, each exact in the float32 sum; the
+// three others are at most 2 x 2^-25 + 2^-34 of the product together.  Six instructions of the bfloat16 rate are 2.6 times the float32
 // instruction's rate.  An infinite factor (or one that rounds to one in bfloat16, from 3.39e38 on) makes its results NaN: its rest is
 // one.
 #pragma once

@@ -205,3 +205,58 @@ def test_the_check_waits_for_the_current_stream_of_the_operators_device(lib, mon
     o.sp_ops_check()
     o.sp_ops_check(stream=types.SimpleNamespace(cuda_stream=12))
     assert seen == [11, 12]
+
+
+# y and dx of few rows, and in tiles
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,k,m", [(40, 32, 48), (6000, 300, 600)])
+@pytest.mark.parametrize("power", [-60, -100, -110, -114, -118, -122, -126, -130])
+def test_small_float32_factors(gpu, ops, n, k, m, power):
+    """Factors of 2^power, which a third bfloat16 number cannot finish below 2^-110, against ordinary ones."""
+    torch, _ = gpu
+    g = torch.Generator(device=DEV).manual_seed(-power)
+    small = lambda *s: torch.randn(*s, device=DEV, generator=g) * 2.0 ** power
+    offsets = offsets_of(torch, (n,))
+    x, w = small(n, k), torch.randn(1, k, m, device=DEV, generator=g)
+
+    def bound(terms, left, right):
+        """left @ right: the float32 sum and what the split leaves out, what is left over of either factor, products below 2^-149."""
+        a, b = left.double().abs(), right.double().abs()
+        over = 2.0 ** -134 * (a.sum(1)[:, None] + b.sum(0)[None])
+        return (terms + 10) * U * (a @ b) + over + 6 * terms * 2.0 ** -149
+
+    y = torch.full((n, m), math.nan, device=DEV)
+    ops.sp_grouped_linear(x, offsets, w, y)
+    assert_within(torch, y, x.double() @ w[0].double(), bound(k, x, w[0]), "y")
+    dy, r = small(n, m), torch.randn(n, k, device=DEV, generator=g)
+    dx, dw, db = torch.full((n, k), math.nan, device=DEV), torch.full((1, k, m), math.nan, device=DEV), torch.full((1, m), math.nan, device=DEV)
+    ops.sp_grouped_linear_backward(dy, r, offsets, w, dx=dx, dw=dw, db=db)
+    wt, rt = w[0].t().contiguous(), r.t().contiguous()
+    assert_within(torch, dx, dy.double() @ wt.double(), bound(m, dy, wt), "dx")
+    assert_within(torch, dw[0], rt.double() @ dy.double(), bound(n, rt, dy), "dw")
+    assert_within(torch, db[0], dy.double().sum(0), (n + 8) * U * dy.double().abs().sum(0) + n * 2.0 ** -149, "db")
+
+
+def test_the_split_of_float32_on_the_host():
+    """Three bfloat16 numbers, each the rounded rest, are the value from 2^-110 on; what the three smallest products come to."""
+    import torch
+    g = torch.Generator().manual_seed(0)
+    v = torch.randn(1 << 16, generator=g) * torch.exp2(torch.randint(-100, 100, (1 << 16,), generator=g).float())
+    v = torch.cat([v, torch.tensor([1.0038986, 1 + 2.0 ** -8, 1 + 2.0 ** -8 - 2.0 ** -23, 2 - 2.0 ** -23, 2.0 ** -110])])
+
+    def split(q):
+        parts = []
+        for _ in range(3):
+            parts.append(q.bfloat16().float())
+            q = q - parts[-1]
+        return parts, q
+
+    (a, b, c), rest = split(v)
+    assert not rest.any()
+    assert bool((b.abs() <= 2.0 ** -8 * v.abs()).all()) and bool((c.abs() <= 2.0 ** -17 * v.abs()).all())
+    u = v.roll(7)
+    (_, d, e), _ = split(u)
+    left_out = (b.double() * e.double()).abs() + (c.double() * d.double()).abs() + (c.double() * e.double()).abs()
+    assert bool((left_out <= 2.0 ** -24 * (1 + 2.0 ** -10) * (v.double() * u.double()).abs()).all())
+    tiny = v.sign() * torch.rand(v.shape, generator=g) * 2.0 ** -110
+    assert bool((split(tiny)[1].abs() <= 2.0 ** -134).all())
