@@ -422,8 +422,8 @@ sp_status sp_debug_copy_rate(int device_id, int64_t bytes, void* stream, double*
  * An sp_ops holds what the calls need besides the caller's arrays: a workspace of device memory and a word in which kernels
  * note bad data.  Calls are enqueued on `stream` and return without waiting, allocate nothing, record no memory operation
  * other than kernels (they may be captured into a graph), and keep nothing of one call for the next.  Calls that share an
- * sp_ops must not overlap on the device: one stream at a time, as for a context.  Results depend on the inputs alone, bit for
- * bit, not on timing.  All arrays are DEVICE arrays unless said otherwise; elements lie at multiples of their own size (4 or 2
+ * sp_ops must not overlap on the device: one stream at a time, as for a context.  The same call (inputs, sizes and strides, which
+ * outputs are asked for) with the same workspace size has the same results, bit for bit, whatever the timing.  All arrays are DEVICE arrays unless said otherwise; elements lie at multiples of their own size (4 or 2
  * bytes), rows of a matrix are contiguous and `*_stride` elements apart (at least the row's length).  Outputs must not overlap
  * inputs or each other unless said otherwise.  Types are sp_dtype; sums, statistics, losses, biases and weight gradients are
  * float32 or wider; an output of fewer bits is rounded once, to the nearest.
@@ -440,7 +440,9 @@ typedef enum { SP_ACT_NONE = 0, SP_ACT_RELU = 1 } sp_activation;
  * fewer than 2^32 threads: SP_ECAPACITY beyond that, from about 2^31 rows on (2^30). */
 
 /* workspace_bytes >= SP_OPS_MIN_WORKSPACE: more of it lets long sums (weight gradients of many rows) be split over more of the
- * device; 32 MiB serve every size that was measured (and are quick to come by).  SP_EINVAL: less, or out NULL. */
+ * device.  A part of a layer's dW takes k m + m floats, and one is set aside for every group: 32 MiB, the Python form's default, hold
+ * 63 parts of 512 -> 256 and 14 of 768 -> 768.  With none to spare every group's rows are one sum, and long groups wait for it.
+ * SP_EINVAL: less, or out NULL. */
 sp_status sp_ops_create(int device_id, int64_t workspace_bytes, sp_ops** out);
 void sp_ops_destroy(sp_ops* ops);
 /* Waits for the stream.  SP_EINVAL if a call on these ops since the last check (or since sp_ops_create) met bad data:
@@ -479,7 +481,8 @@ sp_status sp_grouped_linear(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_
  *   dy [n, m] dtype; act [n, m] dtype or NULL: the layer's y (or act_out, if it has a residual), for SP_ACT_RELU
  *   dx [n, k] dtype or NULL (0 for rows of no group); dw [groups, k, m] float or NULL; db [groups, m] float or NULL (0 for empty
  *     groups).  x is read for dw only, w for dx only (either may be NULL otherwise).  The residual's gradient is dy itself.  dw and
- *     db are sums over the rows in float32; long groups are summed in parts that are then added in their order. */
+ *     db are sums over the rows in float32; long groups are summed in parts, dw and db with it as far as the workspace has room for
+ *     them, that are then added in their order (db alone has parts of its own, and with them its own last bits). */
 sp_status sp_grouped_linear_backward(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_t groups, int32_t dtype, const void* dy,
                                      int64_t dy_stride, const void* act, int64_t act_stride, const void* x, int64_t x_stride,
                                      const int32_t* offsets, const void* w, void* dx, int64_t dx_stride, float* dw, float* db,
