@@ -361,7 +361,8 @@ def _plain(s):
         return (y if s["r"] is None else y + s["r"].float()).to(s["y"].dtype)
     x = s["x"].float()
     top_x = x.abs().amax(1, keepdim=True)
-    q, scale = torch.round(x * (127.0 / top_x)), top_x / 127.0
+    most = torch.full_like(top_x, 127.0)                          # (one rounding: a number over a tensor is a product with its inverse)
+    q, scale = torch.round(x * (most / top_x)), top_x / most
     y = torch.empty_like(s["y"])
     for a in range(experts):
         lo, hi = s["ends"][a], s["ends"][a + 1]
@@ -485,7 +486,8 @@ def exact(case, seed):
     out = torch.empty(n, case["m"], dtype=f64, device=DEV)
     x = s["x"].float()
     high = x.abs().amax(1, keepdim=True)
-    q, scale = torch.round(x * (127.0 / high)).to(f64), (high / 127.0).to(f64)   # what the rows stand for is the operator's definition
+    by = torch.div(torch.full_like(high, 127.0), high)
+    q, scale = torch.round(x * by).to(f64), high.to(f64) / 127.0      # what the rows stand for is the operator's definition
     w = s["w"].to(f64) * s["w_scale"].to(f64)[:, :, None]
     for a, (lo, hi) in enumerate(zip(s["ends"], s["ends"][1:])):
         z = torch.addmm(s["b"][a].to(f64), q[lo:hi] * scale[lo:hi], w[a].t())
