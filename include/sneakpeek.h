@@ -446,8 +446,8 @@ typedef enum { SP_ACT_NONE = 0, SP_ACT_RELU = 1 } sp_activation;
 sp_status sp_ops_create(int device_id, int64_t workspace_bytes, sp_ops** out);
 void sp_ops_destroy(sp_ops* ops);
 /* Waits for the stream.  SP_EINVAL if a call on these ops since the last check (or since sp_ops_create) met bad data:
- * offsets that do not rise from 0 to at most n, an application id, class count or label out of range.  Such data is never
- * followed out of the arrays; results of the rows concerned are unspecified (sp_cross_entropy: 0). */
+ * offsets that do not rise from 0 to at most n, an application id, class count, label, expert or place out of range, a router's logit
+ * of NaN or +inf.  Such data is never followed out of the arrays; results of the rows concerned are unspecified (sp_cross_entropy: 0). */
 sp_status sp_ops_check(sp_ops* ops, void* stream);
 const char* sp_ops_last_hip_error(const sp_ops* ops);
 
@@ -505,6 +505,79 @@ sp_status sp_cross_entropy(sp_ops* ops, int32_t n, int32_t c_max, int32_t dtype,
  *   overlap. */
 sp_status sp_clip_grad_norm(sp_ops* ops, int32_t n_tensors, int32_t dtype, const void* const* grads, const int64_t* sizes, float max_norm,
                             void* const* out, float* norm_out, void* stream);
+
+/*
+ * Operators for heads that are made of experts.
+ *
+ * Such a head has many small networks, the experts, of which a row goes through a few: a router, a linear layer with one output for every
+ * expert, says which and with what weights.  A layer of experts is sp_route, sp_route_order, sp_dispatch, the grouped linear layers above with the
+ * experts as groups, and sp_combine; its gradients are sp_combine_backward, sp_grouped_linear_backward, sp_combine without weights (the
+ * gradient of sp_dispatch) and sp_route_backward.  sp_dropout goes between layers that train; sp_quantize_rows and sp_grouped_linear_quantized
+ * serve with weights of 8 bits.  All are calls on an sp_ops, with what is said of those above.
+ */
+typedef enum { SP_SCORE_SOFTMAX = 0, SP_SCORE_SIGMOID = 1 } sp_score_kind;
+#define SP_MAX_EXPERTS 1024
+#define SP_MAX_TOP 32                     /* experts of a row                    */
+#define SP_MAX_EXPERT_GROUPS 64
+#define SP_MAX_QUANTIZED_INPUTS 131071    /* whose sum 32-bit integers hold      */
+
+/* Each row's `top` experts and their weights.  s = softmax or sigmoid of the row's logits; c = s + bias.  The experts lie in `groups` groups
+ * of experts / groups each, one after the other; a group's value is the sum of its two largest c (its only one, where it has one), and the
+ * top_groups groups of the largest values stay in.  Of their experts the `top` of the largest c are chosen, in that order; ties go to the lowest
+ * number, of groups and experts.  c are compared in 64 bits; without a bias and groups the logits themselves are compared.
+ *   weight_j = scale s_j, or scale s_j / (sum of the chosen s) with renormalize
+ *   logits [n, experts] dtype      bias [experts] float or NULL (it has no gradient: who balances sets it)
+ *   expert int32 [n, top], weight float [n, top], contiguous; top_groups * (experts / groups) >= top
+ * A logit of -inf is an expert that is not there.  Where fewer than `top` can be chosen the rest is -1 with weight 0: a row of -inf has no
+ * expert.  A logit of NaN or +inf is bad data (sp_ops_check), and its row gets no expert. */
+sp_status sp_route(sp_ops* ops, int32_t n, int32_t experts, int32_t top, int32_t dtype, const void* logits, int64_t logits_stride, int32_t score,
+                   const float* bias, int32_t groups, int32_t top_groups, int32_t renormalize, float scale, int32_t* expert, float* weight,
+                   void* stream);
+/* The gradient of the logits from that of the weights, with the experts chosen as they are; 0 for rows without one.  dlogits [n, experts] dtype
+ * (may be logits).  An expert that a row names twice counts twice; a number below -1 or from `experts` on is bad data and counts as -1. */
+sp_status sp_route_backward(sp_ops* ops, int32_t n, int32_t experts, int32_t top, int32_t dtype, const void* logits, int64_t logits_stride,
+                            int32_t score, int32_t renormalize, float scale, const int32_t* expert, const float* dweight, void* dlogits,
+                            int64_t dlogits_stride, void* stream);
+/* The (row, expert) pairs in the order of their experts, pairs of one expert in their own order: offsets int32 [experts + 1] as the grouped linear
+ * layers take them, place int32 [n, top]: where each pair's row lies among the sorted ones, -1 for pairs without an expert.  A number below -1 or
+ * from `experts` on is bad data and counts as -1.  n * top < 2^31. */
+sp_status sp_route_order(sp_ops* ops, int32_t n, int32_t top, int32_t experts, const int32_t* expert, int32_t* offsets, int32_t* place,
+                         void* stream);
+/* xs[place_ij] = x_i.  x [n, d] dtype, place int32 [n, top] of different rows of xs, or -1; xs [rows, d] dtype.  Rows that no place names stay as
+ * they are.  A place below -1 or from `rows` on is bad data and counts as -1, here and below. */
+sp_status sp_dispatch(sp_ops* ops, int32_t n, int32_t d, int32_t top, int32_t dtype, const void* x, int64_t x_stride, const int32_t* place,
+                      int32_t rows, void* xs, int64_t xs_stride, void* stream);
+/* y_i = sum over j of weight_ij ys[place_ij] + residual_i; places of -1 count nothing.  weight float [n, top] or NULL (1: the gradient of
+ * sp_dispatch's x); ys [rows, d], y, residual [n, d] dtype, residual or NULL (may be y). */
+sp_status sp_combine(sp_ops* ops, int32_t n, int32_t d, int32_t top, int32_t dtype, int32_t rows, const void* ys, int64_t ys_stride,
+                     const int32_t* place, const float* weight, const void* residual, int64_t residual_stride, void* y, int64_t y_stride,
+                     void* stream);
+/* dys[place_ij] = weight_ij dy_i and dweight_ij = the product of dy_i and ys[place_ij], 0 for places of -1.  dys [rows, d] dtype or NULL (may be
+ * ys); rows that no place names stay as they are; dweight float [n, top] or NULL (ys is read for it only).  The residual's gradient is dy. */
+sp_status sp_combine_backward(sp_ops* ops, int32_t n, int32_t d, int32_t top, int32_t dtype, const void* dy, int64_t dy_stride, int32_t rows,
+                              const void* ys, int64_t ys_stride, const int32_t* place, const float* weight, void* dys, int64_t dys_stride,
+                              float* dweight, void* stream);
+
+/* y = x / (1 - p) + residual where a random number says so, with probability 1 - p, else residual.  p is taken to the nearest multiple of 2^-16 (but
+ * 0 and 1 for themselves only), in the scale as well.  The numbers are Philox 4x32-10's for the seed, the offset, the row and the column, and for
+ * nothing else: the same call on dy with the same p, seed and offset is the gradient of x.  step int64 [1] or NULL is added to the offset: a
+ * DEVICE array, for calls in a captured graph whose masks are to change from replay to replay.  Every call that is to have its own
+ * numbers takes its own seed or offset.  x, y [n, d] dtype (y may be x); residual [n, d] dtype or NULL (may be y). */
+sp_status sp_dropout(sp_ops* ops, int32_t n, int32_t d, int32_t dtype, const void* x, int64_t x_stride, float p, uint64_t seed, uint64_t offset,
+                     const int64_t* step, const void* residual, int64_t residual_stride, void* y, int64_t y_stride, void* stream);
+
+/* Rows as whole numbers of 8 bits with a scale each: scale_i = max_c |x_ic| / 127 and q_ic = x_ic (127 / max_c |x_ic|) rounded to the nearest, ties
+ * to even; all of it in float32.  A row of zeros has scale 0, one with an infinity or NaN zeros and scale NaN.  x [n, d] dtype, q int8 [n, d],
+ * scale [n] float.  A layer's weights are rounded by the same call, once: rows of w^T, one for every output. */
+sp_status sp_quantize_rows(sp_ops* ops, int32_t n, int32_t d, int32_t dtype, const void* x, int64_t x_stride, int8_t* q, int64_t q_stride,
+                           float* scale, void* stream);
+/* y_i = act(x_scale_i w_scale_go sum_c x_ic w_goc + bias_go) + residual_i for every row i of every group g: sp_grouped_linear with whole numbers
+ * and scales.  x int8 [n, k]; w int8 [groups, m, k], contiguous, an output's inputs next to each other; w_scale float [groups, m]; bias float
+ * [groups, m] or NULL; y, residual [n, m] out_dtype, residual or NULL (may be y); offsets as there.  The sum is exact. */
+sp_status sp_grouped_linear_quantized(sp_ops* ops, int32_t n, int32_t k, int32_t m, int32_t groups, const int8_t* x, int64_t x_stride,
+                                      const float* x_scale, const int32_t* offsets, const int8_t* w, const float* w_scale, const float* bias,
+                                      int32_t activation, int32_t out_dtype, const void* residual, int64_t residual_stride, void* y,
+                                      int64_t y_stride, void* stream);
 
 #ifdef __cplusplus
 }

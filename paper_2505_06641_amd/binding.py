@@ -25,7 +25,9 @@ EXPORTS = ["sp_create", "sp_destroy", "sp_score", "sp_greedy_round", "sp_greedy_
            "sp_rounds_in_one_launch", "sp_rounds_in_one_workgroup", "sp_debug_mfma_rate", "sp_debug_copy_rate", "sp_debug_set_generation", "sp_debug_set_spin_limit", "sp_debug_set_sort_spin_limit", "sp_set_prior", "sp_set_swap_cost", "sp_set_policy",
            "sp_set_timing", "sp_get_timing", "sp_get_round_times",
            "sp_ops_create", "sp_ops_destroy", "sp_ops_check", "sp_ops_last_hip_error", "sp_layer_norm", "sp_layer_norm_backward",
-           "sp_grouped_linear", "sp_grouped_linear_backward", "sp_cross_entropy", "sp_clip_grad_norm"]
+           "sp_grouped_linear", "sp_grouped_linear_backward", "sp_cross_entropy", "sp_clip_grad_norm",
+           "sp_route", "sp_route_backward", "sp_route_order", "sp_dispatch", "sp_combine", "sp_combine_backward", "sp_dropout",
+           "sp_quantize_rows", "sp_grouped_linear_quantized"]
 
 
 class sp_policy(C.Structure):
@@ -173,6 +175,19 @@ def load_library(path: Optional[str] = None):
     lib.sp_cross_entropy.restype = C.c_int
     lib.sp_clip_grad_norm.argtypes = [vp, i32, i32, vp, vp, f32, vp, vp, vp]
     lib.sp_clip_grad_norm.restype = C.c_int
+    u64 = C.c_uint64
+    lib.sp_route.argtypes = [vp, i32, i32, i32, i32, vp, i64, i32, vp, i32, i32, i32, f32, vp, vp, vp]
+    lib.sp_route_backward.argtypes = [vp, i32, i32, i32, i32, vp, i64, i32, i32, f32, vp, vp, vp, i64, vp]
+    lib.sp_route_order.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.sp_dispatch.argtypes = [vp, i32, i32, i32, i32, vp, i64, vp, i32, vp, i64, vp]
+    lib.sp_combine.argtypes = [vp, i32, i32, i32, i32, i32, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+    lib.sp_combine_backward.argtypes = [vp, i32, i32, i32, i32, vp, i64, i32, vp, i64, vp, vp, vp, i64, vp, vp]
+    lib.sp_dropout.argtypes = [vp, i32, i32, i32, vp, i64, f32, u64, u64, vp, vp, i64, vp, i64, vp]
+    lib.sp_quantize_rows.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, vp, vp]
+    lib.sp_grouped_linear_quantized.argtypes = [vp, i32, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, i32, i32, vp, i64, vp, i64, vp]
+    for name in ("sp_route", "sp_route_backward", "sp_route_order", "sp_dispatch", "sp_combine", "sp_combine_backward", "sp_dropout",
+                 "sp_quantize_rows", "sp_grouped_linear_quantized"):
+        getattr(lib, name).restype = C.c_int
     if path is None:
         _lib = lib
     return lib
@@ -440,7 +455,7 @@ class TensorList:
 
 
 def Ops(device: int = 0, workspace_bytes: int = 32 << 20):
-    """One sp_ops: the operators that train the heads.  Its methods carry the names of the C entry points; tensors live on the
+    """One sp_ops: the operators that train the heads, and those for heads that are made of experts.  Its methods carry the names of the C entry points; tensors live on the
     ops' device, matrices have contiguous rows.  What does not fit together raises before anything is launched."""
     return _ops_class()(device, workspace_bytes)
 
@@ -479,7 +494,7 @@ def _ops_class():
 
         def sp_ops_check(self, stream=None):
             """Waits for the stream (by default the current one of the ops' device); raises if a call since the last check met bad offsets,
-            application ids, class counts or labels."""
+            application ids, class counts, labels, router's logits, experts or places."""
             if stream is None:
                 import torch
                 stream = torch.cuda.current_stream(self.device)

@@ -23,7 +23,7 @@ HIPCC_FLAGS = [
 
 
 def sources():
-    return [os.path.join(CSRC, "sp_api.hip"), os.path.join(CSRC, "sp_ops.hip")]
+    return [os.path.join(CSRC, "sp_api.hip"), os.path.join(CSRC, "sp_ops.hip"), os.path.join(CSRC, "sp_ops_experts.hip")]
 
 
 def native_command(hipcc: str):

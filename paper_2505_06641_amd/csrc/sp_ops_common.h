@@ -15,6 +15,9 @@ constexpr uint32_t kErrOffsets = 1u;
 constexpr uint32_t kErrLabel = 2u;
 constexpr uint32_t kErrClassCount = 4u;
 constexpr uint32_t kErrAppId = 8u;
+constexpr uint32_t kErrRouterLogit = 16u;   // a router's logit that is NaN or +inf
+constexpr uint32_t kErrExpert = 32u;
+constexpr uint32_t kErrPlace = 64u;
 
 // Elements of a 16-byte piece.
 template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);

@@ -1,0 +1,271 @@
+// C entry points of the operators for heads that are made of experts: argument checks, workspace, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+
+#include "sneakpeek.h"
+#include "sp_host.h"
+#include "sp_ops_common.h"
+#include "sp_ops_dropout.h"
+#include "sp_ops_host.h"
+#include "sp_ops_move.h"
+#include "sp_ops_quantized.h"
+#include "sp_ops_route.h"
+
+using namespace sp;
+
+static_assert(kMaxExperts == SP_MAX_EXPERTS, "a launch's counters hold all experts");
+
+namespace {
+
+bool score_ok(int32_t s) { return s == SP_SCORE_SOFTMAX || s == SP_SCORE_SIGMOID; }
+
+int power_from(int v) {                // the power of two from v on
+  int p = 1;
+  while (p < v) p *= 2;
+  return p;
+}
+
+// Calls f<T>() with the element type.
+template <typename F>
+void with_type(int32_t dtype, F&& f) {
+  if (dtype == SP_F32) f.template operator()<float>();
+  else f.template operator()<bf16>();
+}
+
+}  // namespace
+
+extern "C" {
+
+sp_status sp_route(sp_ops* o, int32_t n, int32_t experts, int32_t top, int32_t dtype, const void* logits, int64_t logits_stride, int32_t score,
+                   const float* bias, int32_t groups, int32_t top_groups, int32_t renormalize, float scale, int32_t* expert, float* weight,
+                   void* stream) {
+  if (!o || n < 0 || experts < 1 || top < 1 || top > experts || !dtype_ok(dtype) || logits_stride < experts || !score_ok(score)) return SP_EINVAL;
+  if (groups < 1 || experts % groups != 0 || top_groups < 1 || top_groups > groups || (int64_t)top_groups * (experts / groups) < top) return SP_EINVAL;
+  if (!std::isfinite(scale) || (n > 0 && (!logits || !expert || !weight))) return SP_EINVAL;
+  if (!aligned(logits, dtype) || !aligned4(bias) || !aligned4(expert) || !aligned4(weight)) return SP_EINVAL;
+  if (experts > SP_MAX_EXPERTS || top > SP_MAX_TOP || groups > SP_MAX_EXPERT_GROUPS) return SP_ECAPACITY;
+  if (n == 0) return SP_OK;
+  RouteArgs a{};
+  a.n = n; a.experts = experts; a.top = top; a.groups = groups; a.top_groups = top_groups; a.width = experts / groups;
+  a.group_lanes = 64 / power_from(groups);
+  a.sigmoid = score == SP_SCORE_SIGMOID; a.renormalize = renormalize != 0; a.scale = scale;
+  a.z = logits; a.z_stride = logits_stride; a.bias = bias; a.expert = expert; a.weight = weight; a.err = o->err;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  const int per = (a.width + a.group_lanes - 1) / a.group_lanes;
+  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)n + 3) / 4, 16384));
+  with_type(dtype, [&]<typename T>() {
+    auto kernel = per <= 1 ? k_route<T, 1> : per <= 2 ? k_route<T, 2> : per <= 4 ? k_route<T, 4> : per <= 8 ? k_route<T, 8> : per <= 16 ? k_route<T, 16> : k_route<T, 32>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
+  });
+  return launched(o);
+}
+
+sp_status sp_route_backward(sp_ops* o, int32_t n, int32_t experts, int32_t top, int32_t dtype, const void* logits, int64_t logits_stride,
+                            int32_t score, int32_t renormalize, float scale, const int32_t* expert, const float* dweight, void* dlogits,
+                            int64_t dlogits_stride, void* stream) {
+  if (!o || n < 0 || experts < 1 || top < 1 || top > experts || !dtype_ok(dtype) || logits_stride < experts || dlogits_stride < experts ||
+      !score_ok(score))
+    return SP_EINVAL;
+  if (!std::isfinite(scale) || (n > 0 && (!logits || !expert || !dweight || !dlogits))) return SP_EINVAL;
+  if (!aligned(logits, dtype) || !aligned(dlogits, dtype) || !aligned4(expert) || !aligned4(dweight)) return SP_EINVAL;
+  if (experts > SP_MAX_EXPERTS || top > SP_MAX_TOP) return SP_ECAPACITY;
+  if (n == 0) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  with_type(dtype, [&]<typename T>() {
+    auto run = [&]<int TEAM, int C>() {
+      constexpr int rows = 256 / TEAM;
+      const dim3 grid((unsigned)std::min<int64_t>(((int64_t)n + rows - 1) / rows, 8192));
+      hipLaunchKernelGGL((k_route_back<T, TEAM, C>), grid, dim3(256), 0, (hipStream_t)stream, n, experts, top, (const T*)logits, logits_stride,
+                         score == SP_SCORE_SIGMOID, renormalize != 0, scale, expert, dweight, (T*)dlogits, dlogits_stride, o->err);
+    };
+    const int lanes = std::max((experts + kPiece<T> - 1) / kPiece<T>, top);        // (a lane for every chosen expert)
+    if (lanes <= 8) run.template operator()<8, 1>();
+    else if (lanes <= 16) run.template operator()<16, 1>();
+    else if (lanes <= 32) run.template operator()<32, 1>();
+    else if (lanes <= 64) run.template operator()<64, 1>();
+    else if (lanes <= 128) run.template operator()<64, 2>();
+    else run.template operator()<64, 4>();
+  });
+  return launched(o);
+}
+
+sp_status sp_route_order(sp_ops* o, int32_t n, int32_t top, int32_t experts, const int32_t* expert, int32_t* offsets, int32_t* place, void* stream) {
+  if (!o || n < 0 || top < 1 || experts < 1 || !offsets || (n > 0 && (!expert || !place))) return SP_EINVAL;
+  if (!aligned4(expert) || !aligned4(offsets) || !aligned4(place)) return SP_EINVAL;
+  const int64_t pairs = (int64_t)n * top;
+  if (experts > SP_MAX_EXPERTS || top > SP_MAX_TOP || pairs > INT32_MAX) return SP_ECAPACITY;
+  int bits = 0;
+  while ((1 << bits) < experts) ++bits;
+  constexpr int64_t kOne = 16384, kMost = 128;               // pairs of a single tile; tiles
+  const int64_t tile = pairs <= kOne ? kOne : std::max(kOne, ((pairs + kMost - 1) / kMost + 1023) / 1024 * 1024);
+  const int tiles = (int)std::max<int64_t>(1, (pairs + tile - 1) / tile);
+  if (tiles > 1 && (int64_t)tiles * experts * 4 > o->ws_bytes) return SP_ECAPACITY;
+  int32_t* counts = tiles > 1 ? (int32_t*)o->ws : nullptr;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  hipStream_t s = (hipStream_t)stream;
+  if (tiles > 1)
+    hipLaunchKernelGGL(k_order_count, dim3(tiles), dim3(kOrderThreads), 0, s, pairs, (int)tile, experts, expert, counts, o->err);
+  hipLaunchKernelGGL(k_order_place, dim3(tiles), dim3(kOrderThreads), 0, s, pairs, (int)tile, tiles, experts, bits, expert, counts, offsets, place,
+                     o->err);
+  return launched(o);
+}
+
+}  // extern "C"
+
+namespace {
+
+sp_status move_sizes(const sp_ops* o, int32_t n, int32_t d, int32_t top, int32_t dtype, int32_t rows, const int32_t* place) {
+  if (!o || n < 0 || d < 1 || top < 1 || !dtype_ok(dtype) || rows < 0 || (n > 0 && !place) || !aligned4(place)) return SP_EINVAL;
+  if (top > SP_MAX_TOP || d > SP_MAX_LINEAR_DIM) return SP_ECAPACITY;
+  return SP_OK;
+}
+
+// Calls f<T, TEAM>(workgroups): the smallest team that holds a row of up to 64 pieces, a wavefront for longer ones.
+template <typename F>
+void with_rows(int32_t n, int32_t d, int32_t dtype, F&& f) {
+  with_type(dtype, [&]<typename T>() {
+    const int pieces = (d + kPiece<T> - 1) / kPiece<T>;
+    auto run = [&]<int TEAM>() {
+      constexpr int rows = 256 / TEAM;
+      f.template operator()<T, TEAM>(dim3((unsigned)std::min<int64_t>(((int64_t)n + rows - 1) / rows, kMoveBlocks)));
+    };
+    if (pieces <= 4) run.template operator()<4>();
+    else if (pieces <= 8) run.template operator()<8>();
+    else if (pieces <= 16) run.template operator()<16>();
+    else if (pieces <= 32) run.template operator()<32>();
+    else run.template operator()<64>();
+  });
+}
+
+}  // namespace
+
+extern "C" {
+
+sp_status sp_dispatch(sp_ops* o, int32_t n, int32_t d, int32_t top, int32_t dtype, const void* x, int64_t x_stride, const int32_t* place,
+                      int32_t rows, void* xs, int64_t xs_stride, void* stream) {
+  const sp_status bad = move_sizes(o, n, d, top, dtype, rows, place);
+  if (bad != SP_OK) return bad;
+  if (x_stride < d || xs_stride < d || (n > 0 && !x) || (n > 0 && rows > 0 && !xs) || !aligned(x, dtype) || !aligned(xs, dtype)) return SP_EINVAL;
+  if (n == 0) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  with_rows(n, d, dtype, [&]<typename T, int TEAM>(dim3 grid) {
+    hipLaunchKernelGGL((k_dispatch<T, TEAM>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, (const T*)x, x_stride, place, rows, (T*)xs,
+                       xs_stride, o->err);
+  });
+  return launched(o);
+}
+
+sp_status sp_combine(sp_ops* o, int32_t n, int32_t d, int32_t top, int32_t dtype, int32_t rows, const void* ys, int64_t ys_stride,
+                     const int32_t* place, const float* weight, const void* residual, int64_t residual_stride, void* y, int64_t y_stride,
+                     void* stream) {
+  const sp_status bad = move_sizes(o, n, d, top, dtype, rows, place);
+  if (bad != SP_OK) return bad;
+  if (ys_stride < d || y_stride < d || (residual && residual_stride < d) || (n > 0 && !y) || (n > 0 && rows > 0 && !ys)) return SP_EINVAL;
+  if (!aligned(ys, dtype) || !aligned(y, dtype) || !aligned(residual, dtype) || !aligned4(weight)) return SP_EINVAL;
+  if (n == 0) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  with_rows(n, d, dtype, [&]<typename T, int TEAM>(dim3 grid) {
+    hipLaunchKernelGGL((k_combine<T, TEAM>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, rows, (const T*)ys, ys_stride, place, weight,
+                       (const T*)residual, residual_stride, (T*)y, y_stride, o->err);
+  });
+  return launched(o);
+}
+
+sp_status sp_combine_backward(sp_ops* o, int32_t n, int32_t d, int32_t top, int32_t dtype, const void* dy, int64_t dy_stride, int32_t rows,
+                              const void* ys, int64_t ys_stride, const int32_t* place, const float* weight, void* dys, int64_t dys_stride,
+                              float* dweight, void* stream) {
+  const sp_status bad = move_sizes(o, n, d, top, dtype, rows, place);
+  if (bad != SP_OK) return bad;
+  if (dy_stride < d || (dweight && ys_stride < d) || (dys && dys_stride < d) || (n > 0 && !dy) || (n > 0 && rows > 0 && dweight && !ys))
+    return SP_EINVAL;
+  if (!aligned(dy, dtype) || !aligned(ys, dtype) || !aligned(dys, dtype) || !aligned4(weight) || !aligned4(dweight)) return SP_EINVAL;
+  if (n == 0 || (!dys && !dweight)) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  with_rows(n, d, dtype, [&]<typename T, int TEAM>(dim3 grid) {
+    hipLaunchKernelGGL((k_combine_back<T, TEAM>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, (const T*)dy, dy_stride, rows,
+                       (const T*)ys, ys_stride, place, weight, (T*)dys, dys_stride, dweight, o->err);
+  });
+  return launched(o);
+}
+
+sp_status sp_dropout(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const void* x, int64_t x_stride, float p, uint64_t seed, uint64_t offset,
+                     const int64_t* step, const void* residual, int64_t residual_stride, void* y, int64_t y_stride, void* stream) {
+  if (!o || n < 0 || d < 1 || !dtype_ok(dtype) || x_stride < d || y_stride < d || (residual && residual_stride < d)) return SP_EINVAL;
+  if (!(p >= 0.f && p <= 1.f) || (n > 0 && (!x || !y))) return SP_EINVAL;
+  if (!aligned(x, dtype) || !aligned(y, dtype) || !aligned(residual, dtype) || ((uintptr_t)step & 7u)) return SP_EINVAL;
+  if (d > SP_MAX_LINEAR_DIM) return SP_ECAPACITY;
+  DropoutArgs a{};
+  a.n = n; a.d = d; a.pieces = (d + 7) / 8;
+  a.drop = (uint32_t)std::lround((double)p * 65536.0);
+  if (p > 0.f && a.drop == 0) a.drop = 1;
+  if (p < 1.f && a.drop == 65536) a.drop = 65535;
+  a.scale = a.drop == 65536 ? 0.f : 65536.f / (float)(65536 - a.drop);
+  a.key0 = (uint32_t)seed; a.key1 = (uint32_t)(seed >> 32); a.offset = offset; a.step = step;
+  a.x = x; a.x_stride = x_stride; a.residual = residual; a.residual_stride = residual_stride; a.y = y; a.y_stride = y_stride;
+  const int64_t blocks = ((int64_t)n * a.pieces + 256 * kDropoutEach - 1) / (256 * kDropoutEach);
+  if (blocks * 256 > UINT32_MAX) return SP_ECAPACITY;
+  if (n == 0) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  with_type(dtype, [&]<typename T>() { hipLaunchKernelGGL((k_dropout<T>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, a); });
+  return launched(o);
+}
+
+sp_status sp_quantize_rows(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const void* x, int64_t x_stride, int8_t* q, int64_t q_stride,
+                           float* scale, void* stream) {
+  if (!o || n < 0 || d < 1 || !dtype_ok(dtype) || x_stride < d || q_stride < d || (n > 0 && (!x || !q || !scale))) return SP_EINVAL;
+  if (!aligned(x, dtype) || !aligned4(scale)) return SP_EINVAL;
+  if (d > SP_MAX_LINEAR_DIM) return SP_ECAPACITY;
+  if (n == 0) return SP_OK;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  with_type(dtype, [&]<typename T>() {
+    const bool fits = with_team((d + kPiece<T> - 1) / kPiece<T>, [&]<int TEAM, int C>() {
+      constexpr int threads = kTeamThreads<TEAM>, rows = threads / TEAM;
+      const int blocks = (int)std::min<int64_t>(((int64_t)n + rows - 1) / rows, 8192);
+      hipLaunchKernelGGL((k_quantize<T, TEAM, C>), dim3(blocks), dim3(threads), 0, (hipStream_t)stream, n, d, (const T*)x, x_stride, q, q_stride,
+                         scale);
+    });
+    if (!fits)
+      hipLaunchKernelGGL((k_quantize_wide<T>), dim3(std::min(n, 4096)), dim3(1024), 0, (hipStream_t)stream, n, d, (const T*)x, x_stride, q,
+                         q_stride, scale);
+  });
+  return launched(o);
+}
+
+sp_status sp_grouped_linear_quantized(sp_ops* o, int32_t n, int32_t k, int32_t m, int32_t groups, const int8_t* x, int64_t x_stride,
+                                      const float* x_scale, const int32_t* offsets, const int8_t* w, const float* w_scale, const float* bias,
+                                      int32_t activation, int32_t out_dtype, const void* residual, int64_t residual_stride, void* y,
+                                      int64_t y_stride, void* stream) {
+  if (!o || n < 0 || k < 1 || m < 1 || groups < 1 || x_stride < k || y_stride < m || (residual && residual_stride < m)) return SP_EINVAL;
+  if ((activation != SP_ACT_NONE && activation != SP_ACT_RELU) || !dtype_ok(out_dtype)) return SP_EINVAL;
+  if (n > 0 && (!x || !x_scale || !offsets || !w || !w_scale || !y)) return SP_EINVAL;
+  if (!aligned(y, out_dtype) || !aligned(residual, out_dtype) || !aligned4(x_scale) || !aligned4(offsets) || !aligned4(w_scale) || !aligned4(bias))
+    return SP_EINVAL;
+  if (groups > SP_MAX_APPS || k > SP_MAX_QUANTIZED_INPUTS || m > SP_MAX_LINEAR_DIM) return SP_ECAPACITY;
+  if (n == 0) return SP_OK;
+  QuantizedArgs a{};
+  a.n = n; a.k = k; a.m = m; a.groups = groups; a.x = x; a.x_stride = x_stride; a.x_scale = x_scale; a.offsets = offsets; a.w = w;
+  a.w_scale = w_scale; a.bias = bias; a.relu = activation == SP_ACT_RELU; a.residual = residual; a.residual_stride = residual_stride;
+  a.y = y; a.y_stride = y_stride; a.err = o->err;
+  const int64_t row_tiles = std::min<int64_t>(((int64_t)n + 127) / 128 + groups, n), col_tiles = (m + 127) / 128;
+  const int64_t blocks = (row_tiles * col_tiles + kXcds - 1) / kXcds * kXcds;
+  if (blocks * 256 > UINT32_MAX) return SP_ECAPACITY;
+  a.row_tiles = (int)row_tiles;
+  a.col_tiles = (int)col_tiles;
+  DeviceGuard g(o->device);
+  if (!g.ok) return SP_EDEVICE;
+  with_type(out_dtype, [&]<typename T>() { hipLaunchKernelGGL((k_quantized<T>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, a); });
+  return launched(o);
+}
+
+}  // extern "C"

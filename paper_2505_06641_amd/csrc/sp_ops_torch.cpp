@@ -112,6 +112,21 @@ struct Call {
     if (v == -1.0 && PyErr_Occurred()) refuse("");
     return v;
   }
+  int32_t whole_number(PyObject* o, int32_t otherwise) {
+    if (!o) return otherwise;
+    const long v = PyLong_AsLong(o);
+    if (v == -1 && PyErr_Occurred()) refuse("");
+    else if (v < INT32_MIN || v > INT32_MAX) refuse("a number is beyond 32 bits");
+    return (int32_t)v;
+  }
+  // 64 bits, negative numbers among them.
+  uint64_t word(PyObject* o, const char* name) {
+    if (!o) return 0;
+    const uint64_t v = PyLong_Check(o) ? PyLong_AsUnsignedLongLongMask(o) : 0;
+    if (!PyLong_Check(o)) refuse(std::string(name) + " is no whole number");
+    else if (PyErr_Occurred()) refuse("");
+    return v;
+  }
   bool truth(PyObject* o) {
     const int v = o ? PyObject_IsTrue(o) : 0;
     if (v < 0) refuse("");
@@ -313,6 +328,197 @@ PyObject* cross_entropy(OpsObject* self, PyObject* const* args, Py_ssize_t nargs
                                           (float*)weight, scale, (float*)po, gt, pd, ds, s));
 }
 
+// [rows, top] of a routing tensor.
+void shape_of_pairs(Call& c, const at::Tensor* t, const char* name, int64_t* n, int64_t* top) {
+  if (c.bad) return;
+  if (t->dim() != 2) {
+    c.refuse(std::string(name) + " is not [rows, experts of a row]");
+    return;
+  }
+  *n = t->size(0);
+  *top = t->size(1);
+}
+
+PyObject* route(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<10> names({"logits", "expert", "weight", "sigmoid", "bias", "groups", "top_groups", "renormalize", "scale", "stream"});
+  Call c{"sp_route", self->device};
+  PyObject* v[10];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, experts = 0, rows = 0, top = 0, zs;
+  const at::Tensor *z = c.matrix(v[0], "logits", &n, &experts), *expert = c.needed(v[1], "expert"), *weight = c.needed(v[2], "weight");
+  if (c.bad) return nullptr;
+  shape_of_pairs(c, expert, "expert", &rows, &top);
+  const int32_t dt = c.dtype(z, "logits");
+  void *pz = c.rows(z, "logits", z->scalar_type(), n, experts, &zs), *pe = c.whole(expert, "expert", at::kInt, {n, top}),
+       *pw = c.whole(weight, "weight", at::kFloat, {n, top}), *bias = c.whole(v[4], "bias", at::kFloat, {experts});
+  const int32_t score = c.truth(v[3]) ? SP_SCORE_SIGMOID : SP_SCORE_SOFTMAX, again = v[7] ? c.truth(v[7]) : 1;
+  const int32_t groups = c.whole_number(v[5], 1), kept = c.whole_number(v[6], 1);
+  const float scale = (float)c.number(v[8], 1.0);
+  const int32_t ni = c.count(n, "logits' rows"), ei = c.count(experts, "experts"), ti = c.count(top, "experts of a row");
+  void* s = c.stream(v[9]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_route(self->handle, ni, ei, ti, dt, pz, zs, score, (float*)bias, groups, kept, again, scale, (int32_t*)pe, (float*)pw, s));
+}
+
+PyObject* route_backward(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<8> names({"logits", "expert", "dweight", "dlogits", "sigmoid", "renormalize", "scale", "stream"});
+  Call c{"sp_route_backward", self->device};
+  PyObject* v[8];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, experts = 0, rows = 0, top = 0, zs, ds;
+  const at::Tensor *z = c.matrix(v[0], "logits", &n, &experts), *expert = c.needed(v[1], "expert"), *dw = c.needed(v[2], "dweight"),
+                   *dz = c.needed(v[3], "dlogits");
+  if (c.bad) return nullptr;
+  shape_of_pairs(c, expert, "expert", &rows, &top);
+  const int32_t dt = c.dtype(z, "logits");
+  void *pz = c.rows(z, "logits", z->scalar_type(), n, experts, &zs), *pd = c.rows(dz, "dlogits", z->scalar_type(), n, experts, &ds);
+  void *pe = c.whole(expert, "expert", at::kInt, {n, top}), *pw = c.whole(dw, "dweight", at::kFloat, {n, top});
+  const int32_t score = c.truth(v[4]) ? SP_SCORE_SIGMOID : SP_SCORE_SOFTMAX, again = v[5] ? c.truth(v[5]) : 1;
+  const float scale = (float)c.number(v[6], 1.0);
+  const int32_t ni = c.count(n, "logits' rows"), ei = c.count(experts, "experts"), ti = c.count(top, "experts of a row");
+  void* s = c.stream(v[7]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_route_backward(self->handle, ni, ei, ti, dt, pz, zs, score, again, scale, (int32_t*)pe, (float*)pw, pd, ds, s));
+}
+
+PyObject* route_order(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<4> names({"expert", "offsets", "place", "stream"});
+  Call c{"sp_route_order", self->device};
+  PyObject* v[4];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, top = 0;
+  const at::Tensor *expert = c.matrix(v[0], "expert", &n, &top), *offsets = c.needed(v[1], "offsets"), *place = c.needed(v[2], "place");
+  if (c.bad) return nullptr;
+  const int64_t experts = offsets->numel() - 1;
+  void *pe = c.whole(expert, "expert", at::kInt, {n, top}), *po = c.whole(offsets, "offsets", at::kInt, {experts + 1}),
+       *pp = c.whole(place, "place", at::kInt, {n, top});
+  const int32_t ni = c.count(n, "expert's rows"), ei = c.count(experts, "experts"), ti = c.count(top, "experts of a row");
+  void* s = c.stream(v[3]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_route_order(self->handle, ni, ti, ei, (int32_t*)pe, (int32_t*)po, (int32_t*)pp, s));
+}
+
+PyObject* dispatch(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<4> names({"x", "place", "xs", "stream"});
+  Call c{"sp_dispatch", self->device};
+  PyObject* v[4];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, d = 0, rows = 0, width = 0, pn = 0, top = 0, xs, ss;
+  const at::Tensor *x = c.matrix(v[0], "x", &n, &d), *place = c.matrix(v[1], "place", &pn, &top), *sorted = c.matrix(v[2], "xs", &rows, &width);
+  if (c.bad) return nullptr;
+  const int32_t dt = c.dtype(x, "x");
+  void *px = c.rows(x, "x", x->scalar_type(), n, d, &xs), *pp = c.whole(place, "place", at::kInt, {n, top}),
+       *ps = c.rows(sorted, "xs", x->scalar_type(), rows, d, &ss);
+  const int32_t ni = c.count(n, "x's rows"), di = c.count(d, "x's width"), ti = c.count(top, "experts of a row"), ri = c.count(rows, "xs' rows");
+  void* s = c.stream(v[3]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_dispatch(self->handle, ni, di, ti, dt, px, xs, (int32_t*)pp, ri, ps, ss, s));
+}
+
+PyObject* combine(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<6> names({"ys", "place", "y", "weight", "residual", "stream"});
+  Call c{"sp_combine", self->device};
+  PyObject* v[6];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, d = 0, rows = 0, width = 0, pn = 0, top = 0, ss, rs, ys;
+  const at::Tensor *sorted = c.matrix(v[0], "ys", &rows, &width), *place = c.matrix(v[1], "place", &pn, &top), *y = c.matrix(v[2], "y", &n, &d);
+  if (c.bad) return nullptr;
+  const int32_t dt = c.dtype(y, "y");
+  const auto type = y->scalar_type();
+  void *ps = c.rows(sorted, "ys", type, rows, d, &ss), *pp = c.whole(place, "place", at::kInt, {n, top}), *py = c.rows(y, "y", type, n, d, &ys);
+  void *pw = c.whole(v[3], "weight", at::kFloat, {n, top}), *pr = c.rows(v[4], "residual", type, n, d, &rs);
+  const int32_t ni = c.count(n, "y's rows"), di = c.count(d, "y's width"), ti = c.count(top, "experts of a row"), ri = c.count(rows, "ys' rows");
+  void* s = c.stream(v[5]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_combine(self->handle, ni, di, ti, dt, ri, ps, ss, (int32_t*)pp, (float*)pw, pr, rs, py, ys, s));
+}
+
+PyObject* combine_backward(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<7> names({"dy", "ys", "place", "weight", "dys", "dweight", "stream"});
+  Call c{"sp_combine_backward", self->device};
+  PyObject* v[7];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, d = 0, pn = 0, top = 0, gs, ss, os;
+  const at::Tensor *dy = c.matrix(v[0], "dy", &n, &d), *place = c.matrix(v[2], "place", &pn, &top), *sorted = c.tensor(v[1], "ys"),
+                   *out = c.tensor(v[4], "dys"), *some = sorted ? sorted : out;
+  if (c.bad) return nullptr;
+  if (some && some->dim() != 2) c.refuse("ys and dys are matrices");
+  if (c.bad) return nullptr;
+  const int64_t rows = some ? some->size(0) : 0;
+  const int32_t dt = c.dtype(dy, "dy");
+  const auto type = dy->scalar_type();
+  void *pg = c.rows(dy, "dy", type, n, d, &gs), *ps = c.rows(sorted, "ys", type, rows, d, &ss), *po = c.rows(out, "dys", type, rows, d, &os);
+  void *pp = c.whole(place, "place", at::kInt, {n, top}), *pw = c.whole(v[3], "weight", at::kFloat, {n, top}),
+       *pd = c.whole(v[5], "dweight", at::kFloat, {n, top});
+  const int32_t ni = c.count(n, "dy's rows"), di = c.count(d, "dy's width"), ti = c.count(top, "experts of a row"), ri = c.count(rows, "ys' rows");
+  void* s = c.stream(v[6]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_combine_backward(self->handle, ni, di, ti, dt, pg, gs, ri, ps, ss, (int32_t*)pp, (float*)pw, po, os, (float*)pd, s));
+}
+
+PyObject* dropout(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<8> names({"x", "y", "p", "seed", "offset", "step", "residual", "stream"});
+  Call c{"sp_dropout", self->device};
+  PyObject* v[8];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, d = 0, xs, ys, rs;
+  const at::Tensor *x = c.matrix(v[0], "x", &n, &d), *y = c.needed(v[1], "y");
+  if (c.bad) return nullptr;
+  if (!v[2] || !v[3]) c.refuse("p and seed are missing");
+  const int32_t dt = c.dtype(x, "x");
+  const auto type = x->scalar_type();
+  void *px = c.rows(x, "x", type, n, d, &xs), *py = c.rows(y, "y", type, n, d, &ys), *pr = c.rows(v[6], "residual", type, n, d, &rs);
+  void* step = c.whole(v[5], "step", at::kLong, {1});
+  const double p = c.number(v[2], 0.0);
+  const uint64_t seed = c.word(v[3], "seed"), offset = c.word(v[4], "offset");
+  const int32_t ni = c.count(n, "x's rows"), di = c.count(d, "x's width");
+  void* s = c.stream(v[7]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_dropout(self->handle, ni, di, dt, px, xs, (float)p, seed, offset, (int64_t*)step, pr, rs, py, ys, s));
+}
+
+PyObject* quantize_rows(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<4> names({"x", "q", "scale", "stream"});
+  Call c{"sp_quantize_rows", self->device};
+  PyObject* v[4];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, d = 0, xs, qs;
+  const at::Tensor *x = c.matrix(v[0], "x", &n, &d), *q = c.needed(v[1], "q"), *scale = c.needed(v[2], "scale");
+  if (c.bad) return nullptr;
+  const int32_t dt = c.dtype(x, "x");
+  void *px = c.rows(x, "x", x->scalar_type(), n, d, &xs), *pq = c.rows(q, "q", at::kChar, n, d, &qs), *pc = c.whole(scale, "scale", at::kFloat, {n});
+  const int32_t ni = c.count(n, "x's rows"), di = c.count(d, "x's width");
+  void* s = c.stream(v[3]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_quantize_rows(self->handle, ni, di, dt, px, xs, (int8_t*)pq, qs, (float*)pc, s));
+}
+
+PyObject* grouped_linear_quantized(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  static const Names<10> names({"x", "x_scale", "offsets", "w", "w_scale", "y", "bias", "relu", "residual", "stream"});
+  Call c{"sp_grouped_linear_quantized", self->device};
+  PyObject* v[10];
+  if (!names.parse(c, args, nargs, kw, v)) return nullptr;
+  int64_t n = 0, k = 0, xs, ys, rs;
+  const at::Tensor *x = c.matrix(v[0], "x", &n, &k), *x_scale = c.needed(v[1], "x_scale"), *offsets = c.needed(v[2], "offsets"),
+                   *w = c.needed(v[3], "w"), *w_scale = c.needed(v[4], "w_scale"), *y = c.needed(v[5], "y");
+  if (c.bad) return nullptr;
+  if (w->dim() != 3) c.refuse("w is not [groups, outputs, inputs]");
+  if (c.bad) return nullptr;
+  const int64_t groups = w->size(0), m = w->size(1);
+  const int32_t ot = c.dtype(y, "y");
+  const auto out = y->scalar_type();
+  void *px = c.rows(x, "x", at::kChar, n, k, &xs), *pxs = c.whole(x_scale, "x_scale", at::kFloat, {n}),
+       *po = c.whole(offsets, "offsets", at::kInt, {groups + 1}), *pw = c.whole(w, "w", at::kChar, {groups, m, k}),
+       *pws = c.whole(w_scale, "w_scale", at::kFloat, {groups, m}), *py = c.rows(y, "y", out, n, m, &ys);
+  void *bias = c.whole(v[6], "bias", at::kFloat, {groups, m}), *pr = c.rows(v[8], "residual", out, n, m, &rs);
+  const int32_t act = c.truth(v[7]) ? SP_ACT_RELU : SP_ACT_NONE;
+  const int32_t rows = c.count(n, "x's rows"), ki = c.count(k, "inputs"), mo = c.count(m, "outputs"), g = c.count(groups, "groups");
+  void* s = c.stream(v[9]);
+  if (c.bad) return nullptr;
+  return finish(self, c, sp_grouped_linear_quantized(self->handle, rows, ki, mo, g, (int8_t*)px, xs, (float*)pxs, (int32_t*)po, (int8_t*)pw,
+                                                     (float*)pws, (float*)bias, act, ot, pr, rs, py, ys, s));
+}
+
 // A list of tensors as sp_clip_grad_norm takes them.  What is kept is the tensors: one that gets other storage (assignment to .data, set_,
 // resize_) is found where it is at the time of the call, and checked anew.
 struct Packed {
@@ -449,6 +655,29 @@ PyMethodDef ops_methods[] = {
     {"sp_cross_entropy", with_names<cross_entropy>(), METH_FASTCALL | METH_KEYWORDS,
      "sp_cross_entropy(logits, label, loss, app=None, n_classes=None, weight=None, scale=1.0, dlogits=None, stream=None)\n\n"
      "loss [n] and dlogits of softmax cross entropy over the first n_classes[app[i]] columns (all of them without app)."},
+    {"sp_route", with_names<route>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_route(logits, expert, weight, sigmoid=False, bias=None, groups=1, top_groups=1, renormalize=True, scale=1.0, stream=None)\n\n"
+     "expert (int32 [n, top]) and weight (float32 [n, top]) of each row of logits [n, experts]."},
+    {"sp_route_backward", with_names<route_backward>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_route_backward(logits, expert, dweight, dlogits, sigmoid=False, renormalize=True, scale=1.0, stream=None)\n\n"
+     "dlogits of sp_route's weights, with its experts and the arguments that it had."},
+    {"sp_route_order", with_names<route_order>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_route_order(expert, offsets, place, stream=None)\n\n"
+     "offsets (int32 [experts + 1]) and place (int32 [n, top]) of the rows sorted by expert."},
+    {"sp_dispatch", with_names<dispatch>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_dispatch(x, place, xs, stream=None)\n\nxs[place_ij] = x_i; its gradient is sp_combine(dxs, place, dx)."},
+    {"sp_combine", with_names<combine>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_combine(ys, place, y, weight=None, residual=None, stream=None)\n\ny_i = sum of weight_ij ys[place_ij] + residual_i."},
+    {"sp_combine_backward", with_names<combine_backward>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_combine_backward(dy, ys, place, weight=None, dys=None, dweight=None, stream=None)\n\nGradients of sp_combine; ys is read for dweight."},
+    {"sp_dropout", with_names<dropout>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_dropout(x, y, p, seed, offset=0, step=None, residual=None, stream=None)\n\n"
+     "y = x / (1 - p) or 0, plus the residual; the same call on dy is the gradient.  step: int64 [1] on the device, added to offset."},
+    {"sp_quantize_rows", with_names<quantize_rows>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_quantize_rows(x, q, scale, stream=None)\n\nx's rows as int8 q [n, d] with scale float32 [n]."},
+    {"sp_grouped_linear_quantized", with_names<grouped_linear_quantized>(), METH_FASTCALL | METH_KEYWORDS,
+     "sp_grouped_linear_quantized(x, x_scale, offsets, w, w_scale, y, bias=None, relu=False, residual=None, stream=None)\n\n"
+     "y = act(x_scale w_scale x W_g^T + b_g) + residual; x int8 [n, k], w int8 [groups, m, k], w_scale float32 [groups, m]."},
     {"clip_packed", positional<clip_packed, OpsObject>(), METH_FASTCALL, "clip_packed(packed, max_norm, norm, stream): sp_clip_grad_norm of packed tensors"},
     {nullptr, nullptr, 0, nullptr}};
 

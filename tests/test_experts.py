@@ -1,0 +1,929 @@
+"""The operators for heads that are made of experts against their definitions in 64 bits, on the GPU.
+
+Tolerances.  u = 2^-24 is half a step of float32, `half_step` that of the output's type.  exp of a difference d that was rounded is off by
+|d| u, and by 3 |d| u where it is taken as a power of two of a rounded product; the function itself by 2 u.  A sum of t terms is off by at
+most t u times the sum of their magnitudes.  Each bound is written out where it is used.
+"""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DEV = "cuda:0"
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: the gpu-marked tests need a real MI355X")
+    from paper_2505_06641_amd import binding
+    binding.load_library()
+    return torch, binding
+
+
+@pytest.fixture(scope="module")
+def ops(gpu):
+    o = gpu[1].Ops()
+    yield o
+    o.sp_ops_check()
+    o.close()
+
+
+def half_step(torch, t):
+    return torch.finfo(t).eps / 2
+
+
+def dtype_of(torch, name):
+    return {"f32": torch.float32, "bf16": torch.bfloat16}[name]
+
+
+def in_layout(torch, v, layout):
+    """The values of a matrix on the device: contiguous, rows further apart than they are long, or rows that start at any element.  What
+    lies between the rows is NaN (whole numbers: 77)."""
+    n, d = v.shape
+    if layout == "plain":
+        return v.to(DEV)
+    pad, lead = {"apart": (16, 0), "odd": (3, 1)}[layout]
+    fill = float("nan") if v.dtype.is_floating_point else 77
+    store = torch.full((n * (d + pad) + lead + 1,), fill, dtype=v.dtype, device=DEV)
+    out = store[lead:lead + n * (d + pad)].view(n, d + pad)[:, :d]
+    out.copy_(v)
+    return out
+
+
+def assert_within(torch, got, want, bound, what):
+    """|got - want| <= bound everywhere; want and bound are float64."""
+    err = (got.double() - want).abs()
+    bad = ~(err <= bound)
+    assert not bool(bad.any()), (what, int(bad.sum()), float(torch.nan_to_num(err / bound.clamp(min=1e-300)).max()))
+
+
+# ---------------------------------------------------------------- routing
+
+def route_by_definition(torch, z, top, sigmoid, bias, groups, top_groups):
+    """Chosen experts, row by row, in 64 bits on the host.  z float64 [n, experts] with -inf for experts that are not there."""
+    z = z.cpu().numpy().astype(np.float64)
+    n, experts = z.shape
+    out = np.full((n, top), -1, dtype=np.int64)
+    width = experts // groups
+    for i in range(n):
+        there = z[i] > -INF
+        if not there.any():
+            continue
+        if bias is None and groups == 1:
+            c = z[i].copy()
+        else:
+            s = 1.0 / (1.0 + np.exp(-np.where(there, z[i], 0.0))) if sigmoid else np.exp(z[i] - z[i].max()) / np.exp(z[i] - z[i].max()).sum()
+            c = s + (0.0 if bias is None else bias)
+        c[~there] = -INF
+        if groups > 1:
+            value = []
+            for g in range(groups):
+                best = sorted(c[g * width:(g + 1) * width])[::-1][:2]
+                best = [b for b in best if b > -INF]
+                value.append(sum(best) if best else -INF)
+            keep = sorted(range(groups), key=lambda g: (-value[g], g))[:top_groups]
+            for g in range(groups):
+                if g not in keep:
+                    c[g * width:(g + 1) * width] = -INF
+        order = sorted(range(experts), key=lambda e: (-c[e], e))[:top]
+        order = [e for e in order if c[e] > -INF]
+        out[i, :len(order)] = order
+    return torch.from_numpy(out).to(DEV)
+
+
+def weights_by_definition(torch, z, expert, sigmoid, renormalize, scale):
+    """Weights and a bound of their relative error."""
+    got = expert >= 0
+    zc = z.gather(1, expert.clamp(min=0))
+    low = torch.where(got, zc, INF).amin(1, keepdim=True)
+    high = torch.where(got, zc, -INF).amax(1, keepdim=True)
+    spread = torch.where(high > -INF, high - low, 0.0)
+    if renormalize:
+        part = torch.nn.functional.logsigmoid(zc) if sigmoid else zc
+        part = torch.where(got, part, -INF)
+        w = torch.softmax(part, 1).nan_to_num(0.0)
+        # a term: its exp, the sum and quotient below a sigmoid, and the same for the terms of the sum, 32 additions, a quotient, a product
+        rel = (2 * (spread + 8) + 36) * U
+    elif sigmoid:
+        # exp (2 u and that of its rounded argument: none), 1 + exp, a quotient, a product
+        w, rel = torch.sigmoid(zc), torch.full_like(spread, 10 * U)
+    else:
+        top = z.amax(1, keepdim=True)
+        d = torch.where(z > -INF, top - z, 0.0)
+        e = torch.where(z > -INF, torch.exp(-d), 0.0)
+        total = e.sum(1, keepdim=True)
+        w = (e / total).gather(1, expert.clamp(min=0))
+        off = (e * (3 * d + 3)).sum(1, keepdim=True) / total        # of the sum's terms, in u
+        rel = ((top - zc).abs().nan_to_num(0.0, 0.0, 0.0) + off + 45) * U
+    w = torch.where(got, w, 0.0)
+    return w * scale, rel * (w * scale).abs() + 1e-37
+
+
+def places_by_definition(expert, experts):
+    flat = expert.reshape(-1).cpu().numpy()
+    counts = np.bincount(flat[flat >= 0], minlength=experts)
+    offsets = np.concatenate([[0], np.cumsum(counts)])
+    nxt, place = offsets[:-1].copy(), np.full(flat.shape, -1)
+    for i, e in enumerate(flat):
+        if e >= 0:
+            place[i] = nxt[e]
+            nxt[e] += 1
+    return offsets, place.reshape(expert.shape)
+
+
+def run_route(torch, ops, z, top, **kw):
+    n, experts = z.shape
+    expert = torch.full((n, top), 12345, dtype=torch.int32, device=DEV)
+    weight = torch.full((n, top), math.nan, device=DEV)
+    ops.sp_route(z, expert, weight, **kw)
+    return expert, weight
+
+
+def check_route(torch, ops, z, top, sigmoid=False, bias=None, groups=1, top_groups=1, renormalize=True, scale=1.0):
+    expert, weight = run_route(torch, ops, z, top, sigmoid=sigmoid, bias=bias, groups=groups, top_groups=top_groups, renormalize=renormalize,
+                               scale=scale)
+    zd = z.double()
+    want = route_by_definition(torch, zd, top, sigmoid, None if bias is None else bias.cpu().numpy().astype(np.float64), groups, top_groups)
+    assert torch.equal(expert.long(), want), int((expert.long() != want).sum())
+    w, bound = weights_by_definition(torch, zd, want, sigmoid, renormalize, scale)
+    assert_within(torch, weight, w, bound, "weight")
+    return expert, weight
+
+
+ROUTE_SIZES = [(1, 1, 1), (1, 64, 6), (3, 2, 2), (5, 7, 3), (130, 8, 8), (33, 60, 4), (17, 64, 8), (9, 65, 1), (40, 128, 8), (21, 200, 5), (65, 256, 8),
+               (4, 256, 32), (5, 257, 9), (3, 500, 16), (4, 1000, 8), (3, 1024, 32), (2100, 16, 2)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,experts,top", ROUTE_SIZES)
+def test_route(gpu, ops, n, experts, top, dtype):
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    rng = np.random.default_rng(n * 7919 + experts * 31 + top)
+    for turn, (sigmoid, biased, renormalize) in enumerate([(False, False, True), (True, False, True), (False, True, False), (True, True, True),
+                                                           (False, False, False), (True, False, False)]):
+        z = torch.from_numpy(rng.standard_normal((n, experts)) * 2).to(t)
+        z = in_layout(torch, z, ("plain", "odd", "apart")[turn % 3])
+        bias = torch.from_numpy(rng.standard_normal(experts) * 0.2).float().to(DEV) if biased else None
+        check_route(torch, ops, z, top, sigmoid=sigmoid, bias=bias, renormalize=renormalize, scale=1.0 if turn % 2 else 2.5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,experts,groups,top_groups,top", [
+    (1, 64, 8, 4, 6), (33, 64, 8, 4, 8), (21, 256, 8, 4, 8), (40, 60, 4, 2, 5), (9, 60, 3, 1, 7), (17, 63, 7, 3, 8), (5, 64, 64, 5, 5), (3, 1024, 64, 9, 32),
+    (4, 1023, 33, 4, 8), (6, 1020, 17, 5, 9), (7, 1023, 3, 2, 8), (11, 6, 2, 2, 6), (30, 40, 5, 5, 3), (25, 24, 8, 3, 4), (50, 16, 2, 1, 8)])
+def test_route_by_groups(gpu, ops, n, experts, groups, top_groups, top, dtype):
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    rng = np.random.default_rng(experts * 31 + groups)
+    for sigmoid, biased, renormalize, hide in [(True, True, True, 0.0), (False, False, True, 0.0), (False, True, False, 0.3), (True, False, True, 0.7),
+                                               (True, True, False, 0.95)]:
+        z = torch.from_numpy(rng.standard_normal((n, experts)) * 1.5).to(t)
+        z[torch.from_numpy(rng.random((n, experts)) < hide)] = -INF
+        bias = torch.from_numpy(rng.standard_normal(experts) * 0.1).float().to(DEV) if biased else None
+        check_route(torch, ops, z.to(DEV), top, sigmoid=sigmoid, bias=bias, groups=groups, top_groups=top_groups, renormalize=renormalize)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("experts,top", [(8, 4), (60, 8), (256, 8), (500, 6)])
+def test_route_of_masked_and_equal_logits(gpu, ops, experts, top, dtype):
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    rng = np.random.default_rng(experts)
+    lowest = torch.finfo(t).min
+    z = torch.from_numpy(np.round(rng.standard_normal((40, experts)))).to(t)      # many equal ones
+    z[0] = -INF                                            # no expert at all
+    z[1, :] = -INF
+    z[1, experts - 1] = -3.0                               # a single one
+    z[2, :] = 0.0                                          # all equal
+    z[3, :] = lowest                                       # the lowest values are values
+    z[4, ::2] = lowest
+    z[5, 1:] = -INF
+    z[6] *= 40.0                                           # far apart
+    z[7] = z[7] * 1e4
+    z[8] -= 1000.0                                         # sigmoids that underflow, in every row of their sum
+    z[9, : experts // 2] = -INF
+    z[10, -2:] = torch.finfo(t).max
+    for sigmoid in (False, True):
+        for renormalize in (False, True):
+            expert, weight = run_route(torch, ops, z.to(DEV), top, sigmoid=sigmoid, renormalize=renormalize)
+            want = route_by_definition(torch, z.double(), top, sigmoid, None, 1, 1)
+            assert torch.equal(expert.long(), want)
+            assert torch.equal(weight == 0, weight.clamp(max=0) == weight) and bool(torch.isfinite(weight).all())
+            assert bool((weight[expert < 0] == 0).all())
+            if renormalize:
+                some = (expert >= 0).any(1)
+                assert_within(torch, weight[some].sum(1), torch.ones(int(some.sum()), dtype=torch.float64, device=DEV),
+                              torch.full((int(some.sum()),), 100 * U, dtype=torch.float64, device=DEV), "sum of weights")
+    # scores that are equal in 64 bits (sigmoids of 40 and more are 1) go by number, with a bias by the bias
+    z = torch.full((2, experts), 50.0, dtype=t, device=DEV)
+    bias = torch.zeros(experts, device=DEV)
+    expert, _ = run_route(torch, ops, z, top, sigmoid=True, bias=bias)
+    assert expert.tolist() == [list(range(top))] * 2
+    bias[experts - 1] = 2.0 ** -40
+    expert, _ = run_route(torch, ops, z, top, sigmoid=True, bias=bias)
+    assert expert[0].tolist() == [experts - 1] + list(range(top - 1))
+
+
+def test_route_decides_what_float32_cannot(gpu, ops):
+    """Scores whose differences are far below a step of float32: biases and logits that all but cancel."""
+    torch, _ = gpu
+    n, experts, top = 600, 64, 6
+    rng = np.random.default_rng(5)
+    z = torch.from_numpy(rng.standard_normal((n, experts)) * 1e-4).float()
+    bias = torch.from_numpy(rng.standard_normal(experts) * 1e-9).float().to(DEV)
+    for sigmoid in (False, True):
+        for groups in (1, 8):
+            check_route(torch, ops, (z * 1e-4).to(DEV), top, sigmoid=sigmoid, bias=bias, groups=groups, top_groups=max(1, groups // 2))
+            check_route(torch, ops, (1.0 + z.round(decimals=5)).to(DEV), top, sigmoid=sigmoid, bias=bias, groups=groups, top_groups=max(1, groups // 2))
+    # without a bias: logits that differ in their last bit, and rows that span the whole range
+    close = (1.0 + torch.from_numpy(rng.integers(0, 40, (n, experts))) * 2.0 ** -23).float().to(DEV)
+    check_route(torch, ops, close, top)
+    far = torch.from_numpy(rng.standard_normal((n, experts)) * 1e30).float().to(DEV)
+    expert, _ = run_route(torch, ops, far, top, sigmoid=True)
+    assert torch.equal(expert.long(), route_by_definition(torch, far.double(), top, True, None, 1, 1))
+    # biases of a size at which a score is lost in float32
+    big = torch.from_numpy(np.repeat([1e6, -1e6], experts // 2)).float().to(DEV)
+    check_route(torch, ops, torch.from_numpy(rng.standard_normal((n, experts))).float().to(DEV), top, sigmoid=True, bias=big)
+
+
+def test_route_reports_logits_that_are_no_numbers(gpu):
+    torch, binding = gpu
+    o = binding.Ops()
+    for experts in (8, 64, 256, 1000):
+        for value in (math.nan, INF):
+            z = torch.randn(9, experts, device=DEV)
+            clean, _ = run_route(torch, o, z, 4)
+            z[4, experts // 2] = value
+            expert, weight = run_route(torch, o, z, 4)
+            with pytest.raises(binding.SneakPeekError):
+                o.sp_ops_check()
+            o.sp_ops_check()
+            assert bool((expert[4] == -1).all()) and bool((weight[4] == 0).all())
+            rest = torch.arange(9) != 4
+            assert torch.equal(expert[rest.to(DEV)], clean[rest.to(DEV)])
+    o.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,experts,top", ROUTE_SIZES)
+def test_route_backward(gpu, ops, n, experts, top, dtype):
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    rng = np.random.default_rng(n * 31 + experts * 7 + top)
+    for turn, (sigmoid, renormalize) in enumerate([(False, True), (True, True), (False, False), (True, False)]):
+        z = torch.from_numpy(rng.standard_normal((n, experts)) * 2).to(t)
+        z[torch.from_numpy(rng.random((n, experts)) < 0.1)] = -INF
+        if n > 2:
+            z[1] = -INF
+        scale = 1.0 if turn % 2 else 2.5
+        z = in_layout(torch, z, ("plain", "odd", "apart")[turn % 3])
+        expert, _ = run_route(torch, ops, z, top, sigmoid=sigmoid)
+        if n > 4:
+            expert[3, 0] = -1                              # dropped afterwards
+        dw = torch.from_numpy(rng.standard_normal((n, top))).float().to(DEV)
+        dz = in_layout(torch, torch.full((n, experts), math.nan, dtype=t), ("odd", "apart", "plain")[turn % 3])
+        ops.sp_route_backward(z, expert, dw, dz, sigmoid=sigmoid, renormalize=renormalize, scale=scale)
+        # the formula's, by differentiating the definition in 64 bits; float64 on the host, where nothing is fused
+        zd = z.double().cpu().requires_grad_()
+        got, at = (expert >= 0).cpu(), expert.clamp(min=0).long().cpu()
+        if sigmoid:
+            s = torch.sigmoid(zd)
+        else:
+            there = zd.detach() > -INF
+            s = torch.where(there, torch.softmax(torch.where(there, zd, -1e4), 1), 0.0)
+        sc = torch.where(got, s.gather(1, at), 0.0)
+        w = sc * scale
+        if renormalize:
+            w = w / torch.where(sc.sum(1, keepdim=True) > 0, sc.sum(1, keepdim=True), 1.0)
+        (w * dw.double().cpu()).sum().backward()
+        want = zd.grad.nan_to_num(0.0).to(DEV)
+        # every part: (dw - dot) times a share or score.  Shares are off by (2 (spread + 8) + 36) u, softmax scores by less than (3 spread + 60) u,
+        # spread that of the row's logits; dot is a sum of 32 products.  What is 0 by the formula comes out of differentiating in 64 bits as the
+        # difference of numbers of at most mag's size, whose 10 roundings are 2^-53 each: 2^-49 mag
+        zf = torch.where(z.double() > -INF, z.double(), 0.0)
+        rel = 3 * (zf.amax(1, keepdim=True) - zf.amin(1, keepdim=True)) + 120
+        mag = torch.where(expert >= 0, scale * dw.double().abs(), 0.0).sum(1, keepdim=True)
+        share = torch.zeros_like(want).scatter_add(1, expert.clamp(min=0).long(), torch.where(expert >= 0, 1.0, 0.0).double())
+        sd = s.detach().to(DEV)
+        size = share if renormalize or sigmoid else sd + share * sd
+        if sigmoid and not renormalize:
+            size = share * sd
+        bound = rel * U * mag * size * 2 + half_step(torch, t) * want.abs() * 1.01 + 2.0 ** -49 * mag + 1e-37
+        assert_within(torch, dz, want, bound, ("dz", sigmoid, renormalize))
+        if n > 2:
+            assert bool((dz[1] == 0).all())
+
+
+def test_route_backward_against_differences(gpu, ops):
+    torch, _ = gpu
+    n, experts, top, step = 16, 24, 4, 2.0 ** -8
+    g = torch.Generator().manual_seed(3)
+    # every tenth apart, in an order of its own in each row: a step changes no choice
+    z = torch.stack([torch.randperm(experts, generator=g) for _ in range(n)]).float().div(10).to(DEV)
+    up = torch.randn(n, top, generator=g).to(DEV)
+    for sigmoid in (False, True):
+        for renormalize in (False, True):
+            kw = dict(sigmoid=sigmoid, renormalize=renormalize, scale=1.5)
+            expert, _ = run_route(torch, ops, z, top, **kw)
+            dz = torch.empty_like(z)
+            ops.sp_route_backward(z, expert, up, dz, **kw)
+            for e in range(0, experts, 5):
+                side = []
+                for h in (step, -step):
+                    moved = z.clone()
+                    moved[:, e] += h
+                    other, w = run_route(torch, ops, moved, top, **kw)
+                    assert torch.equal(other.sort(1).values, expert.sort(1).values)
+                    w = torch.gather(w, 1, other.argsort(1).gather(1, expert.argsort(1).argsort(1)))    # weights in the first order
+                    side.append((w.double() * up.double()).sum(1))
+                slope = (side[0] - side[1]) / (2 * step)
+                # differences: step^2 / 6 times a third derivative of at most 6 scale sum |up|; weights off by 60 u over 2 step
+                mag = up.double().abs().sum(1) * 1.5
+                assert_within(torch, dz[:, e], slope, mag * (step ** 2 + 60 * U / step), e)
+
+
+def test_route_backward_of_experts_named_twice_and_of_bad_ones(gpu):
+    torch, binding = gpu
+    o = binding.Ops()
+    for experts in (12, 300):
+        z = torch.randn(3, experts, device=DEV)
+        expert = torch.tensor([[4, 4, 4, 1], [2, 0, 2, -1], [5, 6, 7, 8]], dtype=torch.int32, device=DEV)
+        dw = torch.randn(3, 4, device=DEV)
+        for sigmoid in (False, True):
+            for renormalize in (False, True):
+                dz = torch.empty_like(z)
+                o.sp_route_backward(z, expert, dw, dz, sigmoid=sigmoid, renormalize=renormalize)
+                zd = z.double().cpu().requires_grad_()
+                s = (torch.sigmoid(zd) if sigmoid else torch.softmax(zd, 1)).gather(1, expert.cpu().clamp(min=0).long()) * (expert >= 0).cpu()
+                w = s / s.sum(1, keepdim=True) if renormalize else s
+                (w * dw.double().cpu()).sum().backward()
+                mag = dw.double().abs().sum(1, keepdim=True)
+                assert_within(torch, dz, zd.grad.to(DEV), 300 * U * mag.expand(3, experts), "twice")
+        o.sp_ops_check()
+        for value in (-2, experts, 2 ** 31 - 1, -2 ** 31):
+            bad = expert.clone()
+            bad[1, 1] = value
+            o.sp_route_backward(z, bad, dw, dz)
+            with pytest.raises(binding.SneakPeekError):
+                o.sp_ops_check()
+            fine = expert.clone()
+            fine[1, 1] = -1
+            want = torch.empty_like(z)
+            o.sp_route_backward(z, fine, dw, want)
+            o.sp_ops_check()
+            assert torch.equal(dz, want)
+    # in place
+    z = torch.randn(50, 60, device=DEV).bfloat16()
+    expert, _ = run_route(torch, o, z, 4)
+    dw, dz = torch.randn(50, 4, device=DEV), torch.empty_like(z)
+    for kw in (dict(), dict(renormalize=False), dict(sigmoid=True)):
+        same = z.clone()
+        o.sp_route_backward(z, expert, dw, dz, **kw)
+        o.sp_route_backward(same, expert, dw, same, **kw)
+        assert torch.equal(same, dz)
+    o.sp_ops_check()
+    o.close()
+
+
+# ---------------------------------------------------------------- places
+
+@pytest.mark.parametrize("n,top,experts", [(0, 1, 1), (0, 4, 60), (1, 1, 1), (1, 8, 64), (5, 3, 1024), (63, 1, 2), (64, 1, 7), (65, 2, 3), (1000, 8, 256),
+                                           (1023, 1, 1), (4097, 4, 60), (16384, 1, 5), (16385, 1, 5), (9000, 8, 1024), (70001, 7, 100), (262144, 8, 256),
+                                           (300000, 1, 1000)])
+def test_route_order(gpu, ops, n, top, experts):
+    torch, _ = gpu
+    rng = np.random.default_rng(n + top + experts)
+    for none, skew in ((0.0, 1.0), (0.2, 3.0), (1.0, 1.0)):
+        e = np.minimum((rng.random((n, top)) ** skew * experts).astype(np.int32), experts - 1)
+        e[rng.random((n, top)) < none] = -1
+        expert = torch.from_numpy(e).to(DEV)
+        offsets = torch.full((experts + 1,), 999, dtype=torch.int32, device=DEV)
+        place = torch.full((n, top), 999, dtype=torch.int32, device=DEV)
+        ops.sp_route_order(expert, offsets, place)
+        want_o, want_p = places_by_definition(expert, experts)
+        assert np.array_equal(offsets.cpu().numpy(), want_o)
+        assert np.array_equal(place.cpu().numpy(), want_p)
+
+
+def test_route_order_reports_bad_experts(gpu):
+    torch, binding = gpu
+    o = binding.Ops()
+    for n in (50, 30000):
+        e = torch.randint(0, 9, (n, 2), dtype=torch.int32, device=DEV)
+        e[7, 1], e[n - 1, 0] = 9, -5
+        offsets, place = torch.empty(10, dtype=torch.int32, device=DEV), torch.empty(n, 2, dtype=torch.int32, device=DEV)
+        o.sp_route_order(e, offsets, place)
+        with pytest.raises(binding.SneakPeekError):
+            o.sp_ops_check()
+        e[7, 1], e[n - 1, 0] = -1, -1
+        want_o, want_p = places_by_definition(e, 9)
+        assert np.array_equal(offsets.cpu().numpy(), want_o) and np.array_equal(place.cpu().numpy(), want_p)
+    o.close()
+
+
+# ---------------------------------------------------------------- moving rows
+
+MOVE_SIZES = [(1, 1, 1, 1), (1, 512, 8, 8), (3, 5, 2, 4), (130, 8, 1, 5), (33, 100, 4, 40), (9, 257, 3, 9), (17, 512, 8, 64), (6, 1000, 32, 1024), (5, 1027, 6, 7),
+              (4, 2048, 2, 3), (3, 4099, 5, 5), (2, 16384, 2, 2), (5000, 24, 2, 16)]
+
+
+def make_places(torch, rng, n, top, experts, dropped):
+    e = np.argsort(rng.random((n, experts)), axis=1)[:, :top].astype(np.int32) if n * experts < 1 << 22 else \
+        rng.integers(0, experts, (n, top)).astype(np.int32)
+    e[rng.random(e.shape) < dropped] = -1
+    return torch.from_numpy(places_by_definition(torch.from_numpy(e), experts)[1].astype(np.int32)).to(DEV)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d,top,experts", MOVE_SIZES)
+def test_dispatch_and_combine(gpu, ops, n, d, top, experts, dtype):
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    rng = np.random.default_rng(n * 7 + d + top)
+    normal = lambda *s: torch.from_numpy(rng.standard_normal(s)).to(t)
+    for layout, other, dropped in (("plain", "odd", 0.0), ("odd", "apart", 0.3), ("apart", "plain", 1.0)):
+        place = make_places(torch, rng, n, top, experts, dropped)
+        here, at, rows = place >= 0, place.clamp(min=0).long(), n * top
+        x = in_layout(torch, normal(n, d), layout)
+        xs = in_layout(torch, torch.full((rows, d), 5.0, dtype=t), other)
+        ops.sp_dispatch(x, place, xs)
+        want = torch.full((rows, d), 5.0, dtype=t, device=DEV)       # rows behind the last one stay as they are
+        want[at[here]] = x[:, None, :].expand(n, top, d)[here]
+        assert torch.equal(xs, want)
+
+        ys = in_layout(torch, normal(rows, d), other)
+        weight = torch.from_numpy(rng.standard_normal((n, top))).float().to(DEV)
+        held = torch.where(here[:, :, None], ys[at].double(), 0.0)
+        for w in (weight, None):
+            for r in (None, in_layout(torch, normal(n, d), layout)):
+                y = in_layout(torch, torch.full((n, d), math.nan, dtype=t), layout)
+                ops.sp_combine(ys, place, y, weight=w, residual=r)
+                parts = held if w is None else held * w.double()[:, :, None]
+                want = parts.sum(1) + (0.0 if r is None else r.double())
+                bound = (top + 2) * U * (parts.abs().sum(1) + (0.0 if r is None else r.double().abs()))
+                bound = bound + half_step(torch, t) * (want.abs() + bound) + 1e-38
+                assert_within(torch, y, want, bound, "y")
+
+        dy = in_layout(torch, normal(n, d), layout)
+        for w in (weight, None):
+            dys = in_layout(torch, torch.full((rows, d), 5.0, dtype=t), other)
+            dweight = torch.full((n, top), math.nan, device=DEV)
+            ops.sp_combine_backward(dy, ys, place, w, dys=dys, dweight=dweight)
+            full = (dy.float()[:, None, :] * (1.0 if w is None else w[:, :, None])).expand(n, top, d).to(t)
+            want = torch.full((rows, d), 5.0, dtype=t, device=DEV)
+            want[at[here]] = full[here]                             # one product, rounded once (or twice: to float32 and on)
+            assert torch.equal(dys, want)
+            products = held * dy.double()[:, None, :]
+            assert_within(torch, dweight, products.sum(2), (d + 8) * U * products.abs().sum(2) + 1e-38, "dweight")
+            only = torch.full((n, top), math.nan, device=DEV)
+            ops.sp_combine_backward(dy, ys, place, w, dweight=only)
+            assert torch.equal(only, dweight)
+            alone = in_layout(torch, torch.full((rows, d), 5.0, dtype=t), other)
+            ops.sp_combine_backward(dy, None, place, w, dys=alone)
+            assert torch.equal(alone, dys)
+            # the gradient in the rows' own place
+            own = in_layout(torch, ys.clone(), layout)
+            only.fill_(math.nan)
+            ops.sp_combine_backward(dy, own, place, w, dys=own, dweight=only)
+            assert torch.equal(own[at[here]], dys[at[here]]) and torch.equal(only, dweight)
+
+
+def test_combine_in_place_of_the_residual_and_of_numbers_that_are_none(gpu, ops):
+    torch, _ = gpu
+    place = torch.tensor([[0, 2], [1, -1], [-1, -1]], dtype=torch.int32, device=DEV)
+    ys = torch.randn(6, 40, device=DEV)
+    ys[3:] = math.nan                                      # rows that nobody names
+    ys[1, 7] = INF
+    r = torch.randn(3, 40, device=DEV)
+    w = torch.rand(3, 2, device=DEV)
+    w[1, 1], w[2] = math.nan, math.nan                     # weights of pairs without a place
+    y, same = torch.empty_like(r), r.clone()
+    ops.sp_combine(ys, place, y, weight=w, residual=r)
+    ops.sp_combine(ys, place, same, weight=w, residual=same)
+    assert torch.equal(y, same) and torch.equal(y[2], r[2])
+    assert bool(torch.isinf(y[1, 7])) and int(torch.isfinite(y).sum()) == 3 * 40 - 1
+
+
+def test_places_that_are_no_rows_are_reported(gpu):
+    torch, binding = gpu
+    o = binding.Ops()
+    x, xs = torch.randn(5, 33, device=DEV), torch.zeros(8, 33, device=DEV)
+    for value in (8, 9, -2, 2 ** 31 - 1, -2 ** 31):
+        place = torch.tensor([[0, 1], [2, 3], [4, value], [5, -1], [6, 7]], dtype=torch.int32, device=DEV)
+        fine = torch.where((place < 0) | (place > 7), -1, place)
+        for call in (lambda p, out: o.sp_dispatch(x, p, out), lambda p, out: o.sp_combine(xs, p, out[:5]),
+                     lambda p, out: o.sp_combine_backward(x, xs, p, dys=out)):
+            a, b = torch.zeros(8, 33, device=DEV), torch.zeros(8, 33, device=DEV)
+            call(place, a)
+            with pytest.raises(binding.SneakPeekError):
+                o.sp_ops_check()
+            call(fine, b)
+            o.sp_ops_check()
+            assert torch.equal(a, b)
+    # no rows at all
+    none = torch.full((5, 2), -1, dtype=torch.int32, device=DEV)
+    o.sp_dispatch(x, none, torch.empty(0, 33, device=DEV))
+    y = torch.full((5, 33), math.nan, device=DEV)
+    o.sp_combine(torch.empty(0, 33, device=DEV), none, y)
+    assert bool((y == 0).all())
+    o.sp_ops_check()
+    o.close()
+
+
+def test_rows_beyond_32_bits_of_elements(gpu, ops):
+    torch, _ = gpu
+    n, d, far = 3000, 40, 1500000                          # 4.5e9 elements of bfloat16 from the first row to the last
+    big = torch.empty(n * far, dtype=torch.bfloat16, device=DEV)
+    rows = big.view(n, far)[:, :d]
+    x = torch.randn(n, d, device=DEV).bfloat16()
+    place = torch.randperm(n, device=DEV).int()[:, None].contiguous()
+    ops.sp_dispatch(x, place, rows)
+    y = torch.empty_like(x)
+    ops.sp_combine(rows, place, y)
+    assert torch.equal(x, y)
+    drop = torch.empty_like(x)
+    ops.sp_dropout(rows, drop, 0.0, 1)
+    assert torch.equal(drop, rows)
+    q, scale = torch.empty(n, d, dtype=torch.int8, device=DEV), torch.empty(n, device=DEV)
+    ops.sp_quantize_rows(rows, q, scale)
+    q2, scale2 = torch.empty_like(q), torch.empty_like(scale)
+    ops.sp_quantize_rows(rows.contiguous(), q2, scale2)
+    assert torch.equal(q, q2) and torch.equal(scale, scale2)
+    del big, rows
+    torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------- dropout
+
+def philox(counter, key):
+    """Philox 4x32 with ten rounds in plain whole numbers."""
+    c, k = list(counter), list(key)
+    for _ in range(10):
+        a, b = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
+        c = [(b >> 32) ^ c[1] ^ k[0], b & 0xFFFFFFFF, (a >> 32) ^ c[3] ^ k[1], a & 0xFFFFFFFF]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c
+
+
+def kept_by_definition(torch, n, d, p, seed, offset):
+    drop = round(p * 65536)
+    out = np.zeros((n, d), dtype=bool)
+    for i in range(n):
+        for piece in range((d + 7) // 8):
+            words = philox((piece, i, offset & 0xFFFFFFFF, offset >> 32), (seed & 0xFFFFFFFF, seed >> 32))
+            for j in range(min(8, d - 8 * piece)):
+                out[i, 8 * piece + j] = (words[j // 2] >> 16 * (j % 2) & 0xFFFF) >= drop
+    return torch.from_numpy(out).to(DEV)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d", [(1, 1), (1, 8), (3, 7), (2, 9), (5, 33), (17, 64), (3, 129), (130, 24), (2, 1000), (1, 4099)])
+def test_dropout(gpu, ops, n, d, dtype):
+    torch, _ = gpu
+    # the published numbers of counter and key 0, all ones
+    assert philox((0,) * 4, (0,) * 2) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
+    assert philox((0xFFFFFFFF,) * 4, (0xFFFFFFFF,) * 2) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
+    t = dtype_of(torch, dtype)
+    rng = np.random.default_rng(n + d)
+    for layout, p, seed, offset, with_r in (("plain", 0.1, 0, 0, False), ("odd", 0.5, 2 ** 64 - 1, 7, True), ("apart", 0.25, 2 ** 40 + 9, 2 ** 64 - 1, True)):
+        x = in_layout(torch, torch.from_numpy(rng.standard_normal((n, d))).to(t), layout)
+        r = in_layout(torch, torch.from_numpy(rng.standard_normal((n, d))).to(t), layout) if with_r else None
+        y = in_layout(torch, torch.full((n, d), math.nan, dtype=t), layout)
+        ops.sp_dropout(x, y, p, seed, offset=offset, residual=r)
+        kept = kept_by_definition(torch, n, d, p, seed, offset)
+        drop = round(p * 65536) / 65536
+        part = torch.where(kept, x.double() / (1 - drop), 0.0)
+        want = part + (0.0 if r is None else r.double())
+        bound = 2 * U * part.abs() + U * want.abs()
+        bound = bound + half_step(torch, t) * (want.abs() + bound)
+        assert_within(torch, y, want, bound, "y")
+        # what is dropped is exactly the residual, whatever x is there; the same elements in the backward call and in place
+        x2 = torch.where(kept, x, math.nan).to(t)
+        y2 = torch.empty_like(x2)
+        ops.sp_dropout(x2, y2, p, seed, offset=offset, residual=r)
+        assert torch.equal(y2, y)
+        same = x.clone()
+        ops.sp_dropout(same, same, p, seed, offset=offset, residual=r)
+        assert torch.equal(same, y)
+        if r is not None:
+            same = r.clone()
+            ops.sp_dropout(x, same, p, seed, offset=offset, residual=same)
+            assert torch.equal(same, y)
+
+
+def test_dropout_at_the_ends_and_on_average(gpu, ops):
+    torch, _ = gpu
+    x = torch.randn(300, 77, device=DEV)
+    y = torch.full_like(x, math.nan)
+    ops.sp_dropout(x, y, 0.0, 5)
+    assert torch.equal(x, y)
+    ops.sp_dropout(x, y, 1.0, 5)
+    assert bool((y == 0).all())
+    one = torch.ones(2048, 1024, device=DEV)
+    out = torch.empty_like(one)
+    total = one.numel()
+    for p, steps in ((1e-9, 1), (0.1, 6554), (0.5, 32768), (0.9, 58982), (1 - 1e-7, 65535)):
+        ops.sp_dropout(one, out, p, 11)
+        share = float((out == 0).sum()) / total
+        want = steps / 65536
+        assert abs(share - want) < 6 * math.sqrt(want * (1 - want) / total)       # six standard deviations
+        # the scale is that of the probability as it is taken: 1 / (1 - p), rounded once
+        assert float(out.max()) == float(torch.tensor(65536.0 / (65536 - steps)))
+    # neighbours, rows, seeds and offsets do not go together
+    ops.sp_dropout(one, out, 0.5, 11)
+    a = (out > 0).float() - 0.5
+    others = [a.roll(s, 1) for s in (1, 2, 7, 8)] + [a.roll(1, 0)]
+    for kw in (dict(seed=12), dict(seed=11, offset=1), dict(seed=11 + 2 ** 32), dict(seed=11, offset=2 ** 32)):
+        ops.sp_dropout(one, out, 0.5, **kw)
+        others.append((out > 0).float() - 0.5)
+    for b in others:
+        assert abs(float((a * b).sum())) < 6 * 0.25 * math.sqrt(total)
+
+
+def test_dropout_in_a_graph_takes_the_step(gpu, ops):
+    torch, _ = gpu
+    x = torch.randn(64, 200, device=DEV)
+    y, step = torch.empty_like(x), torch.zeros(1, dtype=torch.int64, device=DEV)
+    ops.sp_dropout(x, y, 0.3, 9, offset=100, step=step)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            ops.sp_dropout(x, y, 0.3, 9, offset=100, step=step)
+            step.add_(1)
+    step.zero_()
+    for turn in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = torch.empty_like(x)
+        ops.sp_dropout(x, want, 0.3, 9, offset=100 + turn)
+        assert torch.equal(y, want)
+    step.fill_(-100)
+    ops.sp_dropout(x, y, 0.3, 9, offset=100, step=step)
+    ops.sp_dropout(x, want, 0.3, 9)
+    assert torch.equal(y, want)
+
+
+# ---------------------------------------------------------------- 8 bits
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d", [(1, 1), (1, 512), (3, 5), (130, 16), (5, 33), (17, 100), (9, 257), (33, 770), (4, 1024), (3, 1030), (2, 2048), (2, 5000), (2, 16384),
+                                 (2, 40000), (2100, 64)])
+def test_quantize_rows(gpu, ops, n, d, dtype):
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    rng = np.random.default_rng(n + d)
+    for layout, size in (("plain", 1.0), ("odd", 1e-30), ("apart", 1e30)):
+        x = torch.from_numpy(rng.standard_normal((n, d)) * size).to(t)
+        if n > 1:
+            x[1] = 0.0
+        if n > 4:
+            x[2, d // 2], x[3, 0], x[4, d - 1] = math.nan, INF, -INF
+        high = x.float().abs().amax(1, keepdim=True)
+        finite = torch.isfinite(high) & ~torch.isnan(high)
+        # float32 as the definition has it, on the host; a quotient of two tensors, since a number over a tensor is rounded twice
+        most = torch.full_like(high, 127.0)
+        want_q = torch.where(finite & (high > 0), torch.round(x.float() * (most / high)), 0.0).nan_to_num(0.0).to(torch.int8)
+        want_s = torch.where(finite, high / most, math.nan)[:, 0]
+        q = in_layout(torch, torch.full((n, d), 99, dtype=torch.int8), ("odd", "apart", "plain")[layout == "odd"])
+        scale = torch.full((n,), -1.0, device=DEV)
+        ops.sp_quantize_rows(in_layout(torch, x, layout), q, scale)
+        assert torch.equal(q.cpu(), want_q)
+        assert torch.equal(scale.cpu().nan_to_num(-2.0), want_s.nan_to_num(-2.0))
+
+
+def test_quantize_rows_of_the_smallest_numbers(gpu, ops):
+    torch, _ = gpu
+    x = torch.tensor([[2.0 ** -149, 0.0, -2.0 ** -149], [2.0 ** -126, 2.0 ** -127, -2.0 ** -128], [1e-38, 5e-39, -1e-38], [3e38, -3e38, 1e38]], device=DEV)
+    q, scale = torch.empty(4, 3, dtype=torch.int8, device=DEV), torch.empty(4, device=DEV)
+    ops.sp_quantize_rows(x, q, scale)
+    assert q.tolist() == [[127, 0, -127], [127, 64, -32], [127, 64, -127], [127, -127, 42]]       # (63.5 goes to the even 64)
+    assert bool(torch.isfinite(scale).all())
+
+
+QUANTIZED_SIZES = [(1, 512, 256, 8), (1, 1, 1, 1), (2, 16, 3, 1), (5, 31, 33, 3), (24, 100, 64, 5), (130, 64, 128, 1), (257, 33, 200, 4), (300, 770, 515, 7), (700, 128, 96, 3),
+                   (1000, 1024, 256, 2), (4100, 96, 130, 40), (3000, 257, 129, 16), (64, 4100, 70, 2), (40000, 64, 64, 3), (33000, 256, 256, 5)]
+
+
+def quantized_layer(torch, x, xs, offsets, w, ws, bias, relu, residual):
+    """The definition in 64 bits, and a bound of the error: the sum is a whole number, rounded when it becomes a float32; two products and the
+    sums with bias and residual."""
+    n, m = x.shape[0], w.shape[1]
+    y = torch.zeros(n, m, dtype=torch.float64, device=DEV)
+    bound = torch.zeros_like(y)
+    ends = offsets.tolist()
+    for g in range(w.shape[0]):
+        lo, hi = ends[g], ends[g + 1]
+        if lo == hi:
+            continue
+        z = (x[lo:hi].double() @ w[g].double().t().contiguous()) * xs[lo:hi, None].double() * ws[g].double()
+        b = 3 * U * z.abs() + 1e-37
+        if bias is not None:
+            z = z + bias[g].double()
+            b = b + U * z.abs()
+        if relu:
+            z = torch.where(z < 0, 0.0, z)
+        if residual is not None:
+            z = z + residual[lo:hi].double()
+            b = b + U * z.abs()
+        y[lo:hi], bound[lo:hi] = z, b * 1.001
+    return y, bound
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("n,k,m,groups", QUANTIZED_SIZES)
+def test_grouped_linear_quantized(gpu, ops, n, k, m, groups, out):
+    torch, _ = gpu
+    t = dtype_of(torch, out)
+    rng = np.random.default_rng(n + k + m)
+    for turn, (layout, relu, biased, with_r) in enumerate((("plain", False, True, False), ("odd", True, False, True), ("apart", True, True, False))):
+        cuts = np.sort(rng.integers(0, n + 1, groups - 1)) if turn else np.full(groups - 1, n)      # all rows of one, then any shares
+        ends = np.concatenate([[0], cuts, [n if turn < 2 else n - n // 3]])                        # rows of no group at the end
+        offsets = torch.from_numpy(np.minimum(ends, ends[-1]).astype(np.int32)).to(DEV)
+        x = in_layout(torch, torch.from_numpy(rng.integers(-127, 128, (n, k)).astype(np.int8)), layout)
+        w = torch.from_numpy(rng.integers(-127, 128, (groups, m, k)).astype(np.int8)).to(DEV)
+        xs, ws = (torch.from_numpy(rng.random(s) + 0.01).float().to(DEV) for s in ((n,), (groups, m)))
+        bias = torch.from_numpy(rng.standard_normal((groups, m)) * 1000).float().to(DEV) if biased else None
+        r = in_layout(torch, torch.from_numpy(rng.standard_normal((n, m)) * 1000).to(t), layout) if with_r else None
+        y = in_layout(torch, torch.full((n, m), math.nan, dtype=t), layout)
+        ops.sp_grouped_linear_quantized(x, xs, offsets, w, ws, y, bias=bias, relu=relu, residual=r)
+        want, bound = quantized_layer(torch, x, xs, offsets, w, ws, bias, relu, r)
+        assert_within(torch, y, want, bound + half_step(torch, t) * (want.abs() + bound), ("y", turn))
+        if r is not None:
+            ops.sp_grouped_linear_quantized(x, xs, offsets, w, ws, r, bias=bias, relu=relu, residual=r)
+            assert torch.equal(r, y)
+    ops.sp_ops_check()
+
+
+def test_grouped_linear_quantized_of_the_longest_sums(gpu, ops):
+    torch, _ = gpu
+    k = 131071
+    x = torch.full((3, k), -128, dtype=torch.int8, device=DEV)
+    w = torch.full((1, 2, k), -128, dtype=torch.int8, device=DEV)
+    w[0, 1] = 127
+    one, y = torch.ones(3, device=DEV), torch.empty(3, 2, device=DEV)
+    offsets = torch.tensor([0, 3], dtype=torch.int32, device=DEV)
+    ops.sp_grouped_linear_quantized(x, one, offsets, w, torch.ones(1, 2, device=DEV), y)
+    want = torch.tensor([16384.0 * k, -128.0 * 127 * k], dtype=torch.float64).float()
+    assert torch.equal(y.cpu(), want.expand(3, 2))
+
+
+def test_grouped_linear_quantized_keeps_no_number_to_its_row(gpu, ops):
+    torch, _ = gpu
+    for n in (6, 600):
+        x = torch.randn(n, 96, device=DEV)
+        x[2, 5] = math.nan
+        q, scale = torch.empty(n, 96, dtype=torch.int8, device=DEV), torch.empty(n, device=DEV)
+        ops.sp_quantize_rows(x, q, scale)
+        w = torch.randint(-127, 128, (2, 70, 96), dtype=torch.int8, device=DEV)
+        offsets = torch.tensor([0, n // 2, n], dtype=torch.int32, device=DEV)
+        y = torch.empty(n, 70, device=DEV)
+        ops.sp_grouped_linear_quantized(q, scale, offsets, w, torch.rand(2, 70, device=DEV), y, relu=True)
+        assert bool(torch.isnan(y[2]).all()) and int(torch.isnan(y).sum()) == 70
+
+
+def test_grouped_linear_quantized_reports_bad_offsets(gpu):
+    torch, binding = gpu
+    o = binding.Ops()
+    for n in (6, 900):
+        x, w = torch.ones(n, 32, dtype=torch.int8, device=DEV), torch.ones(3, 8, 32, dtype=torch.int8, device=DEV)
+        y = torch.empty(n, 8, device=DEV)
+        for bad in ([0, 4, 2, n], [1, 2, 3, 4], [0, 1, 2, n + 1], [0, -1, 2, 3]):
+            o.sp_grouped_linear_quantized(x, torch.ones(n, device=DEV), torch.tensor(bad, dtype=torch.int32, device=DEV), w, torch.ones(3, 8, device=DEV), y)
+            with pytest.raises(binding.SneakPeekError):
+                o.sp_ops_check()
+    o.close()
+
+
+# ---------------------------------------------------------------- all of them together
+
+def test_a_layer_of_experts_and_its_gradients(gpu, ops):
+    """y = x + sum over the chosen experts of w_e dropout(relu(x W1_e)) W2_e, the router's logits x R, forward and backward, against the same
+    in 64 bits with the experts that were chosen."""
+    torch, _ = gpu
+    n, d, hidden, experts, top, p = 500, 48, 64, 12, 3, 0.25
+    g = torch.Generator().manual_seed(0)
+    make = lambda *s, scale=1.0: (torch.randn(*s, generator=g) * scale).to(DEV)
+    empty = lambda *s, t=torch.float32: torch.full(s, 0, dtype=t, device=DEV)
+    for sigmoid in (False, True):
+        x, router = make(n, d), make(1, d, experts, scale=d ** -0.5)
+        w1, w2 = make(experts, d, hidden, scale=d ** -0.5), make(experts, hidden, d, scale=hidden ** -0.5)
+        bias, dy = make(experts, scale=0.05), make(n, d)
+        all_rows = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+        z, expert, weight = empty(n, experts), empty(n, top, t=torch.int32), empty(n, top)
+        offsets, place = empty(experts + 1, t=torch.int32), empty(n, top, t=torch.int32)
+        xs, h, hd, ys, y = empty(n * top, d), empty(n * top, hidden), empty(n * top, hidden), empty(n * top, d), empty(n, d)
+        kw = dict(sigmoid=sigmoid, scale=1.5)
+
+        def forward():
+            ops.sp_grouped_linear(x, all_rows, router, z)
+            ops.sp_route(z, expert, weight, bias=bias, groups=4, top_groups=3, **kw)
+            ops.sp_route_order(expert, offsets, place)
+            ops.sp_dispatch(x, place, xs)
+            ops.sp_grouped_linear(xs, offsets, w1, h, relu=True)
+            ops.sp_dropout(h, hd, p, 77)
+            ops.sp_grouped_linear(hd, offsets, w2, ys)
+            ops.sp_combine(ys, place, y, weight=weight, residual=x)
+
+        dys, dweight, dhd, dh, dxs, dx = empty(n * top, d), empty(n, top), empty(n * top, hidden), empty(n * top, hidden), empty(n * top, d), empty(n, d)
+        dz, dw1, dw2, drouter, dxr = empty(n, experts), empty(*w1.shape), empty(*w2.shape), empty(*router.shape), empty(n, d)
+
+        def backward():
+            ops.sp_combine_backward(dy, ys, place, weight, dys=dys, dweight=dweight)
+            ops.sp_grouped_linear_backward(dys, hd, offsets, w2, dx=dhd, dw=dw2)
+            ops.sp_dropout(dhd, dh, p, 77)
+            ops.sp_grouped_linear_backward(dh, xs, offsets, w1, act=h, dx=dxs, dw=dw1)
+            ops.sp_combine(dxs, place, dx, residual=dy)
+            ops.sp_route_backward(z, expert, dweight, dz, **kw)
+            ops.sp_grouped_linear_backward(dz, x, all_rows, router, dx=dxr, dw=drouter)
+
+        forward()
+        backward()
+        ops.sp_ops_check()
+
+        kept = kept_by_definition(torch, n * top, hidden, p, 77, 0).cpu()
+        xd, rd, w1d, w2d = (v.double().cpu().requires_grad_() for v in (x, router, w1, w2))
+        zd = xd @ rd[0]
+        at, pl = expert.cpu().long(), place.cpu().long()
+        assert int(at.min()) >= 0
+        s = torch.sigmoid(zd) if sigmoid else torch.softmax(zd, 1)
+        sc = s.gather(1, at)
+        wd = sc / sc.sum(1, keepdim=True) * 1.5
+        hid = torch.relu(torch.einsum("nd,njdh->njh", xd, w1d[at])) * kept[pl] / 0.75
+        out = xd + (wd[:, :, None] * torch.einsum("njh,njhd->njd", hid, w2d[at])).sum(1)
+        out.backward(dy.double().cpu())
+        # a chain of sums of at most 64 products, 4 of them one behind the other, and sums over the rows of an expert: 1e-5 of the values' size is 60
+        # times what such roundings add up to at random, and far below any part left out
+        for got, want, what in ((y, out.detach(), "y"), (weight, wd.detach(), "weight"), (dx + dxr, xd.grad, "dx"), (dw1, w1d.grad, "dw1"),
+                                (dw2, w2d.grad, "dw2"), (drouter, rd.grad, "drouter")):
+            assert float((got.double().cpu() - want).norm() / want.norm()) < 1e-5, what
+
+        # the same in a captured graph, several times, with other rows each time and eager calls between
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        own = gpu[1].Ops()
+        ops_before, ops = ops, own
+        forward(); backward()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graph, stream=side):
+                forward()
+                backward()
+        results = (y, expert, weight, offsets, place, dx, dxr, dw1, dw2, drouter)
+        for turn in range(3):
+            x.copy_(make(n, d))
+            graph.replay()
+            torch.cuda.synchronize()
+            kept_results = [v.clone() for v in results]
+            forward(); backward()
+            torch.cuda.synchronize()
+            for a, b in zip(results, kept_results):
+                assert torch.equal(a, b)
+        own.sp_ops_check()
+        own.close()
+        ops = ops_before
+
+
+def test_serving_in_8_bits_next_to_32(gpu, ops):
+    """A layer rounded to 8 bits: what it computes differs from the layer in 32 bits by no more than the roundings allow."""
+    torch, _ = gpu
+    n, k, m, groups = 300, 200, 90, 4
+    x, w = torch.randn(n, k, device=DEV), torch.randn(groups, k, m, device=DEV) * k ** -0.5
+    offsets = torch.tensor([0, 100, 100, 250, n], dtype=torch.int32, device=DEV)
+    rows = w.transpose(1, 2).reshape(groups * m, k).contiguous()
+    wq, ws = torch.empty(groups * m, k, dtype=torch.int8, device=DEV), torch.empty(groups * m, device=DEV)
+    ops.sp_quantize_rows(rows, wq, ws)
+    q, scale = torch.empty(n, k, dtype=torch.int8, device=DEV), torch.empty(n, device=DEV)
+    y, full = torch.empty(n, m, device=DEV), torch.empty(n, m, device=DEV)
+    ops.sp_quantize_rows(x, q, scale)
+    ops.sp_grouped_linear_quantized(q, scale, offsets, wq.view(groups, m, k), ws.view(groups, m), y)
+    ops.sp_grouped_linear(x, offsets, w, full)
+    # every factor is off by at most half a step, scale / 2 and a little
+    ends = offsets.tolist()
+    for g in range(groups):
+        lo, hi = ends[g], ends[g + 1]
+        xa, wa = x[lo:hi].double().abs(), w[g].double().abs()
+        hx, hw = scale[lo:hi, None].double() * 0.5001, ws.view(groups, m)[g].double() * 0.5001
+        bound = hx * wa.sum(0) + xa.sum(1, keepdim=True) * hw + k * hx * hw + 1e-4
+        assert_within(torch, y[lo:hi], full[lo:hi].double(), bound, g)
+
+
+def test_calls_on_another_stream(gpu, ops):
+    torch, _ = gpu
+    side = torch.cuda.Stream()
+    z = torch.randn(3000, 64, device=DEV)
+    a, wa = run_route(torch, ops, z, 4)
+    torch.cuda.synchronize()
+    b, wb = torch.empty_like(a), torch.empty_like(wa)
+    offsets, place = torch.empty(65, dtype=torch.int32, device=DEV), torch.empty_like(a)
+    ops.sp_route(z, b, wb, stream=side)
+    ops.sp_route_order(b, offsets, place, stream=side)
+    side.synchronize()
+    assert torch.equal(a, b) and torch.equal(wa, wb)
+    want_o, want_p = places_by_definition(a, 64)
+    assert np.array_equal(offsets.cpu().numpy(), want_o) and np.array_equal(place.cpu().numpy(), want_p)
