@@ -251,20 +251,38 @@ sp_status sp_grouped_linear_quantized(sp_ops* o, int32_t n, int32_t k, int32_t m
   if (n > 0 && (!x || !x_scale || !offsets || !w || !w_scale || !y)) return SP_EINVAL;
   if (!aligned(y, out_dtype) || !aligned(residual, out_dtype) || !aligned4(x_scale) || !aligned4(offsets) || !aligned4(w_scale) || !aligned4(bias))
     return SP_EINVAL;
-  if (groups > SP_MAX_APPS || k > SP_MAX_QUANTIZED_INPUTS || m > SP_MAX_LINEAR_DIM) return SP_ECAPACITY;
+  if (groups > SP_MAX_APPS || k > SP_MAX_QUANTIZED_INPUTS || m > SP_MAX_LINEAR_DIM || x_stride > SP_MAX_LINEAR_STRIDE) return SP_ECAPACITY;
   if (n == 0) return SP_OK;
   QuantizedArgs a{};
   a.n = n; a.k = k; a.m = m; a.groups = groups; a.x = x; a.x_stride = x_stride; a.x_scale = x_scale; a.offsets = offsets; a.w = w;
   a.w_scale = w_scale; a.bias = bias; a.relu = activation == SP_ACT_RELU; a.residual = residual; a.residual_stride = residual_stride;
   a.y = y; a.y_stride = y_stride; a.err = o->err;
-  const int64_t row_tiles = std::min<int64_t>(((int64_t)n + 127) / 128 + groups, n), col_tiles = (m + 127) / 128;
-  const int64_t blocks = (row_tiles * col_tiles + kXcds - 1) / kXcds * kXcds;
-  if (blocks * 256 > UINT32_MAX) return SP_ECAPACITY;
-  a.row_tiles = (int)row_tiles;
-  a.col_tiles = (int)col_tiles;
+  // Pieces of 16 rows while the device holds about all of their workgroups and each is through its depth soon (256 rows, 1024 -> 1024: 7.2 us
+  // against 11.4 in tiles; 1024 rows, 1024 -> 512 11.1 against 10.5, 256 rows, 2048 -> 2048 20.9 against 16.0; addresses that are no multiples of 16 cost
+  // them more: 256 rows of 32 groups, 1023 -> 515 21.4 against 16.6).  Tiles of 256 by 256, one to a compute unit, where there are many long ones
+  // (262144 rows, 2048 -> 2048: 1240 us against 1523 in tiles of 128 by 128, 1024 -> 1024 368 against 401; 65536 rows, 1024 -> 1024 106 against 100,
+  // 262144 rows, 512 -> 512 136 against 126).  y past the caches: 262144 rows, 64 -> 1024 134 us, else 167.
+  const bool direct = (((uintptr_t)x | (uintptr_t)w | (uintptr_t)k | (uintptr_t)x_stride) & 15u) == 0;
+  auto grid = [&](int64_t bm, int64_t bn, int64_t threads) {         // false: more workgroups than a launch holds
+    const int64_t row_tiles = std::min<int64_t>((n + bm - 1) / bm + groups, n), col_tiles = (m + bn - 1) / bn;
+    if ((row_tiles * col_tiles + kXcds) * threads > UINT32_MAX) return false;
+    a.row_tiles = (int)row_tiles;
+    a.col_tiles = (int)col_tiles;
+    return true;
+  };
+  const int64_t few_tiles = (((int64_t)n + kFewQuantizedRows - 1) / kFewQuantizedRows + std::min(n, groups)) * ((m + kFewQuantizedCols - 1) / kFewQuantizedCols);
+  const bool few = few_tiles <= 2048 && few_tiles * k <= (direct ? 1 << 21 : 1 << 20);
+  const bool large = direct && k >= 1024 && ((int64_t)n + 255) / 256 * ((m + 255) / 256) >= 2048;
+  if (!(few ? grid(kFewQuantizedRows, kFewQuantizedCols, kFewQuantizedThreads) : large ? grid(256, 256, 512) : grid(128, 128, 256))) return SP_ECAPACITY;
+  const unsigned blocks = (unsigned)(((int64_t)a.row_tiles * a.col_tiles + kXcds - 1) / kXcds * kXcds);
+  a.past_caches = (int64_t)n * m * elem_bytes(out_dtype) > (int64_t)128 << 20;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
-  with_type(out_dtype, [&]<typename T>() { hipLaunchKernelGGL((k_quantized<T>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, a); });
+  with_type(out_dtype, [&]<typename T>() {
+    auto kernel = few ? k_quantized_few<T> : large ? k_quantized<T, 256, 256, 128, 2, true>
+                  : direct ? k_quantized<T, 128, 128, 64, 3, true> : k_quantized<T, 128, 128, 64, 2, false>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(few ? kFewQuantizedThreads : large ? 512 : 256), 0, (hipStream_t)stream, a);
+  });
   return launched(o);
 }
 

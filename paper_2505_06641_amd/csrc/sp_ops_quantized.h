@@ -4,6 +4,8 @@
 // Weights lie with an output's inputs next to each other, [groups, m, k], so that both sides' 16 consecutive inputs are what a lane of the matrix
 // cores takes.
 #pragma once
+#include <type_traits>
+
 #include "sp_common.h"
 #include "sp_ops_common.h"
 
@@ -113,6 +115,7 @@ struct QuantizedArgs {
   void* y;  int64_t y_stride;                    // [n, m]
   uint32_t* err;
   int row_tiles, col_tiles;
+  bool past_caches;                              // y is too long for the last-level cache: written past it
 };
 
 // Sixteen bytes of a row of `depth` from `t` on; what lies behind the row is 0 (CUT), or whatever is there.  left: bytes from p to the
@@ -140,83 +143,260 @@ __device__ __forceinline__ bytes16 load_bytes(const int8_t* p, int t, int depth,
   return q;
 }
 
-// A tile of 128 rows of one group by 128 columns, four wavefronts of 64 by 64, 128 bytes of the depth at a time through LDS.  Rows and columns
-// beyond the tile's last are that one again, and not written.
-template <typename TO>
-__global__ __launch_bounds__(256) void k_quantized(QuantizedArgs a) {
-  constexpr int BM = 128, BN = 128, D = 128;
-  __shared__ __align__(16) uint8_t lds[(BM + BN) * D];
+// A workgroup computes BM rows of one group by BN columns, wavefronts of 64 by BN / 2, D bytes of the depth at a time by way of LDS.  Rows and
+// columns beyond the tile's last are that one again, and not written.  LDS: [rows of both sides][D bytes], the 16-byte pieces of a row permuted
+// by the row, so that the eight rows that are read together lie in different banks.
+//   DIRECT: memory to LDS without registers, STAGES pieces of the depth in LDS, one of them being multiplied.  For depths, strides and addresses
+//     that are multiples of 16.
+//   else by way of registers, two stages in LDS and one on its way, which takes any address and cuts what lies behind the depth.
+template <int BM, int BN, int D, int STAGES, bool DIRECT>
+struct QuantizedTile {
+  static constexpr int WAVES = BM / 32, FR = 2, FC = BN / 64, kRows = BM + BN;
+  static constexpr int kAcross = D / 16, kRun = 64 / kAcross;         // pieces of a row, rows of a run
+  static constexpr int kChunks = kRows / kRun / WAVES, kOfX = BM / kRun / WAVES;   // a wavefront's runs, the first of them rows of x
+  static constexpr int kSums = WAVES * 32 * (BN / 2) * 4;             // 32 rows of every wavefront's
+  static constexpr int kBytes = STAGES * kRows * D > kSums ? STAGES * kRows * D : kSums;
+  static __device__ __forceinline__ int swap(int row) { return D == 128 ? row & 7 : row >> 1 & 3; }
+  static __device__ __forceinline__ int place(int row, int piece) { return row * D + ((piece ^ swap(row)) * 16); }
+};
+
+// Sixteen bytes for every lane from base + off to LDS: the wavefront's lanes one after the other from `to` on.  (In asm, since the compiler would wait
+// for all such loads before every read of LDS; there is no output that it could take for written.)
+__device__ __forceinline__ void load_to_lds(uint32_t to, const int8_t* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(base) : "memory");
+}
+// Eight results, which nobody reads before much else has gone through the caches.
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void store_past_caches(float* p, const float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 8; h += 4) {
+    const u32x4_at4 q = {__float_as_uint(v[h]), __float_as_uint(v[h + 1]), __float_as_uint(v[h + 2]), __float_as_uint(v[h + 3])};
+    __builtin_nontemporal_store(q, reinterpret_cast<u32x4_at4*>(p + h));
+  }
+}
+__device__ __forceinline__ void store_past_caches(bf16* p, const float (&v)[8]) {
+  u16x8_any q;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint16_t, (bf16)v[i]);
+  __builtin_nontemporal_store(q, reinterpret_cast<u16x8_any*>(p));
+}
+// Until at most N of the wavefront's loads are under way.
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+// All wavefronts have come here, and what they read from LDS before has arrived.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+template <typename TO, int BM, int BN, int D, int STAGES, bool DIRECT>
+__global__ __launch_bounds__(BM * 2, BM == 128 ? 3 : 2) void k_quantized(QuantizedArgs a) {
+  typedef QuantizedTile<BM, BN, D, STAGES, DIRECT> Tile;
+  constexpr int FR = Tile::FR, FC = Tile::FC, CH = Tile::kChunks, CX = Tile::kOfX, WAVES = Tile::WAVES, kStageBytes = Tile::kRows * D;
+  constexpr int WN = BN / 2;                                          // columns of a wavefront
+  __shared__ __align__(16) uint8_t lds[Tile::kBytes];
   if (blockIdx.x == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
   const int tile = xcd_tile(blockIdx.x, a.row_tiles * a.col_tiles);
   if (tile < 0) return;
   RowTile rows;
   const int rt = tile / a.col_tiles, c0 = (tile % a.col_tiles) * BN;
   if (!find_row_tile(a.offsets, a.groups, a.n, BM, rt, &rows)) return;
-  const bool in = rows.g < a.groups;
-  const int depth = in ? a.k : 0, g = min(rows.g, a.groups - 1), last_row = rows.hi - 1, last_col = a.m - 1;
-  const int8_t* w = a.w + (int64_t)g * a.m * a.k;
-  const int64_t x_end = (int64_t)(a.n - 1) * a.x_stride + a.k, w_end = (int64_t)(a.groups - g) * a.m * a.k;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / 2 * 64, wc = wave % 2 * 64;
-  i32x16 acc[2][2] = {};
-  bytes16 raw[2][4];
-  auto load = [&](int t0) {
+  const int depth = a.k, g = min(rows.g, a.groups - 1), n_rows = rows.hi - rows.lo, n_cols = min(BN, a.m - c0);
+  const int stages = (depth + D - 1) / D;
+  const int8_t* x = a.x + (int64_t)rows.lo * a.x_stride;
+  const int8_t* w = a.w + ((int64_t)g * a.m + c0) * a.k;
+  if (rows.g == a.groups) {                                           // rows of no group
+    for (int i = threadIdx.x; i < n_rows * n_cols; i += BM * 2) ((TO*)a.y)[(int64_t)(rows.lo + i / n_cols) * a.y_stride + c0 + i % n_cols] = from_float<TO>(0.f);
+    return;
+  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / 2 * 64, wc = wave % 2 * WN;
+  // what the sums are multiplied by, on its way while they are made: a lane's rows' scales, and those of the columns that it will write
+  constexpr int VO = 8, kAcross = WN / VO, kAtOnce = 64 / kAcross;    // columns of a lane, lanes of a row, rows at once
+  const int mine = (lane % kAcross) * VO, col = c0 + wc + mine, left = a.m - col;
+  float xs[FR], ws[VO], bias[VO] = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int p = threadIdx.x + i * 256, major = p / 8, t = t0 + p % 8 * 16;
-      const int64_t xo = (int64_t)min(rows.lo + major, last_row) * a.x_stride + t, wo = (int64_t)min(c0 + major, last_col) * a.k + t;
-      raw[0][i] = load_bytes<true>(a.x + xo, t, depth, x_end - xo);
-      raw[1][i] = load_bytes<false>(w + wo, t, depth, w_end - wo);
-    }
-  };
-  auto place = [](int major, int piece) { return major * D + ((piece ^ (major & 7)) * 16); };
-  if (depth > 0) load(0);
-  for (int t0 = 0; t0 < depth; t0 += D) {
+  for (int i = 0; i < FR; ++i) xs[i] = a.x_scale[rows.lo + min(wr + i * 32 + (lane & 31), n_rows - 1)];
+  load_some(a.w_scale + (int64_t)g * a.m + col, left, 0.f, ws);
+  if (a.bias) load_some(a.bias + (int64_t)g * a.m + col, left, 0.f, bias);
+
+  // a lane's piece of chunk i: which one of its row, and where from
+  int row_of[CH];
+  uint32_t off[CH];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int p = threadIdx.x + i * 256;
-        *reinterpret_cast<bytes16*>(lds + s * BM * D + place(p / 8, p % 8)) = raw[s][i];
-      }
-    __syncthreads();
-    if (t0 + D < depth) load(t0 + D);
+  for (int i = 0; i < CH; ++i) {
+    const int r = (wave + i * WAVES) * Tile::kRun + lane / Tile::kAcross;                     // rows of x, then columns
+    row_of[i] = r;
+    off[i] = i < CX ? (uint32_t)min(r, n_rows - 1) * (uint32_t)a.x_stride : (uint32_t)min(r - BM, n_cols - 1) * (uint32_t)a.k;
+  }
+  auto piece_of = [&](int i) { return (lane % Tile::kAcross) ^ Tile::swap(row_of[i]); };
+
+  i32x16 acc[FR][FC] = {};
+  auto multiply = [&](const uint8_t* at) {
 #pragma unroll
     for (int step = 0; step < D / 32; ++step) {
-      i32x4 fr[2], fc[2];
+      i32x4 fr[FR], fc[FC];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fr[i] = *reinterpret_cast<const i32x4*>(lds + place(wr + i * 32 + (lane & 31), step * 2 + (lane >> 5)));
-        fc[i] = *reinterpret_cast<const i32x4*>(lds + BM * D + place(wc + i * 32 + (lane & 31), step * 2 + (lane >> 5)));
-      }
+      for (int i = 0; i < FR; ++i) fr[i] = *reinterpret_cast<const i32x4*>(at + Tile::place(wr + i * 32 + (lane & 31), step * 2 + (lane >> 5)));
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < FC; ++j) fc[j] = *reinterpret_cast<const i32x4*>(at + Tile::place(BM + wc + j * 32 + (lane & 31), step * 2 + (lane >> 5)));
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fc[j], fr[i], acc[i][j], 0, 0, 0);
+      for (int i = 0; i < FR; ++i)
+#pragma unroll
+        for (int j = 0; j < FC; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fc[j], fr[i], acc[i][j], 0, 0, 0);
     }
-    __syncthreads();
-  }
-  // lane l has row l % 32, columns 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3
+  };
+
+  if constexpr (DIRECT) {
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    auto load = [&](int s) {                                          // stage s of the depth; pieces behind the depth read the last one
+      const int t0 = s * D, most = (depth - t0) / 16 - 1;
+      const uint32_t to = lds0 + s % STAGES * kStageBytes + wave * 1024;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int row = rows.lo + wr + i * 32 + (lane & 31);
-    if (row > last_row) continue;
-    const float xs = in ? a.x_scale[row] : 0.f;
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int col = c0 + wc + j * 32 + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
-        if (col > last_col) continue;
-        float v = 0.f;
-        if (in) {
-          v = (float)acc[i][j][e] * xs * a.w_scale[(int64_t)g * a.m + col];
-          if (a.bias) v += a.bias[(int64_t)g * a.m + col];
-          if (a.relu) v = v < 0.f ? 0.f : v;
-          if (a.residual) v += to_float(((const TO*)a.residual)[row * a.residual_stride + col]);
-        }
-        ((TO*)a.y)[row * a.y_stride + col] = from_float<TO>(v);
+      for (int i = 0; i < CH; ++i) {
+        const uint32_t from = off[i] + min(piece_of(i), most) * 16;
+        load_to_lds(to + i * WAVES * 1024, (i < CX ? x : w) + t0, from);
       }
+    };
+    constexpr int AHEAD = STAGES - 1;
+    for (int s = 0; s < AHEAD && s < stages; ++s) load(s);
+    for (int s = 0; s < stages; ++s) {
+      // this stage's loads have arrived (the next ones' may be under way), and nobody reads the stage before any more
+      if (s + AHEAD - 1 < stages) wait_loads<CH * (AHEAD - 1)>();
+      else if (AHEAD > 2 && s + 1 < stages) wait_loads<CH>();
+      else wait_loads<0>();
+      uint8_t* at = lds + s % STAGES * kStageBytes;
+      const int most = (depth - s * D) / 16;
+      if (most < Tile::kAcross) {                                                 // x behind the depth is 0
+#pragma unroll
+        for (int i = 0; i < CX; ++i)
+          if (piece_of(i) >= most) *reinterpret_cast<bytes16*>(at + Tile::place(row_of[i], piece_of(i))) = bytes16{0, 0, 0, 0};
+      }
+      meet();
+      if (s + AHEAD < stages) load(s + AHEAD);
+      multiply(at);
+    }
+  } else {
+    bytes16 raw[CH];
+    const int64_t x_end = (int64_t)(a.n - 1 - rows.lo) * a.x_stride + a.k, w_end = ((int64_t)(a.groups - g) * a.m - c0) * a.k;
+    auto load = [&](int s) {
+      if ((s + 1) * D <= depth) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) raw[i] = *reinterpret_cast<const bytes16_any*>((i < CX ? x : w) + s * D + (off[i] + piece_of(i) * 16));
+        return;
+      }
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int t = s * D + piece_of(i) * 16;
+        raw[i] = i < CX ? load_bytes<true>(x + off[i] + t, t, depth, x_end - off[i] - t) : load_bytes<false>(w + off[i] + t, t, depth, w_end - off[i] - t);
+      }
+    };
+    auto store = [&](int s) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) *reinterpret_cast<bytes16*>(lds + s % STAGES * kStageBytes + Tile::place(row_of[i], piece_of(i))) = raw[i];
+    };
+    if (stages > 0) {
+      load(0);
+      store(0);
+      if (stages > 1) load(1);
+    }
+    for (int s = 0; s < stages; ++s) {
+      __syncthreads();
+      if (s + 1 < stages) store(s + 1);
+      if (s + 2 < stages) load(s + 2);
+      multiply(lds + s % STAGES * kStageBytes);
+    }
   }
+
+  // Sums to memory by way of each wavefront's own part of LDS, 32 rows at a time, so that whole lines are written: lane l has row l % 32, of a block's
+  // columns 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3.  The 16-byte pieces of a row are permuted by the row.
+  float* stage = reinterpret_cast<float*>(lds) + wave * 32 * WN;
+  __syncthreads();
+  auto finish = [&](auto whole) {                                     // whole: all of the tile's rows and columns are there
+#pragma unroll
+    for (int i = 0; i < FR; ++i) {
+      const int r = lane & 31;
+#pragma unroll
+      for (int j = 0; j < FC; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4*>(stage + r * WN + (((j * 8 + 2 * q + (lane >> 5)) ^ (r % (WN / 4))) * 4)) =
+              f32x4{(float)acc[i][j][4 * q] * xs[i], (float)acc[i][j][4 * q + 1] * xs[i], (float)acc[i][j][4 * q + 2] * xs[i],
+                    (float)acc[i][j][4 * q + 3] * xs[i]};
+      wave_sync();
+#pragma unroll
+      for (int u = 0; u < 32 / kAtOnce; ++u) {
+        const int sr = u * kAtOnce + lane / kAcross, tr = wr + i * 32 + sr;
+        if (!whole && (tr >= n_rows || left <= 0)) continue;
+        const int64_t row = rows.lo + tr;
+        const int count = whole ? VO : left;
+        float v[VO], res[VO];
+        if (a.residual) load_some((const TO*)a.residual + row * a.residual_stride + col, count, 0.f, res);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 f = *reinterpret_cast<const f32x4*>(stage + sr * WN + (((mine / 4 + h) ^ (sr % (WN / 4))) * 4));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[4 * h + e] = f[e];
+        }
+#pragma unroll
+        for (int e = 0; e < VO; ++e) {
+          v[e] = v[e] * ws[e] + bias[e];
+          if (a.relu) v[e] = v[e] < 0.f ? 0.f : v[e];
+          if (a.residual) v[e] += res[e];
+        }
+        TO* out = (TO*)a.y + row * a.y_stride + col;
+        if (whole && a.past_caches) store_past_caches(out, v);
+        else store_some(out, count, v);
+      }
+      wave_sync();
+    }
+  };
+  if (n_rows == BM && n_cols == BN) finish(std::true_type{});
+  else finish(std::false_type{});
+}
+
+// Few rows: a request, a window of them, a small batch.  A workgroup takes 16 rows of one group and 16 columns, its wavefronts share out the
+// depth, 64 bytes at a time, straight from memory, and their sums meet in LDS.  Bound by trips to memory: offsets, weights and rows, the result.
+constexpr int kFewQuantizedRows = 16, kFewQuantizedCols = 16, kFewQuantizedThreads = 256;
+
+template <typename TO>
+__global__ __launch_bounds__(kFewQuantizedThreads) void k_quantized_few(QuantizedArgs a) {
+  constexpr int WAVES = kFewQuantizedThreads / 64;
+  __shared__ int32_t part[WAVES][16 * 17];
+  if (blockIdx.x == 0 && threadIdx.x < 64) check_offsets(a.offsets, a.groups, a.n, a.err);
+  const int tile = xcd_tile(blockIdx.x, a.row_tiles * a.col_tiles);
+  if (tile < 0) return;
+  const int rt = tile / a.col_tiles, c0 = (tile % a.col_tiles) * kFewQuantizedCols;
+  RowTile rows;
+  if (!find_row_tile(a.offsets, a.groups, a.n, kFewQuantizedRows, rt, &rows)) return;
+  const bool in = rows.g < a.groups;
+  const int n_rows = rows.hi - rows.lo, depth = in ? a.k : 0, g = min(rows.g, a.groups - 1);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = lane & 15, own = 16 * (lane >> 4);
+  const int64_t row_at = (int64_t)(rows.lo + min(mine, n_rows - 1)) * a.x_stride, x_end = (int64_t)(a.n - 1) * a.x_stride + a.k;
+  const int64_t col_at = ((int64_t)g * a.m + min(c0 + mine, a.m - 1)) * a.k, w_end = (int64_t)a.groups * a.m * a.k;
+  // what the sum is multiplied by
+  const int r = threadIdx.x / 16, col = c0 + threadIdx.x % 16;
+  const bool writes = r < n_rows && col < a.m;
+  const int64_t row = rows.lo + r, at = (int64_t)g * a.m + col;
+  float xs = 0.f, ws = 0.f, bias = 0.f, res = 0.f;
+  if (writes && in) {
+    xs = a.x_scale[row];
+    ws = a.w_scale[at];
+    if (a.bias) bias = a.bias[at];
+    if (a.residual) res = to_float(((const TO*)a.residual)[row * a.residual_stride + col]);
+  }
+  i32x4 acc = {0, 0, 0, 0};
+  for (int t0 = wave * 64; t0 < depth; t0 += WAVES * 64) {
+    const int t = t0 + own;
+    const bytes16 fr = load_bytes<true>(a.x + row_at + t, t, depth, x_end - row_at - t), fc = load_bytes<false>(a.w + col_at + t, t, depth, w_end - col_at - t);
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, fc), __builtin_bit_cast(i32x4, fr), acc, 0, 0, 0);
+  }
+  // lane l has row l % 16, columns 4 (l / 16) .. + 3
+#pragma unroll
+  for (int e = 0; e < 4; ++e) part[wave][mine * 17 + 4 * (lane >> 4) + e] = acc[e];
+  __syncthreads();
+  if (!writes) return;
+  int sum = 0;
+#pragma unroll
+  for (int q = 0; q < WAVES; ++q) sum += part[q][r * 17 + threadIdx.x % 16];
+  float v = in ? (float)sum * xs * ws + bias : 0.f;
+  if (a.relu) v = v < 0.f ? 0.f : v;
+  ((TO*)a.y)[row * a.y_stride + col] = from_float<TO>(v + res);
 }
 
 }  // namespace sp

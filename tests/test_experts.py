@@ -708,7 +708,8 @@ def test_quantize_rows_of_the_smallest_numbers(gpu, ops):
 
 
 QUANTIZED_SIZES = [(1, 512, 256, 8), (1, 1, 1, 1), (2, 16, 3, 1), (5, 31, 33, 3), (24, 100, 64, 5), (130, 64, 128, 1), (257, 33, 200, 4), (300, 770, 515, 7), (700, 128, 96, 3),
-                   (1000, 1024, 256, 2), (4100, 96, 130, 40), (3000, 257, 129, 16), (64, 4100, 70, 2), (40000, 64, 64, 3), (33000, 256, 256, 5)]
+                   (1000, 1024, 256, 2), (4100, 96, 130, 40), (3000, 257, 129, 16), (64, 4100, 70, 2), (40000, 64, 64, 3), (33000, 256, 256, 5), (20000, 272, 200, 3),
+                   (131100, 1040, 1030, 3)]
 
 
 def quantized_layer(torch, x, xs, offsets, w, ws, bias, relu, residual):
@@ -759,6 +760,7 @@ def test_grouped_linear_quantized(gpu, ops, n, k, m, groups, out):
             ops.sp_grouped_linear_quantized(x, xs, offsets, w, ws, r, bias=bias, relu=relu, residual=r)
             assert torch.equal(r, y)
     ops.sp_ops_check()
+    torch.cuda.empty_cache()
 
 
 def test_grouped_linear_quantized_of_the_longest_sums(gpu, ops):
