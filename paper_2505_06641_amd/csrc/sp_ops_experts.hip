@@ -55,11 +55,30 @@ sp_status sp_route(sp_ops* o, int32_t n, int32_t experts, int32_t top, int32_t d
   a.z = logits; a.z_stride = logits_stride; a.bias = bias; a.expert = expert; a.weight = weight; a.err = o->err;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
-  const int per = (a.width + a.group_lanes - 1) / a.group_lanes;
-  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)n + 3) / 4, 16384));
+  const int power = power_from(groups);
+  auto per_lane = [&](int team) { return (a.width + team / power - 1) / (team / power); };
+  // a wavefront to a row while the device holds about all of them at once: 2048 rows of 64 bfloat16 experts 4.0 us either way, 16384 rows 4.3 us in
+  // teams of 8 and 11.7 in wavefronts; 256 rows of 256 experts in groups 8.0 us and 5.8
+  const bool narrow = experts <= 256 && top <= 8 && groups <= 8 && per_lane(16) <= 16 && n > 2048;
+  const int team = !narrow ? 64 : per_lane(8) <= 16 ? 8 : 16, per = per_lane(team), rows = 4 * 64 / team;
+  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)n + rows - 1) / rows, 2048));
   with_type(dtype, [&]<typename T>() {
-    auto kernel = per <= 1 ? k_route<T, 1> : per <= 2 ? k_route<T, 2> : per <= 4 ? k_route<T, 4> : per <= 8 ? k_route<T, 8> : per <= 16 ? k_route<T, 16> : k_route<T, 32>;
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
+    auto kernel = [&]<bool BY_LOGIT>() {
+      return team == 16 ? k_route<T, 16, 16, BY_LOGIT>
+             : team == 8 ? (per <= 1   ? k_route<T, 8, 1, BY_LOGIT>
+                            : per <= 2 ? k_route<T, 8, 2, BY_LOGIT>
+                            : per <= 4 ? k_route<T, 8, 4, BY_LOGIT>
+                            : per <= 8 ? k_route<T, 8, 8, BY_LOGIT>
+                                       : k_route<T, 8, 16, BY_LOGIT>)
+                         : (per <= 1    ? k_route<T, 64, 1, BY_LOGIT>
+                            : per <= 2  ? k_route<T, 64, 2, BY_LOGIT>
+                            : per <= 4  ? k_route<T, 64, 4, BY_LOGIT>
+                            : per <= 8  ? k_route<T, 64, 8, BY_LOGIT>
+                            : per <= 16 ? k_route<T, 64, 16, BY_LOGIT>
+                                        : k_route<T, 64, 32, BY_LOGIT>);
+    };
+    hipLaunchKernelGGL((bias || groups > 1 ? kernel.template operator()<false>() : kernel.template operator()<true>()), grid, dim3(256), 0,
+                       (hipStream_t)stream, a);
   });
   return launched(o);
 }
@@ -101,16 +120,19 @@ sp_status sp_route_order(sp_ops* o, int32_t n, int32_t top, int32_t experts, con
   if (experts > SP_MAX_EXPERTS || top > SP_MAX_TOP || pairs > INT32_MAX) return SP_ECAPACITY;
   int bits = 0;
   while ((1 << bits) < experts) ++bits;
-  constexpr int64_t kOne = 16384, kMost = 128;               // pairs of a single tile; tiles
-  const int64_t tile = pairs <= kOne ? kOne : std::max(kOne, ((pairs + kMost - 1) / kMost + 1023) / 1024 * 1024);
+  // One launch whose workgroups each look through all pairs, up to 8192 of them (5.0 us against 6.1; 16388 pairs 6.5 against 6.4, 32768 9.7 against 7.0);
+  // else as many tiles as have 65536 counts together, up to one to every half of a compute unit (2097152 pairs of 256 experts: 64 tiles 41.6 us, 256
+  // 20.3, 512 29.3; 524288 of 1000: 64 tiles 20.4, 256 27.5; 8000000 of 128: 256 tiles 57.5, 512 46.9).
+  const int64_t most = std::clamp(65536 / experts, 64, 512);
+  const bool few = pairs <= 8192;
+  const int64_t tile = few ? 1024 : std::max<int64_t>(((pairs + most - 1) / most + 1023) / 1024 * 1024, 1024);
   const int tiles = (int)std::max<int64_t>(1, (pairs + tile - 1) / tile);
-  if (tiles > 1 && (int64_t)tiles * experts * 4 > o->ws_bytes) return SP_ECAPACITY;
-  int32_t* counts = tiles > 1 ? (int32_t*)o->ws : nullptr;
+  if (!few && (int64_t)tiles * experts * 4 > o->ws_bytes) return SP_ECAPACITY;
+  int32_t* counts = few ? nullptr : (int32_t*)o->ws;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
   hipStream_t s = (hipStream_t)stream;
-  if (tiles > 1)
-    hipLaunchKernelGGL(k_order_count, dim3(tiles), dim3(kOrderThreads), 0, s, pairs, (int)tile, experts, expert, counts, o->err);
+  if (!few) hipLaunchKernelGGL(k_order_count, dim3(tiles), dim3(kOrderThreads), 0, s, pairs, (int)tile, experts, expert, counts, o->err);
   hipLaunchKernelGGL(k_order_place, dim3(tiles), dim3(kOrderThreads), 0, s, pairs, (int)tile, tiles, experts, bits, expert, counts, offsets, place,
                      o->err);
   return launched(o);
