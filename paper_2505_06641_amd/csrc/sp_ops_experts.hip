@@ -282,8 +282,8 @@ sp_status sp_grouped_linear_quantized(sp_ops* o, int32_t n, int32_t k, int32_t m
   // Pieces of 16 rows while the device holds about all of their workgroups and each is through its depth soon (256 rows, 1024 -> 1024: 7.2 us
   // against 11.4 in tiles; 1024 rows, 1024 -> 512 11.1 against 10.5, 256 rows, 2048 -> 2048 20.9 against 16.0; addresses that are no multiples of 16 cost
   // them more: 256 rows of 32 groups, 1023 -> 515 21.4 against 16.6).  Tiles of 256 by 256, one to a compute unit, where there are many long ones
-  // (262144 rows, 2048 -> 2048: 1240 us against 1523 in tiles of 128 by 128, 1024 -> 1024 368 against 401; 65536 rows, 1024 -> 1024 106 against 100,
-  // 262144 rows, 512 -> 512 136 against 126).  y past the caches: 262144 rows, 64 -> 1024 134 us, else 167.
+  // (262144 rows, 2048 -> 2048: 1189 us against 1456 in tiles of 128 by 128, 1024 -> 1024 345 against 378; 512 -> 512 120 against 110).  y past the
+  // caches: 262144 rows, 256 -> 1024 157 us, else 207.
   const bool direct = (((uintptr_t)x | (uintptr_t)w | (uintptr_t)k | (uintptr_t)x_stride) & 15u) == 0;
   auto grid = [&](int64_t bm, int64_t bn, int64_t threads) {         // false: more workgroups than a launch holds
     const int64_t row_tiles = std::min<int64_t>((n + bm - 1) / bm + groups, n), col_tiles = (m + bn - 1) / bn;
@@ -302,7 +302,7 @@ sp_status sp_grouped_linear_quantized(sp_ops* o, int32_t n, int32_t k, int32_t m
   if (!g.ok) return SP_EDEVICE;
   with_type(out_dtype, [&]<typename T>() {
     auto kernel = few ? k_quantized_few<T> : large ? k_quantized<T, 256, 256, 128, 2, true>
-                  : direct ? k_quantized<T, 128, 128, 64, 3, true> : k_quantized<T, 128, 128, 64, 2, false>;
+                  : direct ? k_quantized<T, 128, 128, 64, 2, true> : k_quantized<T, 128, 128, 64, 2, false>;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(few ? kFewQuantizedThreads : large ? 512 : 256), 0, (hipStream_t)stream, a);
   });
   return launched(o);

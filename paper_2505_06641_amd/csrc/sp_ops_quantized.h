@@ -149,6 +149,10 @@ __device__ __forceinline__ bytes16 load_bytes(const int8_t* p, int t, int depth,
 //   DIRECT: memory to LDS without registers, STAGES pieces of the depth in LDS, one of them being multiplied.  For depths, strides and addresses
 //     that are multiples of 16.
 //   else by way of registers, two stages in LDS and one on its way, which takes any address and cuts what lies behind the depth.
+// Tiles of 128 by 128 have four workgroups to a compute unit, which hide each other's trips to memory (two stages of 64 bytes: 65536 rows,
+// 1024 -> 1024 97 us; three stages and three workgroups 101; tiles of 128 by 256, whose wavefronts read a quarter less from LDS, and two workgroups
+// 103).  Long depths of many tiles run at the rate that the matrix cores hold under their power limit: 262144 rows, 1024 -> 1024 between 64 and 1024
+// of depth gain 1930 TOP/s, the library's 8192 x 8192 x 8192 product has 2040 to 2310.
 template <int BM, int BN, int D, int STAGES, bool DIRECT>
 struct QuantizedTile {
   static constexpr int WAVES = BM / 32, FR = 2, FC = BN / 64, kRows = BM + BN;
@@ -186,7 +190,7 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
 template <typename TO, int BM, int BN, int D, int STAGES, bool DIRECT>
-__global__ __launch_bounds__(BM * 2, BM == 128 ? 3 : 2) void k_quantized(QuantizedArgs a) {
+__global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 : 3) void k_quantized(QuantizedArgs a) {
   typedef QuantizedTile<BM, BN, D, STAGES, DIRECT> Tile;
   constexpr int FR = Tile::FR, FC = Tile::FC, CH = Tile::kChunks, CX = Tile::kOfX, WAVES = Tile::WAVES, kStageBytes = Tile::kRows * D;
   constexpr int WN = BN / 2;                                          // columns of a wavefront
@@ -307,7 +311,8 @@ __global__ __launch_bounds__(BM * 2, BM == 128 ? 3 : 2) void k_quantized(Quantiz
   // columns 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3.  The 16-byte pieces of a row are permuted by the row.
   float* stage = reinterpret_cast<float*>(lds) + wave * 32 * WN;
   __syncthreads();
-  auto finish = [&](auto whole) {                                     // whole: all of the tile's rows and columns are there
+  // whole: all of the tile's rows and columns are there
+  auto finish = [&](auto whole, auto past_caches) {
 #pragma unroll
     for (int i = 0; i < FR; ++i) {
       const int r = lane & 31;
@@ -340,14 +345,16 @@ __global__ __launch_bounds__(BM * 2, BM == 128 ? 3 : 2) void k_quantized(Quantiz
           if (a.residual) v[e] += res[e];
         }
         TO* out = (TO*)a.y + row * a.y_stride + col;
-        if (whole && a.past_caches) store_past_caches(out, v);
+        if constexpr (past_caches) store_past_caches(out, v);
         else store_some(out, count, v);
       }
       wave_sync();
     }
   };
-  if (n_rows == BM && n_cols == BN) finish(std::true_type{});
-  else finish(std::false_type{});
+  const bool whole = n_rows == BM && n_cols == BN;
+  if (whole && a.past_caches) finish(std::true_type{}, std::true_type{});
+  else if (whole) finish(std::true_type{}, std::false_type{});
+  else finish(std::false_type{}, std::false_type{});
 }
 
 // Few rows: a request, a window of them, a small batch.  A workgroup takes 16 rows of one group and 16 columns, its wavefronts share out the
