@@ -148,7 +148,7 @@ sp_status move_sizes(const sp_ops* o, int32_t n, int32_t d, int32_t top, int32_t
   return SP_OK;
 }
 
-// Calls f<T, TEAM>(workgroups): the smallest team that holds a row of up to 64 pieces, a wavefront for longer ones.
+// Calls f<T, TEAM>(workgroups) with a team for rows of d columns.
 template <typename F>
 void with_rows(int32_t n, int32_t d, int32_t dtype, F&& f) {
   with_type(dtype, [&]<typename T>() {
@@ -157,10 +157,15 @@ void with_rows(int32_t n, int32_t d, int32_t dtype, F&& f) {
       constexpr int rows = 256 / TEAM;
       f.template operator()<T, TEAM>(dim3((unsigned)std::min<int64_t>(((int64_t)n + rows - 1) / rows, kMoveBlocks)));
     };
-    if (pieces <= 4) run.template operator()<4>();
-    else if (pieces <= 8) run.template operator()<8>();
-    else if (pieces <= 16) run.template operator()<16>();
-    else if (pieces <= 32) run.template operator()<32>();
+    // the largest team that leaves the fewest lanes without a piece in the last turn (96 pieces: 32 lanes in three turns)
+    auto idle = [&](int team) { return (pieces + team - 1) / team * team - pieces; };
+    int best = 64;
+    for (int team = 32; team >= 4; team /= 2)
+      if (idle(team) < idle(best) && (pieces + team - 1) / team <= 4) best = team;
+    if (best == 4) run.template operator()<4>();
+    else if (best == 8) run.template operator()<8>();
+    else if (best == 16) run.template operator()<16>();
+    else if (best == 32) run.template operator()<32>();
     else run.template operator()<64>();
   });
 }

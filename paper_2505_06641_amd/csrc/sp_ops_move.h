@@ -37,6 +37,53 @@ __global__ __launch_bounds__(256) void k_dispatch(int n, int d, int top, const T
   }
 }
 
+// A 16-byte piece as it is in memory: what makes numbers of it would wait for it.  The first `count` elements of it count, as far as the lane has any.
+typedef uint32_t raw_piece __attribute__((ext_vector_type(4)));
+typedef uint32_t raw_piece_any __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T>
+__device__ __forceinline__ raw_piece load_raw_piece(const T* p, int count) {
+  constexpr int V = kPiece<T>;
+  raw_piece q = {0, 0, 0, 0};
+  if (count >= V) {
+    q = *reinterpret_cast<const raw_piece_any*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < count) {
+        if constexpr (V == 4) q[i] = __float_as_uint(p[i]);
+        else q[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (i % 2 * 16);
+      }
+  }
+  return q;
+}
+__device__ __forceinline__ float of_raw(const float*, raw_piece q, int i) { return __uint_as_float(q[i]); }
+__device__ __forceinline__ float of_raw(const bf16*, raw_piece q, int i) {
+  return __uint_as_float(i % 2 ? q[i / 2] & 0xffff0000u : q[i / 2] << 16);
+}
+
+// Up to kAtOnce of a row's pairs: their places and weights, and the pieces at the places, which are on their way together.
+constexpr int kAtOnce = 4;
+struct Pairs {
+  int p[kAtOnce];
+  float w[kAtOnce];
+  __device__ __forceinline__ Pairs(const int32_t* __restrict__ place, const float* __restrict__ weight, int64_t row, int first, int top, int rows,
+                                   uint32_t* err, bool report) {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int64_t pair = row * top + min(first + u, top - 1);
+      p[u] = place_of(place, pair, rows, err, report);
+      w[u] = weight ? weight[pair] : 1.f;
+      if (first + u >= top) p[u] = -1;
+    }
+  }
+  // (a pair without a place reads the first row, if there are any, and does not count)
+  template <typename T>
+  __device__ __forceinline__ void load(const T* ys, int64_t stride, int64_t col, int count, raw_piece (&v)[kAtOnce]) const {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) v[u] = load_raw_piece(ys + max(p[u], 0) * stride + col, count);
+  }
+};
+
 template <typename T, int TEAM>
 __global__ __launch_bounds__(256) void k_combine(int n, int d, int top, int rows, const T* __restrict__ ys, int64_t ys_stride,
                                                  const int32_t* __restrict__ place, const float* __restrict__ weight, const T* residual,
@@ -47,26 +94,28 @@ __global__ __launch_bounds__(256) void k_combine(int n, int d, int top, int rows
     for (int64_t col = t * V; col < d; col += TEAM * V) {
       const int count = (int)min((int64_t)V, d - col);
       float sum[V] = {};
-      for (int j = 0; j < top; ++j) {
-        const int p = place_of(place, row * top + j, rows, err, t == 0);
-        if (p < 0) continue;
-        const float w = weight ? weight[row * top + j] : 1.f;
-        float v[V];
-        load_some(ys + p * ys_stride + col, count, 0.f, v);
+      raw_piece r;
+      if (residual) r = load_raw_piece(residual + row * residual_stride + col, count);
+      for (int j = 0; j < top; j += kAtOnce) {
+        const Pairs q(place, weight, row, j, top, rows, err, t == 0);
+        raw_piece v[kAtOnce];
+        q.load(ys, ys_stride, col, rows > 0 ? count : 0, v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] += w * v[i];
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+          for (int i = 0; i < V; ++i) sum[i] += q.p[u] >= 0 ? q.w[u] * of_raw((const T*)nullptr, v[u], i) : 0.f;
       }
       if (residual) {
-        float r[V];
-        load_some(residual + row * residual_stride + col, count, 0.f, r);
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] += r[i];
+        for (int i = 0; i < V; ++i) sum[i] += of_raw((const T*)nullptr, r, i);
       }
       store_some(y + row * y_stride + col, count, sum);
     }
   }
 }
 
+// dys may lie where ys does: a lane reads its piece of a row before it writes it, and nobody else reads that (a pair without a place reads what it
+// does not use).
 template <typename T, int TEAM>
 __global__ __launch_bounds__(256) void k_combine_back(int n, int d, int top, const T* __restrict__ dy, int64_t dy_stride, int rows,
                                                       const T* ys, int64_t ys_stride, const int32_t* __restrict__ place,
@@ -75,29 +124,40 @@ __global__ __launch_bounds__(256) void k_combine_back(int n, int d, int top, con
   constexpr int V = kPiece<T>, ROWS = 256 / TEAM;
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS) {
-    for (int j = 0; j < top; ++j) {
-      const int p = place_of(place, row * top + j, rows, err, t == 0);
-      const float w = weight ? weight[row * top + j] : 1.f;
-      float dot = 0.f;
-      if (p >= 0)
-        for (int64_t col = t * V; col < d; col += TEAM * V) {
-          const int count = (int)min((int64_t)V, d - col);
-          float g[V], v[V];
-          load_some(dy + row * dy_stride + col, count, 0.f, g);
-          if (dweight) {
-            load_some(ys + p * ys_stride + col, count, 0.f, v);
+    for (int j = 0; j < top; j += kAtOnce) {
+      const Pairs q(place, weight, row, j, top, rows, err, t == 0);
+      float dot[kAtOnce] = {};
+      for (int64_t col = t * V; col < d; col += TEAM * V) {
+        const int count = (int)min((int64_t)V, d - col);
+        const raw_piece raw = load_raw_piece(dy + row * dy_stride + col, count);
+        raw_piece v[kAtOnce];
+        if (dweight) q.load(ys, ys_stride, col, rows > 0 ? count : 0, v);
+        float g[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) dot += g[i] * v[i];
-          }
-          if (dys) {
+        for (int i = 0; i < V; ++i) g[i] = of_raw((const T*)nullptr, raw, i);
+        if (dweight) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] *= w;
-            store_some(dys + p * dys_stride + col, count, g);
-          }
+          for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int i = 0; i < V; ++i) dot[u] += g[i] * of_raw((const T*)nullptr, v[u], i);
         }
+        if (dys) {
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u)
+            if (q.p[u] >= 0) {
+              float o[V];
+#pragma unroll
+              for (int i = 0; i < V; ++i) o[i] = g[i] * q.w[u];
+              store_some(dys + q.p[u] * dys_stride + col, count, o);
+            }
+        }
+      }
       if (dweight) {
-        dot = team_sum<TEAM>(dot, nullptr);
-        if (t == 0) dweight[row * top + j] = dot;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const float s = team_sum<TEAM>(dot[u], nullptr);
+          if (t == 0 && j + u < top) dweight[row * top + j + u] = q.p[u] >= 0 ? s : 0.f;
+        }
       }
     }
   }

@@ -508,7 +508,7 @@ __global__ __launch_bounds__(256, TEAM < 64 ? 4 : 2) void k_route(RouteArgs a) {
 //   renormalised   dz_j = scale w'_j (dw_j - D)   (times 1 - s_j for sigmoid), w' the shares; 0 for experts not chosen
 //   sigmoid        dz_j = scale dw_j s_j (1 - s_j)
 //   softmax        dz_e = s_e (scale dw_e - sum_l scale dw_l s_l), every expert
-// A team holds a row.  Lane j has the j-th chosen expert; what the others need of it goes through LDS.  A row without an expert has gradient 0.
+// A team of lanes of one wavefront holds a row.  Lane j has the j-th chosen expert.  A row without an expert has gradient 0.
 template <typename T, int TEAM, int C>
 __global__ __launch_bounds__(256) void k_route_back(int n, int experts, int top, const T* z, int64_t z_stride, bool sigmoid, bool renormalize,
                                                     float scale, const int32_t* __restrict__ expert, const float* __restrict__ dweight, T* dz,
@@ -552,30 +552,38 @@ __global__ __launch_bounds__(256) void k_route_back(int n, int experts, int top,
     }
     const float share = chosen_weight<TEAM>(zc, sigmoid, renormalize, from, total);         // of the scale
     const float dot = renormalize || all ? team_sum<TEAM>(e >= 0 ? dw * share : 0.f, nullptr) : 0.f;
+    const float by = __builtin_amdgcn_rcpf(total);
     float mine = dw;                                       // what the chosen expert's logit gets (softmax: what its score gets)
     if (!all) {
       mine = share * (dw - dot);
-      if (sigmoid) mine *= zc == -INFINITY ? 1.f : 1.f / (1.f + expf(zc));                  // 1 - s
+      if (sigmoid) mine *= __builtin_amdgcn_rcpf(1.f + exp_near(zc));                       // 1 - s
     }
-    // an expert that is named twice gets both parts, in order
+    // What the others need of it goes through the team's own part of LDS: a wavefront's, which nobody else waits for.
+    const unsigned long long mates = TEAM == 64 ? ~0ull : ((1ull << (TEAM & 63)) - 1) << (threadIdx.x % 64 / TEAM * TEAM);
+    const bool named = (__ballot(e >= 0) & mates) != 0;
+    wave_sync();                                           // the row before has been read
+    if (e >= 0) up[team][e] = __int_as_float(t);
+    wave_sync();
     bool first = e >= 0;
-    float sum = 0.f;
-    int named = 0;
-    for (int j = 0; j < top; ++j) {
-      const int o = __shfl(e, j, TEAM);
-      const float om = __shfl(mine, j, TEAM);
-      named += o >= 0;
-      if (o == e) sum += om;
-      first &= o != e || j >= t;
+    if (__any(first && __float_as_int(up[team][max(e, 0)]) != t)) {
+      // an expert that is named twice gets both parts, in order, from the first lane
+      float sum = 0.f;
+      for (int j = 0; j < top; ++j) {
+        const int o = __shfl(e, j, TEAM);
+        const float om = __shfl(mine, j, TEAM);
+        if (o == e) sum += om;
+        first &= o != e || j >= t;
+      }
+      mine = sum;
     }
-    __syncthreads();                                       // the row before has been read
+    wave_sync();
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int h = 0; h < V; h += 4) *reinterpret_cast<f32x4*>(&up[team][(c * TEAM + t) * V + h]) = f32x4{0.f, 0.f, 0.f, 0.f};
-    __syncthreads();
-    if (first) up[team][e] = sum;
-    __syncthreads();
+    wave_sync();
+    if (first) up[team][e] = mine;
+    wave_sync();
     if (!in) continue;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -584,7 +592,7 @@ __global__ __launch_bounds__(256) void k_route_back(int n, int experts, int top,
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         u[i] = up[team][col + i];
-        if (all) u[i] = named ? v[c][i] / total * (u[i] - dot) : 0.f;
+        if (all) u[i] = named ? v[c][i] * by * (u[i] - dot) : 0.f;
       }
       store_some(dz + row * dz_stride + col, experts - col, u);
     }
