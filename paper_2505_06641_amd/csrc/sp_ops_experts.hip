@@ -148,25 +148,29 @@ sp_status move_sizes(const sp_ops* o, int32_t n, int32_t d, int32_t top, int32_t
   return SP_OK;
 }
 
-// Calls f<T, TEAM>(workgroups) with a team for rows of d columns.
+// Calls f<T, TEAM, AT>(workgroups) with a team for rows of d columns and the pairs of a row that are on their way together.
 template <typename F>
-void with_rows(int32_t n, int32_t d, int32_t dtype, F&& f) {
+void with_rows(int32_t n, int32_t d, int32_t top, int32_t dtype, F&& f) {
   with_type(dtype, [&]<typename T>() {
     const int pieces = (d + kPiece<T> - 1) / kPiece<T>;
-    auto run = [&]<int TEAM>() {
+    auto team = [&]<int TEAM>() {
       constexpr int rows = 256 / TEAM;
-      f.template operator()<T, TEAM>(dim3((unsigned)std::min<int64_t>(((int64_t)n + rows - 1) / rows, kMoveBlocks)));
+      const dim3 grid((unsigned)std::min<int64_t>(((int64_t)n + rows - 1) / rows, kMoveBlocks));
+      if (top == 1) f.template operator()<T, TEAM, 1>(grid);
+      else if (top == 2) f.template operator()<T, TEAM, 2>(grid);
+      else if (top <= 4) f.template operator()<T, TEAM, 4>(grid);
+      else f.template operator()<T, TEAM, 8>(grid);
     };
     // the largest team that leaves the fewest lanes without a piece in the last turn (96 pieces: 32 lanes in three turns)
-    auto idle = [&](int team) { return (pieces + team - 1) / team * team - pieces; };
+    auto idle = [&](int lanes) { return (pieces + lanes - 1) / lanes * lanes - pieces; };
     int best = 64;
-    for (int team = 32; team >= 4; team /= 2)
-      if (idle(team) < idle(best) && (pieces + team - 1) / team <= 4) best = team;
-    if (best == 4) run.template operator()<4>();
-    else if (best == 8) run.template operator()<8>();
-    else if (best == 16) run.template operator()<16>();
-    else if (best == 32) run.template operator()<32>();
-    else run.template operator()<64>();
+    for (int lanes = 32; lanes >= 4; lanes /= 2)
+      if (idle(lanes) < idle(best) && (pieces + lanes - 1) / lanes <= 4) best = lanes;
+    if (best == 4) team.template operator()<4>();
+    else if (best == 8) team.template operator()<8>();
+    else if (best == 16) team.template operator()<16>();
+    else if (best == 32) team.template operator()<32>();
+    else team.template operator()<64>();
   });
 }
 
@@ -182,8 +186,8 @@ sp_status sp_dispatch(sp_ops* o, int32_t n, int32_t d, int32_t top, int32_t dtyp
   if (n == 0) return SP_OK;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
-  with_rows(n, d, dtype, [&]<typename T, int TEAM>(dim3 grid) {
-    hipLaunchKernelGGL((k_dispatch<T, TEAM>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, (const T*)x, x_stride, place, rows, (T*)xs,
+  with_rows(n, d, top, dtype, [&]<typename T, int TEAM, int AT>(dim3 grid) {
+    hipLaunchKernelGGL((k_dispatch<T, TEAM, AT>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, (const T*)x, x_stride, place, rows, (T*)xs,
                        xs_stride, o->err);
   });
   return launched(o);
@@ -199,8 +203,8 @@ sp_status sp_combine(sp_ops* o, int32_t n, int32_t d, int32_t top, int32_t dtype
   if (n == 0) return SP_OK;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
-  with_rows(n, d, dtype, [&]<typename T, int TEAM>(dim3 grid) {
-    hipLaunchKernelGGL((k_combine<T, TEAM>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, rows, (const T*)ys, ys_stride, place, weight,
+  with_rows(n, d, top, dtype, [&]<typename T, int TEAM, int AT>(dim3 grid) {
+    hipLaunchKernelGGL((k_combine<T, TEAM, AT>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, rows, (const T*)ys, ys_stride, place, weight,
                        (const T*)residual, residual_stride, (T*)y, y_stride, o->err);
   });
   return launched(o);
@@ -217,8 +221,8 @@ sp_status sp_combine_backward(sp_ops* o, int32_t n, int32_t d, int32_t top, int3
   if (n == 0 || (!dys && !dweight)) return SP_OK;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
-  with_rows(n, d, dtype, [&]<typename T, int TEAM>(dim3 grid) {
-    hipLaunchKernelGGL((k_combine_back<T, TEAM>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, (const T*)dy, dy_stride, rows,
+  with_rows(n, d, top, dtype, [&]<typename T, int TEAM, int AT>(dim3 grid) {
+    hipLaunchKernelGGL((k_combine_back<T, TEAM, AT>), grid, dim3(256), 0, (hipStream_t)stream, n, d, top, (const T*)dy, dy_stride, rows,
                        (const T*)ys, ys_stride, place, weight, (T*)dys, dys_stride, dweight, o->err);
   });
   return launched(o);

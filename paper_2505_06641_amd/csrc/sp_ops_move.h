@@ -19,41 +19,29 @@ __device__ __forceinline__ int place_of(const int32_t* __restrict__ place, int64
   return -1;
 }
 
-template <typename T, int TEAM>
-__global__ __launch_bounds__(256) void k_dispatch(int n, int d, int top, const T* __restrict__ x, int64_t x_stride,
-                                                  const int32_t* __restrict__ place, int rows, T* __restrict__ xs, int64_t xs_stride,
-                                                  uint32_t* err) {
-  constexpr int V = kPiece<T>, ROWS = 256 / TEAM;
-  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS) {
-    for (int64_t col = t * V; col < d; col += TEAM * V) {
-      float v[V];
-      load_some(x + row * x_stride + col, (int)(d - col), 0.f, v);
-      for (int j = 0; j < top; ++j) {
-        const int p = place_of(place, row * top + j, rows, err, t == 0);
-        if (p >= 0) store_some(xs + p * xs_stride + col, (int)(d - col), v);
-      }
-    }
-  }
-}
-
-// A 16-byte piece as it is in memory: what makes numbers of it would wait for it.  The first `count` elements of it count, as far as the lane has any.
+// A 16-byte piece of a row of d columns as it is in memory, from column `col` on: what makes numbers of it would wait for it.  What lies behind the
+// row is 0; a piece that the row ends in is the row's last 16 bytes, moved down.
 typedef uint32_t raw_piece __attribute__((ext_vector_type(4)));
 typedef uint32_t raw_piece_any __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T>
-__device__ __forceinline__ raw_piece load_raw_piece(const T* p, int count) {
+__device__ __forceinline__ raw_piece load_raw_piece(const T* row, int col, int d) {
   constexpr int V = kPiece<T>;
+  if (col + V <= d) return *reinterpret_cast<const raw_piece_any*>(row + col);
   raw_piece q = {0, 0, 0, 0};
-  if (count >= V) {
-    q = *reinterpret_cast<const raw_piece_any*>(p);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < count) {
-        if constexpr (V == 4) q[i] = __float_as_uint(p[i]);
-        else q[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (i % 2 * 16);
-      }
+  if (d >= V) {
+    q = *reinterpret_cast<const raw_piece_any*>(row + d - V);
+    const uint64_t low = (uint64_t)q[1] << 32 | q[0], high = (uint64_t)q[3] << 32 | q[2];
+    const int by = (col + V - d) * (int)sizeof(T) * 8, rest = by & 63;
+    const uint64_t a = by >= 64 ? high : low, b = by >= 64 ? 0 : high;
+    const uint64_t lo = rest ? a >> rest | b << (64 - rest) : a, hi = b >> rest;
+    return raw_piece{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
   }
+#pragma unroll
+  for (int i = 0; i < V - 1; ++i)                                     // (col is 0: a row of less than a piece)
+    if (i < d) {
+      if constexpr (V == 4) q[i] = __float_as_uint(row[i]);
+      else q[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[i] << (i % 2 * 16);
+    }
   return q;
 }
 __device__ __forceinline__ float of_raw(const float*, raw_piece q, int i) { return __uint_as_float(q[i]); }
@@ -61,62 +49,84 @@ __device__ __forceinline__ float of_raw(const bf16*, raw_piece q, int i) {
   return __uint_as_float(i % 2 ? q[i / 2] & 0xffff0000u : q[i / 2] << 16);
 }
 
-// Up to kAtOnce of a row's pairs: their places and weights, and the pieces at the places, which are on their way together.
-constexpr int kAtOnce = 4;
+// Up to AT of a row's pairs: their places and weights, and the pieces at the places, which are on their way together.  (As many as the row has up to 8: 32768
+// rows of 768 bfloat16 with 8 pairs 97 us, with each read behind the one before 127.)
+template <int AT>
 struct Pairs {
-  int p[kAtOnce];
-  float w[kAtOnce];
+  int p[AT];
+  float w[AT];
   __device__ __forceinline__ Pairs(const int32_t* __restrict__ place, const float* __restrict__ weight, int64_t row, int first, int top, int rows,
                                    uint32_t* err, bool report) {
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
+    for (int u = 0; u < AT; ++u) {
       const int64_t pair = row * top + min(first + u, top - 1);
       p[u] = place_of(place, pair, rows, err, report);
       w[u] = weight ? weight[pair] : 1.f;
       if (first + u >= top) p[u] = -1;
     }
   }
-  // (a pair without a place reads the first row, if there are any, and does not count)
+  // (a pair without a place reads the first row, and does not count)
   template <typename T>
-  __device__ __forceinline__ void load(const T* ys, int64_t stride, int64_t col, int count, raw_piece (&v)[kAtOnce]) const {
+  __device__ __forceinline__ void load(const T* ys, int64_t stride, int col, int d, raw_piece (&v)[AT]) const {
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) v[u] = load_raw_piece(ys + max(p[u], 0) * stride + col, count);
+    for (int u = 0; u < AT; ++u) v[u] = load_raw_piece(ys + max(p[u], 0) * stride, col, d);
   }
 };
 
-template <typename T, int TEAM>
+template <typename T, int TEAM, int AT>
+__global__ __launch_bounds__(256) void k_dispatch(int n, int d, int top, const T* __restrict__ x, int64_t x_stride,
+                                                  const int32_t* __restrict__ place, int rows, T* __restrict__ xs, int64_t xs_stride,
+                                                  uint32_t* err) {
+  constexpr int V = kPiece<T>, ROWS = 256 / TEAM;
+  const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS) {
+    for (int j = 0; j < top; j += AT) {
+      const Pairs<AT> q(place, nullptr, row, j, top, rows, err, t == 0);
+      for (int col = t * V; col < d; col += TEAM * V) {
+        float v[V];
+        load_some(x + row * x_stride + col, d - col, 0.f, v);
+#pragma unroll
+        for (int u = 0; u < AT; ++u)
+          if (q.p[u] >= 0) store_some(xs + q.p[u] * xs_stride + col, d - col, v);
+      }
+    }
+  }
+}
+
+template <typename T, int TEAM, int AT>
 __global__ __launch_bounds__(256) void k_combine(int n, int d, int top, int rows, const T* __restrict__ ys, int64_t ys_stride,
                                                  const int32_t* __restrict__ place, const float* __restrict__ weight, const T* residual,
                                                  int64_t residual_stride, T* y, int64_t y_stride, uint32_t* err) {
   constexpr int V = kPiece<T>, ROWS = 256 / TEAM;
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS) {
-    for (int64_t col = t * V; col < d; col += TEAM * V) {
-      const int count = (int)min((int64_t)V, d - col);
+    const Pairs<AT> first(place, weight, row, 0, top, rows, err, t == 0);
+    for (int col = t * V; col < d; col += TEAM * V) {
       float sum[V] = {};
       raw_piece r;
-      if (residual) r = load_raw_piece(residual + row * residual_stride + col, count);
-      for (int j = 0; j < top; j += kAtOnce) {
-        const Pairs q(place, weight, row, j, top, rows, err, t == 0);
-        raw_piece v[kAtOnce];
-        q.load(ys, ys_stride, col, rows > 0 ? count : 0, v);
+      if (residual) r = load_raw_piece(residual + row * residual_stride, col, d);
+      auto add = [&](const Pairs<AT>& q) {
+        raw_piece v[AT];
+        q.load(ys, ys_stride, col, d, v);
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
+        for (int u = 0; u < AT; ++u)
 #pragma unroll
           for (int i = 0; i < V; ++i) sum[i] += q.p[u] >= 0 ? q.w[u] * of_raw((const T*)nullptr, v[u], i) : 0.f;
-      }
+      };
+      if (rows > 0) add(first);                                       // (no rows: no pair has a place)
+      for (int j = AT; j < top && rows > 0; j += AT) add(Pairs<AT>(place, weight, row, j, top, rows, err, t == 0));
       if (residual) {
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] += of_raw((const T*)nullptr, r, i);
       }
-      store_some(y + row * y_stride + col, count, sum);
+      store_some(y + row * y_stride + col, d - col, sum);
     }
   }
 }
 
 // dys may lie where ys does: a lane reads its piece of a row before it writes it, and nobody else reads that (a pair without a place reads what it
 // does not use).
-template <typename T, int TEAM>
+template <typename T, int TEAM, int AT>
 __global__ __launch_bounds__(256) void k_combine_back(int n, int d, int top, const T* __restrict__ dy, int64_t dy_stride, int rows,
                                                       const T* ys, int64_t ys_stride, const int32_t* __restrict__ place,
                                                       const float* __restrict__ weight, T* dys, int64_t dys_stride,
@@ -124,37 +134,41 @@ __global__ __launch_bounds__(256) void k_combine_back(int n, int d, int top, con
   constexpr int V = kPiece<T>, ROWS = 256 / TEAM;
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS) {
-    for (int j = 0; j < top; j += kAtOnce) {
-      const Pairs q(place, weight, row, j, top, rows, err, t == 0);
-      float dot[kAtOnce] = {};
-      for (int64_t col = t * V; col < d; col += TEAM * V) {
-        const int count = (int)min((int64_t)V, d - col);
-        const raw_piece raw = load_raw_piece(dy + row * dy_stride + col, count);
-        raw_piece v[kAtOnce];
-        if (dweight) q.load(ys, ys_stride, col, rows > 0 ? count : 0, v);
+    for (int j = 0; j < top; j += AT) {
+      const Pairs<AT> q(place, weight, row, j, top, rows, err, t == 0);
+      float dot[AT] = {};
+      for (int col = t * V; col < d; col += TEAM * V) {
+        const raw_piece raw = load_raw_piece(dy + row * dy_stride, col, d);
+        raw_piece v[AT];
+        if (dweight && rows > 0) {
+          q.load(ys, ys_stride, col, d, v);
+        } else {
+#pragma unroll
+          for (int u = 0; u < AT; ++u) v[u] = raw_piece{0, 0, 0, 0};
+        }
         float g[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) g[i] = of_raw((const T*)nullptr, raw, i);
         if (dweight) {
 #pragma unroll
-          for (int u = 0; u < kAtOnce; ++u)
+          for (int u = 0; u < AT; ++u)
 #pragma unroll
             for (int i = 0; i < V; ++i) dot[u] += g[i] * of_raw((const T*)nullptr, v[u], i);
         }
         if (dys) {
 #pragma unroll
-          for (int u = 0; u < kAtOnce; ++u)
+          for (int u = 0; u < AT; ++u)
             if (q.p[u] >= 0) {
               float o[V];
 #pragma unroll
               for (int i = 0; i < V; ++i) o[i] = g[i] * q.w[u];
-              store_some(dys + q.p[u] * dys_stride + col, count, o);
+              store_some(dys + q.p[u] * dys_stride + col, d - col, o);
             }
         }
       }
       if (dweight) {
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
+        for (int u = 0; u < AT; ++u) {
           const float s = team_sum<TEAM>(dot[u], nullptr);
           if (t == 0 && j + u < top) dweight[row * top + j + u] = q.p[u] >= 0 ? s : 0.f;
         }
