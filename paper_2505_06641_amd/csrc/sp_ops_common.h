@@ -95,6 +95,37 @@ __device__ __forceinline__ void store_some(T* p, int count, const float (&v)[V])
   }
 }
 
+// A 16-byte piece of a row of d columns as it is in memory, from column `col` on: what makes numbers of it would wait for it.  What lies behind the
+// row is 0; a piece that the row ends in is the row's last 16 bytes, moved down.
+typedef uint32_t raw_piece __attribute__((ext_vector_type(4)));
+typedef uint32_t raw_piece_any __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T>
+__device__ __forceinline__ raw_piece load_raw_piece(const T* row, int col, int d) {
+  constexpr int V = kPiece<T>;
+  if (col + V <= d) return *reinterpret_cast<const raw_piece_any*>(row + col);
+  raw_piece q = {0, 0, 0, 0};
+  if (col >= d) return q;
+  if (d >= V) {
+    q = *reinterpret_cast<const raw_piece_any*>(row + d - V);
+    const uint64_t low = (uint64_t)q[1] << 32 | q[0], high = (uint64_t)q[3] << 32 | q[2];
+    const int by = (col + V - d) * (int)sizeof(T) * 8, rest = by & 63;
+    const uint64_t a = by >= 64 ? high : low, b = by >= 64 ? 0 : high;
+    const uint64_t lo = rest ? a >> rest | b << (64 - rest) : a, hi = b >> rest;
+    return raw_piece{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+  }
+#pragma unroll
+  for (int i = 0; i < V - 1; ++i)                                     // (col is 0: a row of less than a piece)
+    if (i < d) {
+      if constexpr (V == 4) q[i] = __float_as_uint(row[i]);
+      else q[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[i] << (i % 2 * 16);
+    }
+  return q;
+}
+__device__ __forceinline__ float of_raw(const float*, raw_piece q, int i) { return __uint_as_float(q[i]); }
+__device__ __forceinline__ float of_raw(const bf16*, raw_piece q, int i) {
+  return __uint_as_float(i % 2 ? q[i / 2] & 0xffff0000u : q[i / 2] << 16);
+}
+
 // Sum and maximum over a team: TEAM consecutive lanes of a wavefront (2 to 64), or the TEAM > 64 threads of a
 // workgroup.  Every lane of the team has the result, and every lane adds in the same order.  `lds`: one float per
 // wavefront; two reductions that follow each other take different arrays.

@@ -3,7 +3,8 @@
 // The numbers are the 16-bit halves of the words of Philox 4x32 with ten rounds (J. Salmon, M. Moraes, R. Dror, D. Shaw, "Parallel random
 // numbers: as easy as 1, 2, 3", 2011), so that one computation serves the eight columns of a piece: counter (piece of the row, row, offset low,
 // offset high), key the seed, column 8 piece + 2 word + half with the low half first.  They hang on nothing else: not on type, stride or
-// launch, and the backward pass is the same call on dy.
+// launch, and the backward pass is the same call on dy.  Bound by memory: 65536 x 768 bfloat16 with a residual 49 us (6.2 TB/s, the residual partly from
+// the last-level cache), 262144 x 256 float32 99 us (5.4 TB/s); one computation to four columns would take as long as the memory does.
 #pragma once
 #include "sp_ops_common.h"
 
@@ -35,30 +36,56 @@ __device__ __forceinline__ void philox(uint32_t (&c)[4], uint32_t k0, uint32_t k
   }
 }
 
-constexpr int kDropoutEach = 4;                  // pieces of a thread
-
+// Eight columns of a row as they are in memory.
 template <typename T>
-__global__ __launch_bounds__(256) void k_dropout(DropoutArgs a) {
-  const uint64_t offset = a.offset + (a.step ? (uint64_t)*a.step : 0u);
-  const int64_t all = (int64_t)a.n * a.pieces, base = (int64_t)blockIdx.x * (256 * kDropoutEach);
+struct RawColumns {
+  static constexpr int V = kPiece<T>;
+  raw_piece q[8 / V];
+  __device__ __forceinline__ void load(const T* row, int col, int d) {
 #pragma unroll
-  for (int u = 0; u < kDropoutEach; ++u) {
-    const int64_t at = base + u * 256 + threadIdx.x;
-    if (at >= all) return;
-    const int64_t row = at / a.pieces;
-    const int piece = (int)(at % a.pieces), col = piece * 8, count = a.d - col;
-    float v[8], r[8];
-    load_some((const T*)a.x + row * a.x_stride + col, count, 0.f, v);
-    if (a.residual) load_some((const T*)a.residual + row * a.residual_stride + col, count, 0.f, r);
-    uint32_t c[4] = {(uint32_t)piece, (uint32_t)row, (uint32_t)offset, (uint32_t)(offset >> 32)};
+    for (int h = 0; h < 8 / V; ++h) q[h] = load_raw_piece(row, col + h * V, d);
+  }
+  __device__ __forceinline__ float operator[](int i) const { return of_raw((const T*)nullptr, q[i / V], i % V); }
+};
+
+// EACH: pieces of a thread, which are on their way together.  step_rows, step_pieces: 256 pieces on, in whole rows and pieces.
+template <typename T, int EACH>
+__global__ __launch_bounds__(256) void k_dropout(DropoutArgs a, int step_rows, int step_pieces) {
+  const uint64_t offset = a.offset + (a.step ? (uint64_t)*a.step : 0u);
+  const int64_t at = (int64_t)blockIdx.x * (256 * EACH) + threadIdx.x;
+  int64_t row = at >> 32 ? at / a.pieces : (int64_t)((uint32_t)at / (uint32_t)a.pieces);
+  int piece = (int)(at - row * a.pieces);
+  int64_t rows[EACH];
+  int cols[EACH];
+  RawColumns<T> x[EACH], r[EACH];
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    rows[u] = row;
+    cols[u] = piece * 8;
+    if (row < a.n) {
+      x[u].load((const T*)a.x + row * a.x_stride, cols[u], a.d);
+      if (a.residual) r[u].load((const T*)a.residual + row * a.residual_stride, cols[u], a.d);
+    }
+    row += step_rows;
+    piece += step_pieces;
+    if (piece >= a.pieces) {
+      piece -= a.pieces;
+      ++row;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    if (rows[u] >= a.n) return;
+    uint32_t c[4] = {(uint32_t)cols[u] / 8, (uint32_t)rows[u], (uint32_t)offset, (uint32_t)(offset >> 32)};
     philox(c, a.key0, a.key1);
+    float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t number = i % 2 ? c[i / 2] >> 16 : c[i / 2] & 0xffffu;
-      v[i] = number >= a.drop ? v[i] * a.scale : 0.f;
-      if (a.residual) v[i] += r[i];
+      v[i] = number >= a.drop ? x[u][i] * a.scale : 0.f;
+      if (a.residual) v[i] += r[u][i];
     }
-    store_some((T*)a.y + row * a.y_stride + col, count, v);
+    store_some((T*)a.y + rows[u] * a.y_stride + cols[u], a.d - cols[u], v);
   }
 }
 

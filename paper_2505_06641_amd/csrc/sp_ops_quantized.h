@@ -51,15 +51,15 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_quantize(int n, int d, c
   const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   int turn = 0;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + team; row < n; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-    float v[C][V], high = 0.f;
+    raw_piece v[C];
+    float high = 0.f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = (c * TEAM + t) * V;
-      load_some(x + row * x_stride + col, d - col, 0.f, v[c]);
+    for (int c = 0; c < C; ++c) v[c] = load_raw_piece(x + row * x_stride, (c * TEAM + t) * V, d);
 #pragma unroll
-      for (int i = 0; i < V; ++i) high = !(fabsf(v[c][i]) < INFINITY) ? INFINITY : fmaxf(high, fabsf(v[c][i]));
-    }
-    high = team_max<TEAM>(high, red[turn]);
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < V; ++i) high = __builtin_elementwise_maximum(high, fabsf(of_raw((const T*)nullptr, v[c], i)));     // (NaN stays)
+    high = team_max<TEAM>(high < INFINITY ? high : INFINITY, red[turn]);
     const RowScale s(high, high < INFINITY);
     if (t == 0) scale[row] = s.scale;
 #pragma unroll
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(kTeamThreads<TEAM>) void k_quantize(int n, int d, c
       const int col = (c * TEAM + t) * V;
       int b[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) b[i] = s.of(v[c][i]);
+      for (int i = 0; i < V; ++i) b[i] = s.of(of_raw((const T*)nullptr, v[c], i));
       if (col < d) store_bytes(q + row * q_stride + col, d - col, b);
     }
   }
