@@ -59,23 +59,23 @@ sp_status sp_route(sp_ops* o, int32_t n, int32_t experts, int32_t top, int32_t d
   auto per_lane = [&](int team) { return (a.width + team / power - 1) / (team / power); };
   // a wavefront to a row while the device holds about all of them at once: 2048 rows of 64 bfloat16 experts 4.0 us either way, 16384 rows 4.3 us in
   // teams of 8 and 11.7 in wavefronts; 256 rows of 256 experts in groups 8.0 us and 5.8
-  const bool narrow = experts <= 256 && top <= 8 && groups <= 8 && per_lane(16) <= 16 && n > 2048;
-  const int team = !narrow ? 64 : per_lane(8) <= 16 ? 8 : 16, per = per_lane(team), rows = 4 * 64 / team;
+  const bool narrow = experts <= 256 && top <= 8 && groups <= 8 && per_lane(8) <= 32 && n > 2048;
+  const int team = narrow ? 8 : 64, per = per_lane(team), rows = 4 * 64 / team;
   const dim3 grid((unsigned)std::min<int64_t>(((int64_t)n + rows - 1) / rows, 2048));
   with_type(dtype, [&]<typename T>() {
     auto kernel = [&]<bool BY_LOGIT>() {
-      return team == 16 ? k_route<T, 16, 16, BY_LOGIT>
-             : team == 8 ? (per <= 1   ? k_route<T, 8, 1, BY_LOGIT>
-                            : per <= 2 ? k_route<T, 8, 2, BY_LOGIT>
-                            : per <= 4 ? k_route<T, 8, 4, BY_LOGIT>
-                            : per <= 8 ? k_route<T, 8, 8, BY_LOGIT>
-                                       : k_route<T, 8, 16, BY_LOGIT>)
-                         : (per <= 1    ? k_route<T, 64, 1, BY_LOGIT>
-                            : per <= 2  ? k_route<T, 64, 2, BY_LOGIT>
-                            : per <= 4  ? k_route<T, 64, 4, BY_LOGIT>
-                            : per <= 8  ? k_route<T, 64, 8, BY_LOGIT>
-                            : per <= 16 ? k_route<T, 64, 16, BY_LOGIT>
-                                        : k_route<T, 64, 32, BY_LOGIT>);
+      return narrow ? (per <= 1    ? k_route<T, 8, 1, BY_LOGIT>
+                       : per <= 2  ? k_route<T, 8, 2, BY_LOGIT>
+                       : per <= 4  ? k_route<T, 8, 4, BY_LOGIT>
+                       : per <= 8  ? k_route<T, 8, 8, BY_LOGIT>
+                       : per <= 16 ? k_route<T, 8, 16, BY_LOGIT>
+                                   : k_route<T, 8, 32, BY_LOGIT>)
+                    : (per <= 1    ? k_route<T, 64, 1, BY_LOGIT>
+                       : per <= 2  ? k_route<T, 64, 2, BY_LOGIT>
+                       : per <= 4  ? k_route<T, 64, 4, BY_LOGIT>
+                       : per <= 8  ? k_route<T, 64, 8, BY_LOGIT>
+                       : per <= 16 ? k_route<T, 64, 16, BY_LOGIT>
+                                   : k_route<T, 64, 32, BY_LOGIT>);
     };
     hipLaunchKernelGGL((bias || groups > 1 ? kernel.template operator()<false>() : kernel.template operator()<true>()), grid, dim3(256), 0,
                        (hipStream_t)stream, a);

@@ -25,14 +25,13 @@ struct RouteArgs {
 
 __device__ __forceinline__ float exp_below(float d) { return __builtin_amdgcn_exp2f(d * 1.44269504f); }     // d <= 0; NaN stays NaN
 
-// Lane l ^ S of every sixteen lanes.
+// Lane l ^ S of every eight lanes.
 template <int S>
 __device__ __forceinline__ float lane_xor(float v) {
-  static_assert(S > 0 && S < 16, "of sixteen lanes");
-  constexpr int h = S < 8 ? S : S ^ 15, q = h < 4 ? h : h ^ 7, perm = (0 ^ q) | (1 ^ q) << 2 | (2 ^ q) << 4 | (3 ^ q) << 6;
+  static_assert(S > 0 && S < 8, "of eight lanes");
+  constexpr int q = S < 4 ? S : S ^ 7, perm = (0 ^ q) | (1 ^ q) << 2 | (2 ^ q) << 4 | (3 ^ q) << 6;
   int x = __float_as_int(v);
-  if (S >= 8) x = __builtin_amdgcn_update_dpp(0, x, 0x140, 0xf, 0xf, false);          // row_mirror: lane ^ 15
-  if (h >= 4) x = __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false);          // row_half_mirror: lane ^ 7
+  if (S >= 4) x = __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false);          // row_half_mirror: lane ^ 7
   if (q) x = __builtin_amdgcn_update_dpp(0, x, perm, 0xf, 0xf, false);
   return __int_as_float(x);
 }
@@ -42,9 +41,8 @@ __device__ __forceinline__ float team_fold(float v, F f) {
   v = f(v, lane_xor<1>(v));
   v = f(v, lane_xor<2>(v));
   v = f(v, lane_xor<7>(v));
-  if (TEAM >= 16) v = f(v, lane_xor<15>(v));
 #pragma unroll
-  for (int s = 16; s < TEAM; s *= 2) v = f(v, __shfl_xor(v, s));
+  for (int s = 8; s < TEAM; s *= 2) v = f(v, __shfl_xor(v, s));
   return v;
 }
 template <int TEAM>
@@ -52,8 +50,7 @@ __device__ __forceinline__ uint32_t team_max_u32(uint32_t v) {
   if (TEAM == 64) return wave_max_u32(v);
   v = wave_max_step32<0xB1, 0xf>(v);
   v = wave_max_step32<0x4E, 0xf>(v);
-  v = wave_max_step32<0x141, 0xf>(v);
-  return TEAM == 16 ? wave_max_step32<0x140, 0xf>(v) : v;
+  return wave_max_step32<0x141, 0xf>(v);
 }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
@@ -116,8 +113,10 @@ __device__ __forceinline__ void route_row(const RouteArgs& a, int64_t row, doubl
     sum += x;
     if (!by_logit) c[e] = v == -INFINITY ? v : a.sigmoid ? 1.0 / (1.0 + x) : x;
   }
+  if (!a.sigmoid) {
 #pragma unroll
-  for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s);
+    for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s);
+  }
   double m1 = -INFINITY, m2 = -INFINITY;                   // the lane's, then the group's two largest
 #pragma unroll 4
   for (int e = begin; e < end && !by_logit; e += step) {
@@ -183,7 +182,7 @@ __device__ __forceinline__ void load_run(const T* p, int count, int there, float
   }
 }
 
-// The N (a power of two up to 16) keys of a lane in descending order, the nine largest of them.
+// The N (a power of two up to 32) keys of a lane in descending order, the nine largest of them.
 __device__ __forceinline__ void order(uint32_t& a, uint32_t& b) {
   const uint32_t high = max(a, b);
   b = min(a, b);
@@ -199,7 +198,29 @@ __device__ __forceinline__ void sort_8(uint32_t (&k)[8]) {            // Batcher
 }
 template <int N>
 __device__ __forceinline__ void sort_keys(const uint32_t (&key)[N], uint32_t (&list)[10]) {
-  if constexpr (N == 16) {
+  if constexpr (N == 32) {
+    uint32_t half[16], other[10] = {};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) half[i] = key[i];
+    sort_keys<16>(half, list);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) half[i] = key[16 + i];
+    sort_keys<16>(half, other);
+    uint32_t ninth = max(list[8], other[8]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = list[i], b = list[7 - i];
+      ninth = max(ninth, max(min(a, other[7 - i]), min(b, other[i])));
+      list[i] = max(a, other[7 - i]);
+      list[7 - i] = max(b, other[i]);
+    }
+#pragma unroll
+    for (int s = 4; s > 0; s /= 2)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (!(i & s)) order(list[i], list[i + s]);
+    list[8] = ninth;
+  } else if constexpr (N == 16) {
     uint32_t a[8], b[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -240,16 +261,18 @@ __device__ __forceinline__ void sort_keys(const uint32_t (&key)[N], uint32_t (&l
   }
 }
 
-// Rows by teams of 8 or 16 lanes (up to 128 or 256 experts, 8 of a row, 8 groups) or of 64, in 32 bits where that decides, else by route_row.
+// Rows by teams of 8 lanes (up to 256 experts, 8 of a row, 8 groups) or of 64, in 32 bits where that decides, else by route_row.
 //   c is computed in float32, with a bound `off` of its error.  Every expert gets a key of 31 bits, its c as a whole number of 23 bits between a bound that
 //   the `top` largest c are above and the largest c, and 2^8 or 2^10 less its number, so that keys are different and the larger one of equal c is that
 //   of the lower number.  Each lane sorts its keys, and a round pops the largest of the lanes' first ones; where a lane may have more than nine to give
 //   (teams of 64), a round takes the largest key below the one before, of differences in 32 bits the largest.  A row is settled where all of its
-//   chosen keys and the next one are further apart than the errors can be, or two
-//   chosen ones belong to the same logit and bias; groups likewise.  The others, rows that end early and rows with logits that are no numbers are few, and are taken by the whole
-//   wavefront in 64 bits.
+//   chosen keys and the next one are further apart than the errors can be, or two chosen ones belong to the same logit and bias; groups likewise.  The
+//   others, rows that end early and rows with logits that are no numbers are few (a thousandth of rows of 256 experts); each wavefront takes its own in
+//   64 bits when it is through, some 6 us a row.
+// Bound by vector instructions in teams of 8 (262144 rows of 256 float32: by logits 60 us, 4.8 TB/s; sigmoid and bias 104, with 4 of 8 groups 127; a
+// wavefront to a row in 64 bits 640), whose lanes share what a row costs besides its experts: teams of 16 took 73, 108 and 137.
 template <typename T, int TEAM, int PER, bool BY_LOGIT>
-__global__ __launch_bounds__(256, TEAM < 64 ? 4 : 2) void k_route(RouteArgs a) {
+__global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 4) void k_route(RouteArgs a) {
   constexpr int ROWS = 64 / TEAM, BITS = TEAM < 64 ? 8 : 10, LAST = (1 << BITS) - 1, FIELD = 31 - BITS;
   constexpr int V = PER < kPiece<T> ? 1 : kPiece<T>;                  // experts that lie next to each other
   constexpr float U = 0x1p-24f, kTop = (float)(1 << FIELD);
@@ -378,8 +401,7 @@ __global__ __launch_bounds__(256, TEAM < 64 ? 4 : 2) void k_route(RouteArgs a) {
         if (lanes > 1) join(lane_xor<1>(g1), lane_xor<1>(g2));
         if (lanes > 2) join(lane_xor<2>(g1), lane_xor<2>(g2));
         if (lanes > 4) join(lane_xor<7>(g1), lane_xor<7>(g2));
-        if (lanes > 8) join(lane_xor<15>(g1), lane_xor<15>(g2));
-        for (int s = 16; s < lanes; s *= 2) {
+        for (int s = 8; s < lanes; s *= 2) {
           const float o1 = __shfl_xor(g1, s), o2 = __shfl_xor(g2, s);
           join(o1, o2);
         }
@@ -394,16 +416,6 @@ __global__ __launch_bounds__(256, TEAM < 64 ? 4 : 2) void k_route(RouteArgs a) {
             against.template operator()<2>(); against.template operator()<6>();
           }
           if (lanes <= 4) against.template operator()<4>();
-          if constexpr (TEAM == 16) {
-            if (lanes == 1) {
-              against.template operator()<9>(); against.template operator()<11>(); against.template operator()<13>(); against.template operator()<15>();
-            }
-            if (lanes <= 2) {
-              against.template operator()<10>(); against.template operator()<14>();
-            }
-            if (lanes <= 4) against.template operator()<12>();
-            if (lanes <= 8) against.template operator()<8>();
-          }
         } else {
           for (int h = 0; h < a.groups; ++h) before += __shfl(value, h * lanes) > value;
         }
