@@ -266,9 +266,9 @@ __device__ __forceinline__ void sort_keys(const uint32_t (&key)[N], uint32_t (&l
 //   the `top` largest c are above and the largest c, and 2^8 or 2^10 less its number, so that keys are different and the larger one of equal c is that
 //   of the lower number.  Each lane sorts its keys, and a round pops the largest of the lanes' first ones; where a lane may have more than nine to give
 //   (teams of 64), a round takes the largest key below the one before, of differences in 32 bits the largest.  A row is settled where all of its
-//   chosen keys and the next one are further apart than the errors can be, or two chosen ones belong to the same logit and bias; groups likewise.  The
-//   others, rows that end early and rows with logits that are no numbers are few (a thousandth of rows of 256 experts); each wavefront takes its own in
-//   64 bits when it is through, some 6 us a row.
+//   chosen keys and the next one are further apart than the errors can be, or where those that are not prove to be in order when they are compared in
+//   64 bits; groups that are close leave it open.  Rows left open, rows that end early and rows with logits that are no numbers are few (of 256 experts
+//   some 3 in 10000); each wavefront takes its own in 64 bits when it is through, some 6 us a row.
 // Bound by vector instructions in teams of 8 (262144 rows of 256 float32: by logits 60 us, 4.8 TB/s; sigmoid and bias 104, with 4 of 8 groups 127; a
 // wavefront to a row in 64 bits 640), whose lanes share what a row costs besides its experts: teams of 16 took 73, 108 and 137.
 template <typename T, int TEAM, int PER, bool BY_LOGIT>
@@ -364,8 +364,8 @@ __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 
     float off = 0.f;
     if constexpr (!BY_LOGIT) {
       if (a.sigmoid) {
-        // exp2 of a rounded product, 1 + it, its reciprocal: 5 u
-        off = 8.f * U;
+        // with e = exp(-z) s is off by s (1 - s) (0.85 |z log2(e)| + 2) u for the rounded product and exp2, 3 s u for 1 + e and its reciprocal
+        off = 4.f * U;
         auto score = [](float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504f)); };
         if (__any(low == -INFINITY)) {                                // experts that are not there, for some lane of the wavefront
 #pragma unroll
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 
 #pragma unroll
         for (int i = 0; i < PER; ++i) c[i] += biases[i / V][t][i % V];
       }
-      off += 2.f * U * (1.f + bias_size);
+      off += U * (1.f + bias_size);
       m1 = -INFINITY;
       if (a.groups > 1) {
 #pragma unroll
@@ -442,7 +442,7 @@ __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 
       for (int i = 0; i < PER; ++i) {
         const int x = __float_as_int(c[i] + 0.f);
         const uint32_t rank = (uint32_t)(x ^ (x >> 31 | INT32_MIN)) >> 16;
-        key[i] = c[i] == -INFINITY ? 0u : (rank << BITS) + low_bits(i);
+        key[i] = (c[i] == -INFINITY ? 0u : rank << BITS) + low_bits(i);
       }
     } else {
       // a bound that `top` experts reach: each lane's largest c, or its two largest ones, where enough lanes have them
@@ -461,41 +461,62 @@ __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 
         if (TEAM == 64) key[i] &= 0x7fffffffu;
       }
     }
-    uint32_t last = 0x80000000u, mine = 0;
+    // lane j has the j-th key; `next` is the one behind the chosen ones, `last` the one behind that
+    uint32_t last = 0x80000000u, mine = 0, next = 0;
     if constexpr (TEAM < 64) {
       // the lane's keys in order, as far as they can be among the `top` and the one behind: a round pops the largest of the lanes' first
       uint32_t list[10] = {};
       sort_keys<PER>(key, list);
-      for (int j = 0; j <= a.top; ++j) {
+      for (int j = 0; j <= a.top + 1; ++j) {
         last = team_max_u32<TEAM>(list[0]);
         if (t == j) mine = last;
+        if (j == a.top) next = last;
         const bool mine_was = list[0] == last;
 #pragma unroll
         for (int i = 0; i < (PER < 9 ? PER : 9); ++i) list[i] = mine_was ? list[i + 1] : list[i];
         if (j < a.top) settled &= last >> BITS != 0;
       }
-      if (last >> BITS == 0) last = 0;
+      settled &= PER < 10 || list[0] != 0;                            // (nine from one lane: it may have had more)
     } else {
-      for (int j = 0; j <= a.top; ++j) {
-        uint32_t next = 0;
+      for (int j = 0; j <= a.top + 1; ++j) {
+        uint32_t below = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) next = max(next, key[i] - last);
-        next = team_max_u32<TEAM>(next);
-        last = next & 0x80000000u ? next + last : 0;                  // 0: there is none
-        if ((last >> BITS) == 0) last = 0;
+        for (int i = 0; i < PER; ++i) below = max(below, key[i] - last);
+        below = team_max_u32<TEAM>(below);
+        last = below & 0x80000000u ? below + last : 0;                // 0: there is none
         if (t == j) mine = last;
-        if (j < a.top) settled &= last != 0;
+        if (j == a.top) next = last;
+        if (j < a.top) settled &= last >> BITS != 0;
       }
     }
-    // lane j has the j-th key; `last` is the one behind the chosen ones
+    const uint32_t none = (1u << BITS) - 1;                           // keys up to there are of no expert
     uint32_t after = (uint32_t)__shfl_down((int)mine, 1, TEAM);
-    if (t == a.top - 1) after = last;
-    const bool chosen = t < a.top && mine != 0;
+    if (t == a.top - 1) after = next;
+    const bool chosen = t < a.top && mine > none;
     const int e = LAST - (int)(mine & LAST), ea = LAST - (int)(after & LAST);
     const float zc = chosen ? to_float(z[e]) : -INFINITY;
-    if (chosen && after != 0 && (int)(mine >> BITS) - (int)(after >> BITS) <= apart) {
-      const float za = to_float(z[ea]);
-      settled &= t < a.top - 1 && za == zc && (!a.bias || a.bias[e] == a.bias[ea]);
+    const bool close = chosen && after > none && (int)(mine >> BITS) - (int)(after >> BITS) <= apart;
+    if (__any(close)) {
+      // neighbours that are close are compared in 64 bits; the last chosen one has to be apart from the key behind the next one as well
+      bool right = t < a.top - 1 || last <= none || (int)(mine >> BITS) - (int)(last >> BITS) > apart;
+      if (close) {
+        const float za = to_float(z[ea]);
+        if constexpr (BY_LOGIT) {
+          right &= zc > za || (zc == za && e < ea);
+        } else {
+          const double bc = a.bias ? (double)a.bias[e] : 0.0, ba = a.bias ? (double)a.bias[ea] : 0.0;
+          const double xc = exp(a.sigmoid ? -(double)zc : (double)zc - from), xa = exp(a.sigmoid ? -(double)za : (double)za - from);
+          if (a.sigmoid) {
+            const double cc = 1.0 / (1.0 + xc) + bc, ca = 1.0 / (1.0 + xa) + ba;
+            right &= cc > ca || (cc == ca && e < ea);
+          } else {
+            // the sum of all is one of 32 bits: twice its error, of the difference
+            const double d = (xc - xa) / total, sure = d + (bc - ba) - 256.0 * 0x1p-24 * fabs(d);
+            right &= sure > 0.0 || (zc == za && bc == ba && e < ea);
+          }
+        }
+        settled &= right;
+      }
     }
     const float w = chosen_weight<TEAM>(zc, a.sigmoid, a.renormalize, from, total);
     const unsigned long long open = __ballot(!settled);

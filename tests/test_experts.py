@@ -157,7 +157,8 @@ def check_route(torch, ops, z, top, sigmoid=False, bias=None, groups=1, top_grou
 
 
 ROUTE_SIZES = [(1, 1, 1), (1, 64, 6), (3, 2, 2), (5, 7, 3), (130, 8, 8), (33, 60, 4), (17, 64, 8), (9, 65, 1), (40, 128, 8), (21, 200, 5), (65, 256, 8),
-               (4, 256, 32), (5, 257, 9), (3, 500, 16), (4, 1000, 8), (3, 1024, 32), (2100, 16, 2)]
+               (4, 256, 32), (5, 257, 9), (3, 500, 16), (4, 1000, 8), (3, 1024, 32), (2100, 1, 1), (2100, 5, 3), (2100, 8, 8), (2100, 16, 2), (2100, 30, 4),
+               (2100, 64, 8), (2101, 100, 7), (2100, 200, 8), (2100, 256, 8), (2100, 255, 1)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -177,7 +178,9 @@ def test_route(gpu, ops, n, experts, top, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,experts,groups,top_groups,top", [
     (1, 64, 8, 4, 6), (33, 64, 8, 4, 8), (21, 256, 8, 4, 8), (40, 60, 4, 2, 5), (9, 60, 3, 1, 7), (17, 63, 7, 3, 8), (5, 64, 64, 5, 5), (3, 1024, 64, 9, 32),
-    (4, 1023, 33, 4, 8), (6, 1020, 17, 5, 9), (7, 1023, 3, 2, 8), (11, 6, 2, 2, 6), (30, 40, 5, 5, 3), (25, 24, 8, 3, 4), (50, 16, 2, 1, 8)])
+    (4, 1023, 33, 4, 8), (6, 1020, 17, 5, 9), (7, 1023, 3, 2, 8), (11, 6, 2, 2, 6), (30, 40, 5, 5, 3), (25, 24, 8, 3, 4), (50, 16, 2, 1, 8),
+    (2100, 256, 8, 4, 8), (2101, 60, 4, 2, 5), (2100, 128, 2, 1, 3), (2100, 40, 5, 3, 8), (2100, 96, 6, 2, 7), (2100, 8, 8, 5, 4), (2100, 24, 3, 2, 8),
+    (2100, 12, 2, 1, 6)])
 def test_route_by_groups(gpu, ops, n, experts, groups, top_groups, top, dtype):
     torch, _ = gpu
     t = dtype_of(torch, dtype)
@@ -191,13 +194,14 @@ def test_route_by_groups(gpu, ops, n, experts, groups, top_groups, top, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("experts,top", [(8, 4), (60, 8), (256, 8), (500, 6)])
-def test_route_of_masked_and_equal_logits(gpu, ops, experts, top, dtype):
+@pytest.mark.parametrize("rows", [40, 2100])
+@pytest.mark.parametrize("experts,top", [(8, 4), (60, 8), (100, 8), (256, 8), (500, 6)])
+def test_route_of_masked_and_equal_logits(gpu, ops, experts, top, rows, dtype):
     torch, _ = gpu
     t = dtype_of(torch, dtype)
     rng = np.random.default_rng(experts)
     lowest = torch.finfo(t).min
-    z = torch.from_numpy(np.round(rng.standard_normal((40, experts)))).to(t)      # many equal ones
+    z = torch.from_numpy(np.round(rng.standard_normal((rows, experts)))).to(t)    # many equal ones
     z[0] = -INF                                            # no expert at all
     z[1, :] = -INF
     z[1, experts - 1] = -3.0                               # a single one
@@ -222,19 +226,19 @@ def test_route_of_masked_and_equal_logits(gpu, ops, experts, top, dtype):
                 assert_within(torch, weight[some].sum(1), torch.ones(int(some.sum()), dtype=torch.float64, device=DEV),
                               torch.full((int(some.sum()),), 100 * U, dtype=torch.float64, device=DEV), "sum of weights")
     # scores that are equal in 64 bits (sigmoids of 40 and more are 1) go by number, with a bias by the bias
-    z = torch.full((2, experts), 50.0, dtype=t, device=DEV)
+    z = torch.full((rows, experts), 50.0, dtype=t, device=DEV)
     bias = torch.zeros(experts, device=DEV)
     expert, _ = run_route(torch, ops, z, top, sigmoid=True, bias=bias)
-    assert expert.tolist() == [list(range(top))] * 2
+    assert expert.tolist() == [list(range(top))] * rows
     bias[experts - 1] = 2.0 ** -40
     expert, _ = run_route(torch, ops, z, top, sigmoid=True, bias=bias)
     assert expert[0].tolist() == [experts - 1] + list(range(top - 1))
 
 
-def test_route_decides_what_float32_cannot(gpu, ops):
+@pytest.mark.parametrize("n,experts,top", [(600, 64, 6), (2100, 64, 6), (2100, 200, 8)])
+def test_route_decides_what_float32_cannot(gpu, ops, n, experts, top):
     """Scores whose differences are far below a step of float32: biases and logits that all but cancel."""
     torch, _ = gpu
-    n, experts, top = 600, 64, 6
     rng = np.random.default_rng(5)
     z = torch.from_numpy(rng.standard_normal((n, experts)) * 1e-4).float()
     bias = torch.from_numpy(rng.standard_normal(experts) * 1e-9).float().to(DEV)
@@ -248,6 +252,16 @@ def test_route_decides_what_float32_cannot(gpu, ops):
     far = torch.from_numpy(rng.standard_normal((n, experts)) * 1e30).float().to(DEV)
     expert, _ = run_route(torch, ops, far, top, sigmoid=True)
     assert torch.equal(expert.long(), route_by_definition(torch, far.double(), top, True, None, 1, 1))
+    # a few experts far above the others, all of them with one lane
+    lift = torch.zeros(n, experts)
+    lift[:, :32] += 8.0
+    check_route(torch, ops, (torch.from_numpy(rng.standard_normal((n, experts))).float() + lift).to(DEV), top)
+    lift[:, 8:] = 0.0
+    check_route(torch, ops, (torch.from_numpy(rng.standard_normal((n, experts))).float() + lift).to(DEV), top, sigmoid=True, bias=bias)
+    # logits that differ by a step or two of float32, and some that are equal
+    steps = torch.from_numpy(rng.integers(0, 3, (n, experts))).float() * 2.0 ** -23
+    check_route(torch, ops, (1.0 + steps).to(DEV), top, sigmoid=True, bias=bias)
+    check_route(torch, ops, (1.0 + steps).to(DEV), top, bias=bias)
     # biases of a size at which a score is lost in float32
     big = torch.from_numpy(np.repeat([1e6, -1e6], experts // 2)).float().to(DEV)
     check_route(torch, ops, torch.from_numpy(rng.standard_normal((n, experts))).float().to(DEV), top, sigmoid=True, bias=big)
@@ -256,18 +270,19 @@ def test_route_decides_what_float32_cannot(gpu, ops):
 def test_route_reports_logits_that_are_no_numbers(gpu):
     torch, binding = gpu
     o = binding.Ops()
-    for experts in (8, 64, 256, 1000):
+    for rows, experts in ((9, 8), (9, 64), (9, 256), (9, 1000), (2100, 8), (2100, 100), (2100, 256)):
         for value in (math.nan, INF):
-            z = torch.randn(9, experts, device=DEV)
-            clean, _ = run_route(torch, o, z, 4)
-            z[4, experts // 2] = value
-            expert, weight = run_route(torch, o, z, 4)
-            with pytest.raises(binding.SneakPeekError):
+            for kw in (dict(), dict(sigmoid=True, bias=torch.randn(experts, device=DEV)), dict(groups=2, top_groups=1)):
+                z = torch.randn(rows, experts, device=DEV)
+                clean, _ = run_route(torch, o, z, 4, **kw)
+                z[4, experts // 2] = value
+                expert, weight = run_route(torch, o, z, 4, **kw)
+                with pytest.raises(binding.SneakPeekError):
+                    o.sp_ops_check()
                 o.sp_ops_check()
-            o.sp_ops_check()
-            assert bool((expert[4] == -1).all()) and bool((weight[4] == 0).all())
-            rest = torch.arange(9) != 4
-            assert torch.equal(expert[rest.to(DEV)], clean[rest.to(DEV)])
+                assert bool((expert[4] == -1).all()) and bool((weight[4] == 0).all())
+                rest = (torch.arange(rows) != 4).to(DEV)
+                assert torch.equal(expert[rest], clean[rest])
     o.close()
 
 
