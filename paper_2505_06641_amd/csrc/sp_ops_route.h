@@ -57,7 +57,7 @@ __device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b);
 // NaN if either is.
 __device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// exp(d), to 3 u: the product with log2(e) in two parts, the second of which exp2 does not get.
+// exp(d) for d <= 0, to 3 u: the product with log2(e) in two parts, the second of which exp2 does not get.
 __device__ __forceinline__ float exp_near(float d) {
   const float p = d * 1.44269502f;
   float r = fmaf(d, 1.44269502f, -p);
@@ -349,6 +349,7 @@ __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 
     float m1 = high, m2 = -INFINITY;                                  // the lane's two largest c
     high = team_fold<TEAM>(high, maximum);
     const float from = high == -INFINITY ? 0.f : high;
+    const bool empty = high == -INFINITY;
     bool settled = high < INFINITY;                                   // (NaN and inf: no)
     float total = 1.f;
     if (!a.sigmoid && (!a.renormalize || !BY_LOGIT)) {
@@ -519,11 +520,12 @@ __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 
       }
     }
     const float w = chosen_weight<TEAM>(zc, a.sigmoid, a.renormalize, from, total);
+    // (a row without any expert is settled too: there may be many where a batch is padded)
     const unsigned long long open = __ballot(!settled);
-    const bool mine_open = (open & mates) != 0;
+    const bool mine_open = !empty && (open & mates) != 0;
     if (in && t < a.top && !mine_open) {
-      a.expert[row * a.top + t] = e;
-      a.weight[row * a.top + t] = a.scale * w;
+      a.expert[row * a.top + t] = empty ? -1 : e;
+      a.weight[row * a.top + t] = empty ? 0.f : a.scale * w;
     }
     const unsigned long long heads = __ballot(in && t == 0 && mine_open);
     if (heads) {
@@ -585,11 +587,14 @@ __global__ __launch_bounds__(256) void k_route_back(int n, int experts, int top,
     }
     const float share = chosen_weight<TEAM>(zc, sigmoid, renormalize, from, total);         // of the scale
     const float dot = renormalize || all ? team_sum<TEAM>(e >= 0 ? dw * share : 0.f, nullptr) : 0.f;
-    const float by = __builtin_amdgcn_rcpf(total);
+    const float by = total > 0.f ? __builtin_amdgcn_rcpf(total) : 0.f;
     float mine = dw;                                       // what the chosen expert's logit gets (softmax: what its score gets)
     if (!all) {
       mine = share * (dw - dot);
-      if (sigmoid) mine *= __builtin_amdgcn_rcpf(1.f + exp_near(zc));                       // 1 - s
+      if (sigmoid) {                                       // 1 - s
+        const float x = exp_near(-fabsf(zc));
+        mine *= (zc > 0.f ? x : 1.f) * __builtin_amdgcn_rcpf(1.f + x);
+      }
     }
     // What the others need of it goes through the team's own part of LDS: a wavefront's, which nobody else waits for.
     const unsigned long long mates = TEAM == 64 ? ~0ull : ((1ull << (TEAM & 63)) - 1) << (threadIdx.x % 64 / TEAM * TEAM);

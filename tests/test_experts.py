@@ -203,6 +203,7 @@ def test_route_of_masked_and_equal_logits(gpu, ops, experts, top, rows, dtype):
     lowest = torch.finfo(t).min
     z = torch.from_numpy(np.round(rng.standard_normal((rows, experts)))).to(t)    # many equal ones
     z[0] = -INF                                            # no expert at all
+    z[20:30] = -INF
     z[1, :] = -INF
     z[1, experts - 1] = -3.0                               # a single one
     z[2, :] = 0.0                                          # all equal
@@ -334,6 +335,34 @@ def test_route_backward(gpu, ops, n, experts, top, dtype):
         assert_within(torch, dz, want, bound, ("dz", sigmoid, renormalize))
         if n > 2:
             assert bool((dz[1] == 0).all())
+
+
+def test_route_backward_of_far_logits(gpu, ops):
+    """Scores that are 0 or 1 in float32 and softmaxes of a single expert: finite gradients, 0 where the score does not move."""
+    torch, _ = gpu
+    z = torch.tensor([[100.0, -100.0, 90.0, 3e38, -3e38, 0.0, 88.8, -88.8], [200.0, 199.0, -1e4, 0.0, 1.0, 2.0, 3.0, 4.0], [-500.0] * 8, [700.0] * 8], device=DEV)
+    expert = torch.tensor([[3, 0, 1, 4], [0, 1, 2, 7], [0, 1, 2, 3], [4, 5, 6, 7]], dtype=torch.int32, device=DEV)
+    dw = torch.tensor([[1.0, -2.0, 3.0, 0.5]] * 4, device=DEV)
+    for sigmoid in (False, True):
+        for renormalize in (False, True):
+            dz = torch.full_like(z, math.nan)
+            ops.sp_route_backward(z, expert, dw, dz, sigmoid=sigmoid, renormalize=renormalize)
+            zd = z.double().gather(1, expert.long())
+            if renormalize:
+                part = torch.nn.functional.logsigmoid(zd) if sigmoid else zd
+                w = torch.softmax(part, 1)
+                got = w * (dw.double() - (w * dw.double()).sum(1, keepdim=True))
+                if sigmoid:
+                    got = got * torch.sigmoid(-zd)
+                want = torch.zeros_like(z, dtype=torch.float64).scatter_add(1, expert.long(), got)
+            elif sigmoid:
+                want = torch.zeros_like(z, dtype=torch.float64).scatter_add(1, expert.long(), dw.double() * torch.sigmoid(zd) * torch.sigmoid(-zd))
+            else:
+                p = torch.softmax(z.double(), 1)
+                up = torch.zeros_like(p).scatter_add(1, expert.long(), dw.double())
+                want = p * (up - (p * up).sum(1, keepdim=True))
+            # |dw| add up to 6.5; scores and shares of far logits are off by less than 100 u
+            assert_within(torch, dz, want, torch.full_like(want, 100 * U * 6.5), (sigmoid, renormalize))
 
 
 def test_route_backward_against_differences(gpu, ops):
