@@ -526,7 +526,7 @@ typedef enum { SP_SCORE_SOFTMAX = 0, SP_SCORE_SIGMOID = 1 } sp_score_kind;
  * top_groups groups of the largest values stay in.  Of their experts the `top` of the largest c are chosen, in that order; ties go to the lowest
  * number, of groups and experts.  c are compared in 64 bits; without a bias and groups the logits themselves are compared.
  *   weight_j = scale s_j, or scale s_j / (sum of the chosen s) with renormalize
- *   logits [n, experts] dtype      bias [experts] float or NULL (it has no gradient: who balances sets it)
+ *   logits [n, experts] dtype      bias [experts] float or NULL (it has no gradient: who balances sets it); -inf or NaN keeps an expert out
  *   expert int32 [n, top], weight float [n, top], contiguous; top_groups * (experts / groups) >= top
  * A logit of -inf is an expert that is not there.  Where fewer than `top` can be chosen the rest is -1 with weight 0: a row of -inf has no
  * expert.  A logit of NaN or +inf is bad data (sp_ops_check), and its row gets no expert. */

@@ -122,6 +122,7 @@ __device__ __forceinline__ void route_row(const RouteArgs& a, int64_t row, doubl
   for (int e = begin; e < end && !by_logit; e += step) {
     double s = a.sigmoid ? c[e] : c[e] / sum;
     if (a.bias) s += (double)a.bias[e];
+    if (s != s) s = -INFINITY;                             // (a bias that is no number)
     c[e] = s;
     m2 = fmax(m2, fmin(m1, s));
     m1 = fmax(m1, s);
@@ -266,14 +267,15 @@ __device__ __forceinline__ void sort_keys(const uint32_t (&key)[N], uint32_t (&l
 }
 
 // Rows by teams of 8 lanes (up to 256 experts, 8 of a row, 8 groups) or of 64, in 32 bits where that decides, else by route_row.
-//   c is computed in float32, with a bound `off` of its error.  Every expert gets a key of 31 bits, its c as a whole number of 23 bits between a bound that
-//   the `top` largest c are above and the largest c, and 2^8 or 2^10 less its number, so that keys are different and the larger one of equal c is that
-//   of the lower number.  Each lane sorts its keys, and a round pops the largest of the lanes' first ones; where a lane may have more than nine to give
+//   c is computed in float32, with a bound `off` of its error.  Every expert gets a key of 31 bits, its c as a whole number of 23 (21) bits between a
+//   bound that the `top` largest c are above and the largest c, and 2^8 (2^10) less its number, so that keys are different and the larger one of equal
+//   c is that of the lower number.
+//   Each lane sorts its keys, and a round pops the largest of the lanes' first ones; where a lane may have more than nine to give
 //   (teams of 64), a round takes the largest key below the one before, of differences in 32 bits the largest.  A row is settled where all of its
 //   chosen keys and the next one are further apart than the errors can be, or where those that are not prove to be in order when they are compared in
 //   64 bits; groups that are close leave it open.  Rows left open, rows that end early and rows with logits that are no numbers are few (of 256 experts
 //   some 3 in 10000); each wavefront takes its own in 64 bits when it is through, some 6 us a row.
-// Bound by vector instructions in teams of 8 (262144 rows of 256 float32: by logits 60 us, 4.8 TB/s; sigmoid and bias 104, with 4 of 8 groups 127; a
+// Bound by vector instructions in teams of 8 (262144 rows of 256 float32: by logits 59 us, 4.9 TB/s; sigmoid and bias 97, with 4 of 8 groups 121; a
 // wavefront to a row in 64 bits 640), whose lanes share what a row costs besides its experts: teams of 16 took 73, 108 and 137.
 template <typename T, int TEAM, int PER, bool BY_LOGIT>
 __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 4) void k_route(RouteArgs a) {
@@ -301,245 +303,246 @@ __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 
 #pragma unroll 1
       for (int h = 0; h < V; ++h) {
         const bool is = h < count(p * V);
-        const float b = is ? a.bias[number(p * V) + h] : 0.f;
+        float b = is ? a.bias[number(p * V) + h] : 0.f;
+        if (b != b) b = -INFINITY;                                    // (no number in a maximum or a median)
         if (threadIdx.x < TEAM) biases[p][t][h] = b;
-        if (is) {
+        if (is && b > -INFINITY) {                                    // (-inf: so is c, whatever the score)
           bias_low = fminf(bias_low, b);
           bias_high = fmaxf(bias_high, b);
         }
       }
     bias_low = team_fold<TEAM>(bias_low, smaller);
     bias_high = team_fold<TEAM>(bias_high, larger);
-    bias_size = fmaxf(fabsf(bias_low), fabsf(bias_high));
+    bias_size = bias_low <= bias_high ? fmaxf(fabsf(bias_low), fabsf(bias_high)) : 0.f;
     __syncthreads();
   }
   int64_t base = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * ROWS;
   while (base < a.n) {
-  int kept = 0;
-  for (; base < a.n && kept <= kKept - ROWS; base += (int64_t)gridDim.x * 4 * ROWS) {
-    const int64_t row = base + team;
-    const bool in = row < a.n;
-    const T* z = (const T*)a.z + (in ? row : base) * a.z_stride;
-    const unsigned long long mates = TEAM == 64 ? ~0ull : ((1ull << (TEAM & 63)) - 1) << (team * TEAM);
-    asm volatile("" : "+v"(first), "+v"(left));                       // (else what follows from them is kept for all rows, in registers that are not there)
-    float c[PER];
-    float high = -INFINITY, low = INFINITY;
-    if (whole) {
-#pragma unroll
-      for (int i = 0; i < PER; i += V) {
-        if constexpr (V == 1) {
-          c[i] = to_float(z[number(i)]);
-        } else {
+    int kept = 0;
+    for (; base < a.n && kept <= kKept - ROWS; base += (int64_t)gridDim.x * 4 * ROWS) {
+      const int64_t row = base + team;
+      const bool in = row < a.n;
+      const T* z = (const T*)a.z + (in ? row : base) * a.z_stride;
+      const unsigned long long mates = TEAM == 64 ? ~0ull : ((1ull << (TEAM & 63)) - 1) << (team * TEAM);
+      asm volatile("" : "+v"(first), "+v"(left));                       // (else what follows from them is kept for all rows, in registers that are not there)
+      float c[PER];
+      float high = -INFINITY, low = INFINITY;
+      if (whole) {
+  #pragma unroll
+        for (int i = 0; i < PER; i += V) {
+          if constexpr (V == 1) {
+            c[i] = to_float(z[number(i)]);
+          } else {
+            float v[V];
+            load_piece(z + number(i), v);
+  #pragma unroll
+            for (int h = 0; h < V; ++h) c[i + h] = v[h];
+          }
+        }
+      } else {
+  #pragma unroll
+        for (int i = 0; i < PER; i += V) {
           float v[V];
-          load_piece(z + number(i), v);
-#pragma unroll
+          load_run(z, number(i), a.experts, count(i), v);
+  #pragma unroll
           for (int h = 0; h < V; ++h) c[i + h] = v[h];
         }
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < PER; i += V) {
-        float v[V];
-        load_run(z, number(i), a.experts, count(i), v);
-#pragma unroll
-        for (int h = 0; h < V; ++h) c[i + h] = v[h];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      high = maximum(high, c[i]);
-      low = fminf(low, c[i]);
-    }
-    float m1 = high, m2 = -INFINITY;                                  // the lane's two largest c
-    high = team_fold<TEAM>(high, maximum);
-    const float from = high == -INFINITY ? 0.f : high;
-    const bool empty = high == -INFINITY;
-    bool settled = high < INFINITY;                                   // (NaN and inf: no)
-    float total = 1.f;
-    if (!a.sigmoid && (!a.renormalize || !BY_LOGIT)) {
-      total = 0.f;
-#pragma unroll
+  #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const float e = exp_below(c[i] - from);
-        total += e;
-        if (!BY_LOGIT) c[i] = c[i] == -INFINITY ? -INFINITY : e;
+        high = maximum(high, c[i]);
+        low = fminf(low, c[i]);
       }
-      total = team_sum<TEAM>(total, nullptr);
-    }
-    float off = 0.f;
-    if constexpr (!BY_LOGIT) {
-      if (a.sigmoid) {
-        // with e = exp(-z) s is off by s (1 - s) (0.85 |z log2(e)| + 2) u for the rounded product and exp2, 3 s u for 1 + e and its reciprocal
-        off = 4.f * U;
-        auto score = [](float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504f)); };
-        if (__any(low == -INFINITY)) {                                // experts that are not there, for some lane of the wavefront
-#pragma unroll
-          for (int i = 0; i < PER; ++i) c[i] = c[i] == -INFINITY ? -INFINITY : score(c[i]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < PER; ++i) c[i] = score(c[i]);
-        }
-      } else {
-        // a term is off by (2.3 d + 3) e^-d u, the sum by less than (2.3 ln experts + 3 + 40) u of itself
-        const float by = __builtin_amdgcn_rcpf(total);
-        off = 72.f * U * by;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) c[i] *= by;
-      }
-      if (a.bias) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) c[i] += biases[i / V][t][i % V];
-      }
-      off += U * (1.f + bias_size);
-      m1 = -INFINITY;
-      if (a.groups > 1) {
-#pragma unroll
+      float m1 = high, m2 = -INFINITY;                                  // the lane's two largest c
+      high = team_fold<TEAM>(high, maximum);
+      const float from = high == -INFINITY ? 0.f : high;
+      const bool empty = high == -INFINITY;
+      bool settled = high < INFINITY;                                   // (NaN and inf: no)
+      float total = 1.f;
+      if (!a.sigmoid && (!a.renormalize || !BY_LOGIT)) {
+        total = 0.f;
+  #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          m2 = __builtin_amdgcn_fmed3f(m1, m2, c[i]);
-          m1 = fmaxf(m1, c[i]);
+          const float e = exp_below(c[i] - from);
+          total += e;
+          if (!BY_LOGIT) c[i] = c[i] == -INFINITY ? -INFINITY : e;
         }
-        float g1 = m1, g2 = m2;                                       // the group's
-        auto join = [&](float o1, float o2) {
-          g2 = fmaxf(fminf(g1, o1), fmaxf(g2, o2));
-          g1 = fmaxf(g1, o1);
-        };
-        if (lanes > 1) join(lane_xor<1>(g1), lane_xor<1>(g2));
-        if (lanes > 2) join(lane_xor<2>(g1), lane_xor<2>(g2));
-        if (lanes > 4) join(lane_xor<7>(g1), lane_xor<7>(g2));
-        for (int s = 8; s < lanes; s *= 2) {
-          const float o1 = __shfl_xor(g1, s), o2 = __shfl_xor(g2, s);
-          join(o1, o2);
-        }
-        const float value = g2 == -INFINITY ? g1 : g1 + g2;
-        int before = 0;                                               // groups of a larger value
-        if constexpr (TEAM < 64) {
-          auto against = [&]<int S>() { before += lane_xor<S>(value) > value; };
-          if (lanes == 1) {
-            against.template operator()<1>(); against.template operator()<3>(); against.template operator()<5>(); against.template operator()<7>();
+        total = team_sum<TEAM>(total, nullptr);
+      }
+      float off = 0.f;
+      if constexpr (!BY_LOGIT) {
+        if (a.sigmoid) {
+          // with e = exp(-z) s is off by s (1 - s) (0.85 |z log2(e)| + 2) u for the rounded product and exp2, 3 s u for 1 + e and its reciprocal
+          off = 4.f * U;
+          auto score = [](float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504f)); };
+          if (__any(low == -INFINITY)) {                                // experts that are not there, for some lane of the wavefront
+  #pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] = c[i] == -INFINITY ? -INFINITY : score(c[i]);
+          } else {
+  #pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] = score(c[i]);
           }
-          if (lanes <= 2) {
-            against.template operator()<2>(); against.template operator()<6>();
-          }
-          if (lanes <= 4) against.template operator()<4>();
         } else {
-          for (int h = 0; h < a.groups; ++h) before += __shfl(value, h * lanes) > value;
+          // a term is off by (2.3 d + 3) e^-d u, the sum by less than (2.3 ln experts + 3 + 40) u of itself
+          const float by = __builtin_amdgcn_rcpf(total);
+          off = 72.f * U * by;
+  #pragma unroll
+          for (int i = 0; i < PER; ++i) c[i] *= by;
         }
-        const bool stays = before < a.top_groups && value > -INFINITY;
-        const float least = team_fold<TEAM>(stays ? value : INFINITY, smaller), most = team_fold<TEAM>(stays ? -INFINITY : value, larger);
-        settled &= most == -INFINITY || least - most > 4.f * off + 8.f * U * (1.f + bias_size);
-        settled &= __popcll(__ballot(stays && sub == 0) & mates) <= a.top_groups;          // (more where values are equal)
-        if (!stays) {
-          m1 = m2 = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < PER; ++i) c[i] = -INFINITY;
+        if (a.bias) {
+  #pragma unroll
+          for (int i = 0; i < PER; ++i) c[i] += biases[i / V][t][i % V];
+        }
+        off += U * (1.f + bias_size);
+        m1 = -INFINITY;
+        if (a.groups > 1) {
+  #pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            m2 = __builtin_amdgcn_fmed3f(m1, m2, c[i]);
+            m1 = fmaxf(m1, c[i]);
+          }
+          float g1 = m1, g2 = m2;                                       // the group's
+          auto join = [&](float o1, float o2) {
+            g2 = fmaxf(fminf(g1, o1), fmaxf(g2, o2));
+            g1 = fmaxf(g1, o1);
+          };
+          if (lanes > 1) join(lane_xor<1>(g1), lane_xor<1>(g2));
+          if (lanes > 2) join(lane_xor<2>(g1), lane_xor<2>(g2));
+          if (lanes > 4) join(lane_xor<7>(g1), lane_xor<7>(g2));
+          for (int s = 8; s < lanes; s *= 2) {
+            const float o1 = __shfl_xor(g1, s), o2 = __shfl_xor(g2, s);
+            join(o1, o2);
+          }
+          const float value = g2 == -INFINITY ? g1 : g1 + g2;
+          int before = 0;                                               // groups of a larger value
+          if constexpr (TEAM < 64) {
+            auto against = [&]<int S>() { before += lane_xor<S>(value) > value; };
+            if (lanes == 1) {
+              against.template operator()<1>(); against.template operator()<3>(); against.template operator()<5>(); against.template operator()<7>();
+            }
+            if (lanes <= 2) {
+              against.template operator()<2>(); against.template operator()<6>();
+            }
+            if (lanes <= 4) against.template operator()<4>();
+          } else {
+            for (int h = 0; h < a.groups; ++h) before += __shfl(value, h * lanes) > value;
+          }
+          const bool stays = before < a.top_groups && value > -INFINITY;
+          const float least = team_fold<TEAM>(stays ? value : INFINITY, smaller), most = team_fold<TEAM>(stays ? -INFINITY : value, larger);
+          settled &= most == -INFINITY || least - most > 4.f * off + 8.f * U * (1.f + bias_size);
+          settled &= __popcll(__ballot(stays && sub == 0) & mates) <= a.top_groups;          // (more where values are equal)
+          if (!stays) {
+            m1 = m2 = -INFINITY;
+  #pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] = -INFINITY;
+          }
+        } else {
+  #pragma unroll
+          for (int i = 0; i < PER; ++i) m1 = fmaxf(m1, c[i]);
+        }
+        high = team_fold<TEAM>(m1, larger);
+      }
+      uint32_t key[PER];
+      int apart = -1;                                                   // keys that are no further apart settle nothing
+      if constexpr (sizeof(T) == 2 && BY_LOGIT) {
+        // bfloat16 logits: all 16 bits, in the order of the numbers (adding 0 makes -0 a 0)
+  #pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int x = __float_as_int(c[i] + 0.f);
+          const uint32_t rank = (uint32_t)(x ^ (x >> 31 | INT32_MIN)) >> 16;
+          key[i] = (c[i] == -INFINITY ? 0u : rank << BITS) + low_bits(i);
         }
       } else {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) m1 = fmaxf(m1, c[i]);
-      }
-      high = team_fold<TEAM>(m1, larger);
-    }
-    uint32_t key[PER];
-    int apart = -1;                                                   // keys that are no further apart settle nothing
-    if constexpr (sizeof(T) == 2 && BY_LOGIT) {
-      // bfloat16 logits: all 16 bits, in the order of the numbers (adding 0 makes -0 a 0)
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int x = __float_as_int(c[i] + 0.f);
-        const uint32_t rank = (uint32_t)(x ^ (x >> 31 | INT32_MIN)) >> 16;
-        key[i] = (c[i] == -INFINITY ? 0u : rank << BITS) + low_bits(i);
-      }
-    } else {
-      // a bound that `top` experts reach: each lane's largest c, or its two largest ones, where enough lanes have them
-      const int ones = __popcll(__ballot(m1 > -INFINITY) & mates), twos = __popcll(__ballot(m2 > -INFINITY) & mates);
-      const bool by_two = ones < a.top;
-      float bound = team_fold<TEAM>(by_two ? (m2 > -INFINITY ? m2 : INFINITY) : (m1 > -INFINITY ? m1 : INFINITY), smaller);
-      if (by_two && 2 * twos < a.top) bound = high - (BY_LOGIT ? 64.f : 1.f + (bias_high - bias_low));
-      const float range = fmaxf(high - bound + 4.f * off, 1e-30f), scale = (kTop - 32.f) * __builtin_amdgcn_rcpf(range);
-      const float shift = fmaf(-high, scale, 0x1p24f - 16.f);         // (its rounding moves all keys alike)
-      apart = 4 + (int)fminf(2.f * off * scale, kTop);
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        // below 2^24 a float32's steps are 1: the whole number stands in the low bits
-        const float f = __builtin_amdgcn_fmed3f(fmaf(c[i], scale, shift), 0x1p24f - kTop, 0x1p24f - 1.f);
-        key[i] = (__float_as_uint(f) << BITS) + low_bits(i);
-        if (TEAM == 64) key[i] &= 0x7fffffffu;
-      }
-    }
-    // lane j has the j-th key; `next` is the one behind the chosen ones, `last` the one behind that
-    uint32_t last = 0x80000000u, mine = 0, next = 0;
-    if constexpr (TEAM < 64) {
-      // the lane's keys in order, as far as they can be among the `top` and the one behind: a round pops the largest of the lanes' first
-      uint32_t list[10] = {};
-      sort_keys<PER>(key, list);
-      for (int j = 0; j <= a.top + 1; ++j) {
-        last = team_max_u32<TEAM>(list[0]);
-        if (t == j) mine = last;
-        if (j == a.top) next = last;
-        const bool mine_was = list[0] == last;
-#pragma unroll
-        for (int i = 0; i < (PER < 9 ? PER : 9); ++i) list[i] = mine_was ? list[i + 1] : list[i];
-        if (j < a.top) settled &= last >> BITS != 0;
-      }
-      settled &= PER < 10 || list[0] != 0;                            // (nine from one lane: it may have had more)
-    } else {
-      for (int j = 0; j <= a.top + 1; ++j) {
-        uint32_t below = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) below = max(below, key[i] - last);
-        below = team_max_u32<TEAM>(below);
-        last = below & 0x80000000u ? below + last : 0;                // 0: there is none
-        if (t == j) mine = last;
-        if (j == a.top) next = last;
-        if (j < a.top) settled &= last >> BITS != 0;
-      }
-    }
-    const uint32_t none = (1u << BITS) - 1;                           // keys up to there are of no expert
-    uint32_t after = (uint32_t)__shfl_down((int)mine, 1, TEAM);
-    if (t == a.top - 1) after = next;
-    const bool chosen = t < a.top && mine > none;
-    const int e = LAST - (int)(mine & LAST), ea = LAST - (int)(after & LAST);
-    const float zc = chosen ? to_float(z[e]) : -INFINITY;
-    const bool close = chosen && after > none && (int)(mine >> BITS) - (int)(after >> BITS) <= apart;
-    if (__any(close)) {
-      // neighbours that are close are compared in 64 bits; the last chosen one has to be apart from the key behind the next one as well
-      bool right = t < a.top - 1 || last <= none || (int)(mine >> BITS) - (int)(last >> BITS) > apart;
-      if (close) {
-        const float za = to_float(z[ea]);
-        if constexpr (BY_LOGIT) {
-          right &= zc > za || (zc == za && e < ea);
-        } else {
-          const double bc = a.bias ? (double)a.bias[e] : 0.0, ba = a.bias ? (double)a.bias[ea] : 0.0;
-          const double xc = exp(a.sigmoid ? -(double)zc : (double)zc - from), xa = exp(a.sigmoid ? -(double)za : (double)za - from);
-          if (a.sigmoid) {
-            const double cc = 1.0 / (1.0 + xc) + bc, ca = 1.0 / (1.0 + xa) + ba;
-            right &= cc > ca || (cc == ca && e < ea);
-          } else {
-            // the sum of all is one of 32 bits: twice its error, of the difference
-            const double d = (xc - xa) / total, sure = d + (bc - ba) - 256.0 * 0x1p-24 * fabs(d);
-            right &= sure > 0.0 || (zc == za && bc == ba && e < ea);
-          }
+        // a bound that `top` experts reach: each lane's largest c, or its two largest ones, where enough lanes have them
+        const int ones = __popcll(__ballot(m1 > -INFINITY) & mates), twos = __popcll(__ballot(m2 > -INFINITY) & mates);
+        const bool by_two = ones < a.top;
+        float bound = team_fold<TEAM>(by_two ? (m2 > -INFINITY ? m2 : INFINITY) : (m1 > -INFINITY ? m1 : INFINITY), smaller);
+        if (by_two && 2 * twos < a.top) bound = high - (BY_LOGIT ? 64.f : 1.f + (bias_high - bias_low));
+        const float range = fmaxf(high - bound + 4.f * off, 1e-30f), scale = (kTop - 32.f) * __builtin_amdgcn_rcpf(range);
+        const float shift = fmaf(-high, scale, 0x1p24f - 16.f);         // (its rounding moves all keys alike)
+        apart = 4 + (int)fminf(2.f * off * scale, kTop);
+  #pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          // below 2^24 a float32's steps are 1: the whole number stands in the low bits
+          const float f = __builtin_amdgcn_fmed3f(fmaf(c[i], scale, shift), 0x1p24f - kTop, 0x1p24f - 1.f);
+          key[i] = (__float_as_uint(f) << BITS) + low_bits(i);
+          if (TEAM == 64) key[i] &= 0x7fffffffu;
         }
-        settled &= right;
+      }
+      // lane j has the j-th key; `next` is the one behind the chosen ones, `last` the one behind that
+      uint32_t last = 0x80000000u, mine = 0, next = 0;
+      if constexpr (TEAM < 64) {
+        // the lane's keys in order, as far as they can be among the `top` and the two behind: a round pops the largest of the lanes' first
+        uint32_t list[10] = {};
+        sort_keys<PER>(key, list);
+        for (int j = 0; j <= a.top + 1; ++j) {
+          last = team_max_u32<TEAM>(list[0]);
+          if (t == j) mine = last;
+          if (j == a.top) next = last;
+          const bool mine_was = list[0] == last;
+  #pragma unroll
+          for (int i = 0; i < (PER < 9 ? PER : 9); ++i) list[i] = mine_was ? list[i + 1] : list[i];
+          if (j < a.top) settled &= last >> BITS != 0;
+        }
+        settled &= PER < 10 || list[0] != 0;                            // (nine from one lane: it may have had more)
+      } else {
+        for (int j = 0; j <= a.top + 1; ++j) {
+          uint32_t below = 0;
+  #pragma unroll
+          for (int i = 0; i < PER; ++i) below = max(below, key[i] - last);
+          below = team_max_u32<TEAM>(below);
+          last = below & 0x80000000u ? below + last : 0;                // 0: there is none
+          if (t == j) mine = last;
+          if (j == a.top) next = last;
+          if (j < a.top) settled &= last >> BITS != 0;
+        }
+      }
+      const uint32_t none = (1u << BITS) - 1;                           // keys up to there are of no expert
+      uint32_t after = (uint32_t)__shfl_down((int)mine, 1, TEAM);
+      if (t == a.top - 1) after = next;
+      const bool chosen = t < a.top && mine > none;
+      const int e = LAST - (int)(mine & LAST), ea = LAST - (int)(after & LAST);
+      const float zc = chosen ? to_float(z[e]) : -INFINITY;
+      const bool close = chosen && after > none && (int)(mine >> BITS) - (int)(after >> BITS) <= apart;
+      if (__any(close)) {
+        // neighbours that are close are compared in 64 bits; the last chosen one has to be apart from the key behind the next one as well
+        bool right = t < a.top - 1 || last <= none || (int)(mine >> BITS) - (int)(last >> BITS) > apart;
+        if (close) {
+          const float za = to_float(z[ea]);
+          if constexpr (BY_LOGIT) {
+            right &= zc > za || (zc == za && e < ea);
+          } else {
+            const double bc = a.bias ? (double)a.bias[e] : 0.0, ba = a.bias ? (double)a.bias[ea] : 0.0;
+            const double xc = exp(a.sigmoid ? -(double)zc : (double)zc - from), xa = exp(a.sigmoid ? -(double)za : (double)za - from);
+            if (a.sigmoid) {
+              const double cc = 1.0 / (1.0 + xc) + bc, ca = 1.0 / (1.0 + xa) + ba;
+              right &= cc > ca || (cc == ca && e < ea);
+            } else {
+              // the sum of all is one of 32 bits: twice its error, of the difference
+              const double d = (xc - xa) / total, sure = d + (bc - ba) - 256.0 * 0x1p-24 * fabs(d);
+              right &= sure > 0.0 || (zc == za && bc == ba && e < ea);
+            }
+          }
+          settled &= right;
+        }
+      }
+      const float w = chosen_weight<TEAM>(zc, a.sigmoid, a.renormalize, from, total);
+      // (a row without any expert is settled too: there may be many where a batch is padded)
+      const unsigned long long open = __ballot(!settled);
+      const bool mine_open = !empty && (open & mates) != 0;
+      if (in && t < a.top && !mine_open) {
+        a.expert[row * a.top + t] = empty ? -1 : e;
+        a.weight[row * a.top + t] = empty ? 0.f : a.scale * w;
+      }
+      const unsigned long long heads = __ballot(in && t == 0 && mine_open);
+      if (heads) {
+        if (heads >> lane & 1) later[threadIdx.x >> 6][kept + __popcll(heads & ((1ull << lane) - 1))] = (int32_t)row;
+        kept += __popcll(heads);
       }
     }
-    const float w = chosen_weight<TEAM>(zc, a.sigmoid, a.renormalize, from, total);
-    // (a row without any expert is settled too: there may be many where a batch is padded)
-    const unsigned long long open = __ballot(!settled);
-    const bool mine_open = !empty && (open & mates) != 0;
-    if (in && t < a.top && !mine_open) {
-      a.expert[row * a.top + t] = empty ? -1 : e;
-      a.weight[row * a.top + t] = empty ? 0.f : a.scale * w;
-    }
-    const unsigned long long heads = __ballot(in && t == 0 && mine_open);
-    if (heads) {
-      if (heads >> lane & 1) later[threadIdx.x >> 6][kept + __popcll(heads & ((1ull << lane) - 1))] = (int32_t)row;
-      kept += __popcll(heads);
-    }
-  }
-  wave_sync();
-  for (int q = 0; q < kept; ++q) route_row<T>(a, later[threadIdx.x >> 6][q], row_c[threadIdx.x >> 6]);
-  wave_sync();
+    wave_sync();
+    for (int q = 0; q < kept; ++q) route_row<T>(a, later[threadIdx.x >> 6][q], row_c[threadIdx.x >> 6]);
+    wave_sync();
   }
 }
 

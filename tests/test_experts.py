@@ -266,6 +266,18 @@ def test_route_decides_what_float32_cannot(gpu, ops, n, experts, top):
     # biases of a size at which a score is lost in float32
     big = torch.from_numpy(np.repeat([1e6, -1e6], experts // 2)).float().to(DEV)
     check_route(torch, ops, torch.from_numpy(rng.standard_normal((n, experts))).float().to(DEV), top, sigmoid=True, bias=big)
+    # experts that the bias keeps out
+    out = bias.clone()
+    out[:: 3] = -INF
+    for groups in (1, 8):
+        logits = torch.from_numpy(rng.standard_normal((n, experts))).float().to(DEV)
+        kw = dict(sigmoid=True, groups=groups, top_groups=max(1, groups // 2))
+        expert, weight = check_route(torch, ops, logits, top, bias=out, **kw)
+        again, same = run_route(torch, ops, logits, top, bias=torch.where(out == -INF, math.nan, out), **kw)
+        assert torch.equal(again, expert) and torch.equal(same, weight)
+    out[top - 2:] = -INF
+    expert, weight = check_route(torch, ops, torch.from_numpy(rng.standard_normal((n, experts))).float().to(DEV), top, bias=out)
+    assert bool((expert[:, -2:] == -1).all())
 
 
 def test_route_reports_logits_that_are_no_numbers(gpu):
