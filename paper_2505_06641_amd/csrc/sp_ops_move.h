@@ -3,8 +3,8 @@
 //   combine        y_i = sum over j of w_ij ys[place_ij] + r_i
 //   its gradients  dys[place_ij] = w_ij dy_i        dw_ij = dy_i . ys[place_ij]
 // A team of lanes takes a row of x, y or dy; the rows at the places are whole rows somewhere else, so that every access is a run of
-// 16-byte pieces.  Bound by memory: 65536 x 512 bfloat16 to 4 places each 68 us (5.0 TB/s), 65536 x 256 float32 of 2 places and a residual 51 (5.3), the gradients
-// of 32768 x 768 bfloat16 with 8 places each 169 (4.9).
+// 16-byte pieces.  Bound by memory: 65536 x 512 bfloat16 to 4 places each 68 us (5.0 TB/s), 65536 x 256 float32 of 2 places and a residual 51
+// (5.3), the gradients of 32768 x 768 bfloat16 with 8 places each 169 (4.9).
 #pragma once
 #include "sp_ops_common.h"
 
