@@ -8,6 +8,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <memory>
 #include <new>
 #include <sstream>
@@ -470,11 +471,15 @@ PyObject* dropout(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyOb
   void *px = c.rows(x, "x", type, n, d, &xs), *py = c.rows(y, "y", type, n, d, &ys), *pr = c.rows(v[6], "residual", type, n, d, &rs);
   void* step = c.whole(v[5], "step", at::kLong, {1});
   const double p = c.number(v[2], 0.0);
+  float near = (float)p;                                   // 0 and 1 for themselves only
+  if (p > 0.0 && near == 0.f) near = 0x1p-126f;
+  if (p < 1.0 && near == 1.f) near = std::nextafterf(1.f, 0.f);
+  if (p < 0.0 || p > 1.0) near = -1.f;
   const uint64_t seed = c.word(v[3], "seed"), offset = c.word(v[4], "offset");
   const int32_t ni = c.count(n, "x's rows"), di = c.count(d, "x's width");
   void* s = c.stream(v[7]);
   if (c.bad) return nullptr;
-  return finish(self, c, sp_dropout(self->handle, ni, di, dt, px, xs, (float)p, seed, offset, (int64_t*)step, pr, rs, py, ys, s));
+  return finish(self, c, sp_dropout(self->handle, ni, di, dt, px, xs, near, seed, offset, (int64_t*)step, pr, rs, py, ys, s));
 }
 
 PyObject* quantize_rows(OpsObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {

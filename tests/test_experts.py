@@ -675,7 +675,7 @@ def test_dropout(gpu, ops, n, d, dtype):
 
 
 def test_dropout_at_the_ends_and_on_average(gpu, ops):
-    torch, _ = gpu
+    torch, binding = gpu
     x = torch.randn(300, 77, device=DEV)
     y = torch.full_like(x, math.nan)
     ops.sp_dropout(x, y, 0.0, 5)
@@ -692,6 +692,13 @@ def test_dropout_at_the_ends_and_on_average(gpu, ops):
         assert abs(share - want) < 6 * math.sqrt(want * (1 - want) / total)       # six standard deviations
         # the scale is that of the probability as it is taken: 1 / (1 - p), rounded once
         assert float(out.max()) == float(torch.tensor(65536.0 / (65536 - steps)))
+    # numbers of 64 bits that float32 would take for 0 and 1, and for what may be
+    for p, steps in ((1e-60, 1), (1 - 1e-12, 65535)):
+        ops.sp_dropout(one, out, p, 11)
+        assert float(out.max()) == float(torch.tensor(65536.0 / (65536 - steps))) and float(out.min()) == 0.0
+    for p in (-1e-60, 1 + 1e-12, math.nan):
+        with pytest.raises(binding.SneakPeekError):
+            ops.sp_dropout(one, out, p, 11)
     # neighbours, rows, seeds and offsets do not go together
     ops.sp_dropout(one, out, 0.5, 11)
     a = (out > 0).float() - 0.5
