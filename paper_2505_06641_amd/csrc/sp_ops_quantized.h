@@ -166,9 +166,10 @@ struct QuantizedTile {
 };
 
 // Sixteen bytes for every lane from base + off to LDS: the wavefront's lanes one after the other from `to` on.  (In asm, since the compiler would wait
-// for all such loads before every read of LDS; there is no output that it could take for written.)
+// for all such loads before every read of LDS; there is no output that it could take for written.)  The load takes `to` from M0, one wait state behind
+// a scalar write of it at the earliest, which the compiler does not see to in front of asm.
 __device__ __forceinline__ void load_to_lds(uint32_t to, const int8_t* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(base) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(to), "v"(off), "s"(base) : "memory");
 }
 // Eight results, which nobody reads before much else has gone through the caches.
 typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
