@@ -443,6 +443,7 @@ PyObject* combine_backward(OpsObject* self, PyObject* const* args, Py_ssize_t na
   const at::Tensor *dy = c.matrix(v[0], "dy", &n, &d), *place = c.matrix(v[2], "place", &pn, &top), *sorted = c.tensor(v[1], "ys"),
                    *out = c.tensor(v[4], "dys"), *some = sorted ? sorted : out;
   if (c.bad) return nullptr;
+  if (!sorted && c.tensor(v[5], "dweight")) c.refuse("ys is missing, which dweight is made of");
   if (some && some->dim() != 2) c.refuse("ys and dys are matrices");
   if (c.bad) return nullptr;
   const int64_t rows = some ? some->size(0) : 0;
@@ -674,7 +675,7 @@ PyMethodDef ops_methods[] = {
     {"sp_combine", with_names<combine>(), METH_FASTCALL | METH_KEYWORDS,
      "sp_combine(ys, place, y, weight=None, residual=None, stream=None)\n\ny_i = sum of weight_ij ys[place_ij] + residual_i."},
     {"sp_combine_backward", with_names<combine_backward>(), METH_FASTCALL | METH_KEYWORDS,
-     "sp_combine_backward(dy, ys, place, weight=None, dys=None, dweight=None, stream=None)\n\nGradients of sp_combine; ys is read for dweight."},
+     "sp_combine_backward(dy, ys, place, weight=None, dys=None, dweight=None, stream=None)\n\nGradients of sp_combine; ys is read for dweight, and may be None without it."},
     {"sp_dropout", with_names<dropout>(), METH_FASTCALL | METH_KEYWORDS,
      "sp_dropout(x, y, p, seed, offset=0, step=None, residual=None, stream=None)\n\n"
      "y = x / (1 - p) or 0, plus the residual; the same call on dy is the gradient.  step: int64 [1] on the device, added to offset."},
