@@ -186,6 +186,11 @@ __device__ __forceinline__ void store_past_caches(bf16* p, const float (&v)[8]) 
   for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint16_t, (bf16)v[i]);
   __builtin_nontemporal_store(q, reinterpret_cast<u16x8_any*>(p));
 }
+// A sum, of less than 2^31, is multiplied by its row's scale and then by its output's.  The scale of a row of large numbers comes last: the sum times it might
+// pass float32 where the result does not.
+constexpr float kLateScale = 0x1p64f;
+__device__ __forceinline__ float early_scale(float s) { return s > kLateScale ? 1.f : s; }
+__device__ __forceinline__ float late_scale(float s) { return s > kLateScale ? s : 1.f; }
 // Until at most N of the wavefront's loads are under way.
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 // All wavefronts have come here, and what they read from LDS before has arrived.
@@ -313,22 +318,25 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
   // columns 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3.  The 16-byte pieces of a row are permuted by the row.
   float* stage = reinterpret_cast<float*>(lds) + wave * 32 * WN;
   __syncthreads();
-  // whole: all of the tile's rows and columns are there
-  auto finish = [&](auto whole, auto past_caches) {
+  // whole: all of the tile's rows and columns are there; late: some of the wavefront's rows have scales that come last (a way of its own, since the
+  // choice for each row costs 262144 rows, 1024 -> 1024 30 us)
+  auto finish = [&](auto whole, auto past_caches, auto late) {
 #pragma unroll
     for (int i = 0; i < FR; ++i) {
       const int r = lane & 31;
+      const float by = late ? early_scale(xs[i]) : xs[i];
 #pragma unroll
       for (int j = 0; j < FC; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *reinterpret_cast<f32x4*>(stage + r * WN + (((j * 8 + 2 * q + (lane >> 5)) ^ (r % (WN / 4))) * 4)) =
-              f32x4{(float)acc[i][j][4 * q] * xs[i], (float)acc[i][j][4 * q + 1] * xs[i], (float)acc[i][j][4 * q + 2] * xs[i],
-                    (float)acc[i][j][4 * q + 3] * xs[i]};
+              f32x4{(float)acc[i][j][4 * q] * by, (float)acc[i][j][4 * q + 1] * by, (float)acc[i][j][4 * q + 2] * by,
+                    (float)acc[i][j][4 * q + 3] * by};
       wave_sync();
 #pragma unroll
       for (int u = 0; u < 32 / kAtOnce; ++u) {
         const int sr = u * kAtOnce + lane / kAcross, tr = wr + i * 32 + sr;
+        const float then = late ? late_scale(__shfl(xs[i], sr)) : 1.f;
         if (!whole && (tr >= n_rows || left <= 0)) continue;
         const int64_t row = rows.lo + tr;
         const int count = whole ? VO : left;
@@ -342,7 +350,7 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
         }
 #pragma unroll
         for (int e = 0; e < VO; ++e) {
-          v[e] = v[e] * ws[e] + bias[e];
+          v[e] = (late ? v[e] * ws[e] * then : v[e] * ws[e]) + bias[e];
           if (a.relu) v[e] = v[e] < 0.f ? 0.f : v[e];
           if (a.residual) v[e] += res[e];
         }
@@ -354,9 +362,13 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
     }
   };
   const bool whole = n_rows == BM && n_cols == BN;
-  if (whole && a.past_caches) finish(std::true_type{}, std::true_type{});
-  else if (whole) finish(std::true_type{}, std::false_type{});
-  else finish(std::false_type{}, std::false_type{});
+  bool late = false;
+#pragma unroll
+  for (int i = 0; i < FR; ++i) late |= xs[i] > kLateScale;
+  if (__any(late)) finish(std::false_type{}, std::false_type{}, std::true_type{});
+  else if (whole && a.past_caches) finish(std::true_type{}, std::true_type{}, std::false_type{});
+  else if (whole) finish(std::true_type{}, std::false_type{}, std::false_type{});
+  else finish(std::false_type{}, std::false_type{}, std::false_type{});
 }
 
 // Few rows: a request, a window of them, a small batch.  A workgroup takes 16 rows of one group and 16 columns, its wavefronts share out the
@@ -404,7 +416,7 @@ __global__ __launch_bounds__(kFewQuantizedThreads) void k_quantized_few(Quantize
   int sum = 0;
 #pragma unroll
   for (int q = 0; q < WAVES; ++q) sum += part[q][r * 17 + threadIdx.x % 16];
-  float v = in ? (float)sum * xs * ws + bias : 0.f;
+  float v = in ? (float)sum * early_scale(xs) * ws * late_scale(xs) + bias : 0.f;
   if (a.relu) v = v < 0.f ? 0.f : v;
   ((TO*)a.y)[row * a.y_stride + col] = from_float<TO>(v + res);
 }
