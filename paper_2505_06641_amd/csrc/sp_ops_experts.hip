@@ -319,8 +319,8 @@ sp_status sp_grouped_linear_quantized(sp_ops* o, int32_t n, int32_t k, int32_t m
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
   with_type(out_dtype, [&]<typename T>() {
-    auto kernel = few ? k_quantized_few<T> : large ? k_quantized<T, 256, 256, 128, 2, true>
-                  : direct ? k_quantized<T, 128, 128, 64, 2, true> : k_quantized<T, 128, 128, 64, 2, false>;
+    auto kernel = few ? k_quantized_few<T> : large ? k_quantized<T, 256, 256, 128, true>
+                  : direct ? k_quantized<T, 128, 128, 64, true> : k_quantized<T, 128, 128, 64, false>;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(few ? kFewQuantizedThreads : large ? 512 : 256), 0, (hipStream_t)stream, a);
   });
   return launched(o);

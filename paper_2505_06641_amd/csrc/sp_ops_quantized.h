@@ -146,21 +146,20 @@ __device__ __forceinline__ bytes16 load_bytes(const int8_t* p, int t, int depth,
 
 // A workgroup computes BM rows of one group by BN columns, wavefronts of 64 by BN / 2, D bytes of the depth at a time by way of LDS.  Rows and
 // columns beyond the tile's last are that one again, and not written.  LDS: [rows of both sides][D bytes], the 16-byte pieces of a row permuted
-// by the row, so that the eight rows that are read together lie in different banks.
-//   DIRECT: memory to LDS without registers, STAGES pieces of the depth in LDS, one of them being multiplied.  For depths, strides and addresses
-//     that are multiples of 16.
-//   else by way of registers, two stages in LDS and one on its way, which takes any address and cuts what lies behind the depth.
+// by the row, so that the eight rows that are read together lie in different banks.  Two stages of the depth lie there, one of them being multiplied.
+//   DIRECT: memory to LDS without registers.  For depths, strides and addresses that are multiples of 16.
+//   else by way of registers, which takes any address and cuts what lies behind the depth.
 // Tiles of 128 by 128 have four workgroups to a compute unit, which hide each other's trips to memory (two stages of 64 bytes: 65536 rows,
 // 1024 -> 1024 97 us; three stages and three workgroups 101; tiles of 128 by 256, whose wavefronts read a quarter less from LDS, and two workgroups
 // 103).  Many tiles of long depths come near the library's rate: 262144 rows, 64 -> 1024 and 1024 -> 1024 differ by the time of 1930 TOP/s, the
 // library's 8192 x 8192 x 8192 product has 2040 to 2310; what is left is the time before a tile's first and behind its last product.
-template <int BM, int BN, int D, int STAGES, bool DIRECT>
+template <int BM, int BN, int D>
 struct QuantizedTile {
   static constexpr int WAVES = BM / 32, FR = 2, FC = BN / 64, kRows = BM + BN;
   static constexpr int kAcross = D / 16, kRun = 64 / kAcross;         // pieces of a row, rows of a run
   static constexpr int kChunks = kRows / kRun / WAVES, kOfX = BM / kRun / WAVES;   // a wavefront's runs, the first of them rows of x
   static constexpr int kSums = WAVES * 32 * (BN / 2) * 4;             // 32 rows of every wavefront's
-  static constexpr int kBytes = STAGES * kRows * D > kSums ? STAGES * kRows * D : kSums;
+  static constexpr int kBytes = 2 * kRows * D > kSums ? 2 * kRows * D : kSums;
   static __device__ __forceinline__ int swap(int row) { return D == 128 ? row & 7 : row >> 1 & 3; }
   static __device__ __forceinline__ int place(int row, int piece) { return row * D + ((piece ^ swap(row)) * 16); }
 };
@@ -191,14 +190,14 @@ __device__ __forceinline__ void store_past_caches(bf16* p, const float (&v)[8]) 
 constexpr float kLateScale = 0x1p64f;
 __device__ __forceinline__ float early_scale(float s) { return s > kLateScale ? 1.f : s; }
 __device__ __forceinline__ float late_scale(float s) { return s > kLateScale ? s : 1.f; }
-// Until at most N of the wavefront's loads are under way.
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+// Until the wavefront's loads have arrived.
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 // All wavefronts have come here, and what they read from LDS before has arrived.
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
-template <typename TO, int BM, int BN, int D, int STAGES, bool DIRECT>
-__global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 : 3) void k_quantized(QuantizedArgs a) {
-  typedef QuantizedTile<BM, BN, D, STAGES, DIRECT> Tile;
+template <typename TO, int BM, int BN, int D, bool DIRECT>
+__global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT ? 4 : 3) void k_quantized(QuantizedArgs a) {
+  typedef QuantizedTile<BM, BN, D> Tile;
   constexpr int FR = Tile::FR, FC = Tile::FC, CH = Tile::kChunks, CX = Tile::kOfX, WAVES = Tile::WAVES, kStageBytes = Tile::kRows * D;
   constexpr int WN = BN / 2;                                          // columns of a wavefront
   __shared__ __align__(16) uint8_t lds[Tile::kBytes];
@@ -257,29 +256,25 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     auto load = [&](int s) {                                          // stage s of the depth; pieces behind the depth read the last one
       const int t0 = s * D, most = (depth - t0) / 16 - 1;
-      const uint32_t to = lds0 + s % STAGES * kStageBytes + wave * 1024;
+      const uint32_t to = lds0 + s % 2 * kStageBytes + wave * 1024;
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const uint32_t from = off[i] + min(piece_of(i), most) * 16;
         load_to_lds(to + i * WAVES * 1024, (i < CX ? x : w) + t0, from);
       }
     };
-    constexpr int AHEAD = STAGES - 1;
-    for (int s = 0; s < AHEAD && s < stages; ++s) load(s);
+    load(0);
     for (int s = 0; s < stages; ++s) {
-      // this stage's loads have arrived (the next ones' may be under way), and nobody reads the stage before any more
-      if (s + AHEAD - 1 < stages) wait_loads<CH * (AHEAD - 1)>();
-      else if (AHEAD > 2 && s + 1 < stages) wait_loads<CH>();
-      else wait_loads<0>();
-      uint8_t* at = lds + s % STAGES * kStageBytes;
+      wait_loads();                                                   // (this stage's)
+      uint8_t* at = lds + s % 2 * kStageBytes;
       const int most = (depth - s * D) / 16;
       if (most < Tile::kAcross) {                                                 // x behind the depth is 0
 #pragma unroll
         for (int i = 0; i < CX; ++i)
           if (piece_of(i) >= most) *reinterpret_cast<bytes16*>(at + Tile::place(row_of[i], piece_of(i))) = bytes16{0, 0, 0, 0};
       }
-      meet();
-      if (s + AHEAD < stages) load(s + AHEAD);
+      meet();                                                         // (nobody reads the stage before any more)
+      if (s + 1 < stages) load(s + 1);
       multiply(at);
     }
   } else {
@@ -299,18 +294,14 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
     };
     auto store = [&](int s) {
 #pragma unroll
-      for (int i = 0; i < CH; ++i) *reinterpret_cast<bytes16*>(lds + s % STAGES * kStageBytes + Tile::place(row_of[i], piece_of(i))) = raw[i];
+      for (int i = 0; i < CH; ++i) *reinterpret_cast<bytes16*>(lds + s % 2 * kStageBytes + Tile::place(row_of[i], piece_of(i))) = raw[i];
     };
-    if (stages > 0) {
-      load(0);
-      store(0);
-      if (stages > 1) load(1);
-    }
+    load(0);
     for (int s = 0; s < stages; ++s) {
+      store(s);
+      if (s + 1 < stages) load(s + 1);
       __syncthreads();
-      if (s + 1 < stages) store(s + 1);
-      if (s + 2 < stages) load(s + 2);
-      multiply(lds + s % STAGES * kStageBytes);
+      multiply(lds + s % 2 * kStageBytes);
     }
   }
 
@@ -318,13 +309,17 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
   // columns 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3.  The 16-byte pieces of a row are permuted by the row.
   float* stage = reinterpret_cast<float*>(lds) + wave * 32 * WN;
   __syncthreads();
-  // whole: all of the tile's rows and columns are there; late: some of the wavefront's rows have scales that come last (a way of its own, since the
-  // choice for each row costs 262144 rows, 1024 -> 1024 30 us)
-  auto finish = [&](auto whole, auto past_caches, auto late) {
+  // all: all of the tile's rows and columns are there, and none of the wavefront's rows has a scale that comes last (to ask for each row costs 262144 rows,
+  // 1024 -> 1024 30 us)
+  bool late = false;
+#pragma unroll
+  for (int i = 0; i < FR; ++i) late |= xs[i] > kLateScale;
+  const bool whole = n_rows == BM && n_cols == BN && !__any(late);
+  auto finish = [&](auto all, auto past_caches) {
 #pragma unroll
     for (int i = 0; i < FR; ++i) {
       const int r = lane & 31;
-      const float by = late ? early_scale(xs[i]) : xs[i];
+      const float by = all ? xs[i] : early_scale(xs[i]);
 #pragma unroll
       for (int j = 0; j < FC; ++j)
 #pragma unroll
@@ -336,10 +331,10 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
 #pragma unroll
       for (int u = 0; u < 32 / kAtOnce; ++u) {
         const int sr = u * kAtOnce + lane / kAcross, tr = wr + i * 32 + sr;
-        const float then = late ? late_scale(__shfl(xs[i], sr)) : 1.f;
-        if (!whole && (tr >= n_rows || left <= 0)) continue;
+        const float then = all ? 1.f : late_scale(__shfl(xs[i], sr));
+        if (!all && (tr >= n_rows || left <= 0)) continue;
         const int64_t row = rows.lo + tr;
-        const int count = whole ? VO : left;
+        const int count = all ? VO : left;
         float v[VO], res[VO];
         if (a.residual) load_some((const TO*)a.residual + row * a.residual_stride + col, count, 0.f, res);
 #pragma unroll
@@ -350,7 +345,7 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
         }
 #pragma unroll
         for (int e = 0; e < VO; ++e) {
-          v[e] = (late ? v[e] * ws[e] * then : v[e] * ws[e]) + bias[e];
+          v[e] = (all ? v[e] * ws[e] : v[e] * ws[e] * then) + bias[e];
           if (a.relu) v[e] = v[e] < 0.f ? 0.f : v[e];
           if (a.residual) v[e] += res[e];
         }
@@ -361,14 +356,9 @@ __global__ __launch_bounds__(BM * 2, BM == 256 ? 2 : DIRECT && STAGES == 2 ? 4 :
       wave_sync();
     }
   };
-  const bool whole = n_rows == BM && n_cols == BN;
-  bool late = false;
-#pragma unroll
-  for (int i = 0; i < FR; ++i) late |= xs[i] > kLateScale;
-  if (__any(late)) finish(std::false_type{}, std::false_type{}, std::true_type{});
-  else if (whole && a.past_caches) finish(std::true_type{}, std::true_type{}, std::false_type{});
-  else if (whole) finish(std::true_type{}, std::false_type{}, std::false_type{});
-  else finish(std::false_type{}, std::false_type{}, std::false_type{});
+  if (whole && a.past_caches) finish(std::true_type{}, std::true_type{});
+  else if (whole) finish(std::true_type{}, std::false_type{});
+  else finish(std::false_type{}, std::false_type{});
 }
 
 // Few rows: a request, a window of them, a small batch.  A workgroup takes 16 rows of one group and 16 columns, its wavefronts share out the

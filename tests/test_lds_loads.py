@@ -14,7 +14,7 @@ __global__ void probe(const int8_t* from, int8_t* out, uint32_t n) {
   __shared__ int8_t lds[4096];
   const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds;
   for (uint32_t i = 0; i < n; ++i) sp::load_to_lds(at + i * 1024, from + i * 1024, threadIdx.x * 16);
-  sp::wait_loads<0>();
+  sp::wait_loads();
   sp::meet();
   out[threadIdx.x] = lds[threadIdx.x];
 }
