@@ -17,6 +17,8 @@
 using namespace sp;
 
 static_assert(kMaxExperts == SP_MAX_EXPERTS, "a launch's counters hold all experts");
+static_assert(SP_MAX_EXPERTS <= 64 * 16, "a wavefront's lanes hold a row of logits");
+static_assert(SP_MAX_EXPERTS <= 64 * 2 * kPiece<bf16> && SP_MAX_EXPERTS <= 64 * 4 * kPiece<float>, "the router's gradient holds a row in a wavefront");
 
 namespace {
 
@@ -74,8 +76,8 @@ sp_status sp_route(sp_ops* o, int32_t n, int32_t experts, int32_t top, int32_t d
                        : per <= 2  ? k_route<T, 64, 2, BY_LOGIT>
                        : per <= 4  ? k_route<T, 64, 4, BY_LOGIT>
                        : per <= 8  ? k_route<T, 64, 8, BY_LOGIT>
-                       : per <= 16 ? k_route<T, 64, 16, BY_LOGIT>
-                                   : k_route<T, 64, 32, BY_LOGIT>);
+                       : BY_LOGIT || per <= 16 ? k_route<T, 64, 16, BY_LOGIT>                        // (without groups a lane has at most 16)
+                                               : k_route<T, 64, BY_LOGIT ? 16 : 32, BY_LOGIT>);
     };
     hipLaunchKernelGGL((bias || groups > 1 ? kernel.template operator()<false>() : kernel.template operator()<true>()), grid, dim3(256), 0,
                        (hipStream_t)stream, a);
@@ -107,8 +109,8 @@ sp_status sp_route_backward(sp_ops* o, int32_t n, int32_t experts, int32_t top, 
     else if (lanes <= 16) run.template operator()<16, 1>();
     else if (lanes <= 32) run.template operator()<32, 1>();
     else if (lanes <= 64) run.template operator()<64, 1>();
-    else if (lanes <= 128) run.template operator()<64, 2>();
-    else run.template operator()<64, 4>();
+    else if (sizeof(T) == 2 || lanes <= 128) run.template operator()<64, 2>();          // (SP_MAX_EXPERTS bfloat16 are 128 pieces)
+    else if constexpr (sizeof(T) == 4) run.template operator()<64, 4>();
   });
   return launched(o);
 }
