@@ -3,8 +3,8 @@
 // The numbers are the 16-bit halves of the words of Philox 4x32 with ten rounds (J. Salmon, M. Moraes, R. Dror, D. Shaw, "Parallel random
 // numbers: as easy as 1, 2, 3", 2011), so that one computation serves the eight columns of a piece: counter (piece of the row, row, offset low,
 // offset high), key the seed, column 8 piece + 2 word + half with the low half first.  They hang on nothing else: not on type, stride or
-// launch, and the backward pass is the same call on dy.  Bound by memory: 65536 x 768 bfloat16 with a residual 49 us (6.2 TB/s, the residual partly from
-// the last-level cache), 262144 x 256 float32 99 us (5.4 TB/s); one computation to four columns would take as long as the memory does.
+// launch, and the backward pass is the same call on dy.  Bound by memory: 65536 x 768 bfloat16 with a residual 52 us (5.8 TB/s, the residual partly from
+// the last-level cache), 262144 x 256 float32 91 us (5.9 TB/s); one computation to four columns would take as long as the memory does.
 #pragma once
 #include "sp_ops_common.h"
 
@@ -48,45 +48,28 @@ struct RawColumns {
   __device__ __forceinline__ float operator[](int i) const { return of_raw((const T*)nullptr, q[i / V], i % V); }
 };
 
-// EACH: pieces of a thread, which are on their way together.  step_rows, step_pieces: 256 pieces on, in whole rows and pieces.
-template <typename T, int EACH>
-__global__ __launch_bounds__(256) void k_dropout(DropoutArgs a, int step_rows, int step_pieces) {
+// A piece to a thread, in launches of one or two dimensions of workgroups.  (Four bfloat16 or two float32 pieces to a thread, on their way together: 65536 x 768
+// bfloat16 with a residual 56 us against 53, 262144 x 256 float32 98 against 91.)
+template <typename T>
+__global__ __launch_bounds__(256) void k_dropout(DropoutArgs a) {
   const uint64_t offset = a.offset + (a.step ? (uint64_t)*a.step : 0u);
-  const int64_t at = (int64_t)blockIdx.x * (256 * EACH) + threadIdx.x;
-  int64_t row = at >> 32 ? at / a.pieces : (int64_t)((uint32_t)at / (uint32_t)a.pieces);
-  int piece = (int)(at - row * a.pieces);
-  int64_t rows[EACH];
-  int cols[EACH];
-  RawColumns<T> x[EACH], r[EACH];
+  const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+  const int64_t row = at >> 32 ? at / a.pieces : (int64_t)((uint32_t)at / (uint32_t)a.pieces);
+  if (row >= a.n) return;
+  const int col = (int)(at - row * a.pieces) * 8;
+  RawColumns<T> x, r;
+  x.load((const T*)a.x + row * a.x_stride, col, a.d);
+  if (a.residual) r.load((const T*)a.residual + row * a.residual_stride, col, a.d);
+  uint32_t c[4] = {(uint32_t)col / 8, (uint32_t)row, (uint32_t)offset, (uint32_t)(offset >> 32)};
+  philox(c, a.key0, a.key1);
+  float v[8];
 #pragma unroll
-  for (int u = 0; u < EACH; ++u) {
-    rows[u] = row;
-    cols[u] = piece * 8;
-    if (row < a.n) {
-      x[u].load((const T*)a.x + row * a.x_stride, cols[u], a.d);
-      if (a.residual) r[u].load((const T*)a.residual + row * a.residual_stride, cols[u], a.d);
-    }
-    row += step_rows;
-    piece += step_pieces;
-    if (piece >= a.pieces) {
-      piece -= a.pieces;
-      ++row;
-    }
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t number = i % 2 ? c[i / 2] >> 16 : c[i / 2] & 0xffffu;
+    v[i] = number >= a.drop ? x[i] * a.scale : 0.f;
+    if (a.residual) v[i] += r[i];
   }
-#pragma unroll
-  for (int u = 0; u < EACH; ++u) {
-    if (rows[u] >= a.n) return;
-    uint32_t c[4] = {(uint32_t)cols[u] / 8, (uint32_t)rows[u], (uint32_t)offset, (uint32_t)(offset >> 32)};
-    philox(c, a.key0, a.key1);
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t number = i % 2 ? c[i / 2] >> 16 : c[i / 2] & 0xffffu;
-      v[i] = number >= a.drop ? x[u][i] * a.scale : 0.f;
-      if (a.residual) v[i] += r[u][i];
-    }
-    store_some((T*)a.y + rows[u] * a.y_stride + cols[u], a.d - cols[u], v);
-  }
+  store_some((T*)a.y + row * a.y_stride + col, a.d - col, v);
 }
 
 }  // namespace sp

@@ -245,19 +245,13 @@ sp_status sp_dropout(sp_ops* o, int32_t n, int32_t d, int32_t dtype, const void*
   a.key0 = (uint32_t)seed; a.key1 = (uint32_t)(seed >> 32); a.offset = offset; a.step = step;
   a.x = x; a.x_stride = x_stride; a.residual = residual; a.residual_stride = residual_stride; a.y = y; a.y_stride = y_stride;
   const int64_t pieces = (int64_t)n * a.pieces;
-  if (pieces / 2 > UINT32_MAX - 512) return SP_ECAPACITY;               // (threads; float32's have two pieces each)
+  if (pieces / 2 > UINT32_MAX - 512) return SP_ECAPACITY;
   if (n == 0) return SP_OK;
   DeviceGuard g(o->device);
   if (!g.ok) return SP_EDEVICE;
+  const int64_t blocks = (pieces + 255) / 256, turns = (blocks + (1 << 23) - 1) >> 23;      // (a launch has less than 2^32 threads in a dimension)
   with_type(dtype, [&]<typename T>() {
-    auto run = [&]<int EACH>() {
-      constexpr int each = 256 * EACH;
-      hipLaunchKernelGGL((k_dropout<T, EACH>), dim3((unsigned)((pieces + each - 1) / each)), dim3(256), 0, (hipStream_t)stream, a, 256 / a.pieces,
-                         256 % a.pieces);
-    };
-    // a piece to a thread while the device holds about all of them at once
-    if (pieces <= 524288) run.template operator()<1>();
-    else run.template operator()<(sizeof(T) == 2 ? 4 : 2)>();
+    hipLaunchKernelGGL(k_dropout<T>, dim3((unsigned)((blocks + turns - 1) / turns), (unsigned)turns), dim3(256), 0, (hipStream_t)stream, a);
   });
   return launched(o);
 }

@@ -185,7 +185,7 @@ def numbers(torch, n, d, seed, offset):
     return torch.stack([words & 0xFFFF, words >> 16], 3).view(n, -1)[:, :d]
 
 
-# more than 524288 pieces of eight columns: several to a thread; 256 pieces on is in the same row, the next one, or 256 rows on
+# pieces of eight columns whose workgroups of 256 lie inside a row, across some, or across 256 rows
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,d", [(60001, 77), (60001, 80), (301, 16390), (2100, 2056), (530001, 8), (530001, 5), (1000003, 9), (8, 524301)])
 def test_dropout_of_many_pieces(gpu, ops, n, d, dtype):
@@ -214,6 +214,30 @@ def test_dropout_of_many_pieces(gpu, ops, n, d, dtype):
         if r is not None:
             ops.sp_dropout(x, r, p, seed, offset=offset, residual=r)
             assert torch.equal(r, y)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_dropout_of_more_than_32_bits_of_pieces(gpu, ops, dtype):
+    """Three pieces to a row, 4.35e9 in all, in place; 50 or 100 GB."""
+    torch, _ = gpu
+    t = dtype_of(torch, dtype)
+    torch.cuda.empty_cache()
+    n, d, p = 1450000000, 17, 0.3
+    x = torch.ones(n * d, dtype=t, device=DEV).view(n, d)
+    ops.sp_dropout(x, x, p, 99, offset=5)
+    drop = round(p * 65536)
+    kept = torch.tensor(65536.0 / (65536 - drop)).to(t)
+    edge = 2 ** 32 // 3                                    # the row that holds piece 2^32
+    for first in (0, 7 * 10 ** 8, edge - 3, n - 100):
+        for i in range(first, first + 6):
+            words = [philox((piece, i, 5, 0), (99, 0)) for piece in range(3)]
+            want = [words[c // 8][c % 8 // 2] >> 16 * (c % 2) & 0xFFFF >= drop for c in range(d)]
+            assert torch.equal(x[i], torch.where(torch.tensor(want, device=DEV), kept.to(DEV), 0.0).to(t)), i
+    # and all of the others: kept or dropped, nothing untouched
+    for part in x.view(-1).split(1 << 30):
+        assert bool(((part == 0) | (part == kept.to(DEV))).all())
+    del x, part
+    torch.cuda.empty_cache()
 
 
 # 32768 rows of a wavefront each at once, 8192 of a workgroup each, 4096 of those that are read twice
