@@ -163,7 +163,9 @@ void with_rows(int32_t n, int32_t d, int32_t top, int32_t dtype, F&& f) {
       else if (top <= 4) f.template operator()<T, TEAM, 4>(grid);
       else f.template operator()<T, TEAM, 8>(grid);
     };
-    // the largest team that leaves the fewest lanes without a piece in the last turn (96 pieces: 32 lanes in three turns)
+    // The largest team that leaves the fewest lanes without a piece in the last turn, in at most four turns.  96 pieces (32768 x 768 bfloat16, 8 pairs): 32 lanes
+    // in three turns combine in 96 us, 64 in two in 107; 16 pieces (262144 x 64 float32, 2 pairs) 16 lanes 44 us, 64 lanes 88; 65 pieces (65536 x 520 bfloat16,
+    // 4 pairs) 32 lanes 75 us, 16 lanes in five turns 82, 64 lanes 81.
     auto idle = [&](int lanes) { return (pieces + lanes - 1) / lanes * lanes - pieces; };
     int best = 64;
     for (int lanes = 32; lanes >= 4; lanes /= 2)
@@ -297,7 +299,8 @@ sp_status sp_grouped_linear_quantized(sp_ops* o, int32_t n, int32_t k, int32_t m
   // against 11.4 in tiles; 1024 rows, 1024 -> 512 11.1 against 10.5, 256 rows, 2048 -> 2048 20.9 against 16.0; addresses that are no multiples of 16 cost
   // them more: 256 rows of 32 groups, 1023 -> 515 21.4 against 16.6).  Tiles of 256 by 256, one to a compute unit, where there are many long ones
   // (262144 rows, 2048 -> 2048: 1189 us against 1456 in tiles of 128 by 128, 1024 -> 1024 345 against 378; 512 -> 512 120 against 110).  y past the
-  // caches: 262144 rows, 256 -> 1024 157 us, else 207.
+  // caches where it is longer than 128 MB, half of the last-level cache (256 -> 1024, bfloat16, past them and through them: 256 MB 83 us and 107, 512 MB 161
+  // and 213; 96 MB 31.5 and 33.3, but 65 and 62 with the next reader of y).
   const bool direct = (((uintptr_t)x | (uintptr_t)w | (uintptr_t)k | (uintptr_t)x_stride) & 15u) == 0;
   auto grid = [&](int64_t bm, int64_t bn, int64_t threads) {         // false: more workgroups than a launch holds
     const int64_t row_tiles = std::min<int64_t>((n + bm - 1) / bm + groups, n), col_tiles = (m + bn - 1) / bn;
