@@ -151,8 +151,10 @@ __device__ __forceinline__ bytes16 load_bytes(const int8_t* p, int t, int depth,
 //   else by way of registers, which takes any address and cuts what lies behind the depth.
 // Tiles of 128 by 128 have four workgroups to a compute unit, which hide each other's trips to memory (two stages of 64 bytes: 65536 rows,
 // 1024 -> 1024 97 us; three stages and three workgroups 101; tiles of 128 by 256, whose wavefronts read a quarter less from LDS, and two workgroups
-// 103).  Many tiles of long depths come near the library's rate: 262144 rows, 64 -> 1024 and 1024 -> 1024 differ by the time of 1930 TOP/s, the
-// library's 8192 x 8192 x 8192 product has 2040 to 2310; what is left is the time before a tile's first and behind its last product.
+// 103).  Many tiles of long depths (256 by 256, one workgroup to a compute unit): 262144 rows of rounded normal numbers, 1024 -> 1024 360 us and 2048 -> 1024 616,
+// so that the sums are made at 2140 TOP/s, near the library's rate on such numbers (8192 x 8192 x 8192 2150, with one side transposed 2520), and some 100 us go
+// to what nothing of a workgroup's own overlaps: its first loads and its results, 512 MB in all.  The cycles are those of zeros, matrix cores and vector instructions
+// busy a third of them each and wavefronts waiting for a third; the clock is not: 2.1 GHz, on zeros 2.4 (316 us).
 template <int BM, int BN, int D>
 struct QuantizedTile {
   static constexpr int WAVES = BM / 32, FR = 2, FC = BN / 64, kRows = BM + BN;

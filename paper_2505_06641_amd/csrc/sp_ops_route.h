@@ -273,10 +273,13 @@ __device__ __forceinline__ void sort_keys(const uint32_t (&key)[N], uint32_t (&l
 //   Each lane sorts its keys, and a round pops the largest of the lanes' first ones; where a lane may have more than nine to give
 //   (teams of 64), a round takes the largest key below the one before, of differences in 32 bits the largest.  A row is settled where all of its
 //   chosen keys and the next one are further apart than the errors can be, or where those that are not prove to be in order when they are compared in
-//   64 bits; groups that are close leave it open.  Rows left open, rows that end early and rows with logits that are no numbers are few (of 256 experts
-//   some 3 in 10000); each wavefront takes its own in 64 bits when it is through, some 6 us a row.
-// Bound by vector instructions in teams of 8 (262144 rows of 256 float32: by logits 59 us, 4.9 TB/s; sigmoid and bias 97, with 4 of 8 groups 121; a
-// wavefront to a row in 64 bits 640), whose lanes share what a row costs besides its experts: teams of 16 took 73, 108 and 137.
+//   64 bits; groups that are close leave it open.  Rows left open, rows that end early and rows with logits that are no numbers go to 64 bits: each wavefront
+//   takes its own when it is through, some 6 us a row.  Of drawn scores of 256 experts some 3 rows in 10000 do, but all rows that have fewer experts than
+//   `top`, and all whose float32 logits tie at the cut: 262144 rows of 256 that are equal 650 us, 262144 of 8 experts of which 8 are asked for 21 us, and 197
+//   where 5% of the logits are -inf.
+// Bound by vector instructions in teams of 8 (262144 rows of 256, 8 chosen, float32 and bfloat16: by logits 62 us and 61, 4.6 and 2.4 TB/s; sigmoid and bias 100
+// and 100, with 4 of 8 groups 120 and 108; a wavefront to a row in 64 bits 640), whose lanes share what a row costs besides its experts: teams of 16 took 73, 108
+// and 137 of float32.
 template <typename T, int TEAM, int PER, bool BY_LOGIT>
 __global__ __launch_bounds__(256, TEAM == 64 ? 2 : PER == 32 && !BY_LOGIT ? 3 : 4) void k_route(RouteArgs a) {
   constexpr int ROWS = 64 / TEAM, BITS = TEAM < 64 ? 8 : 10, LAST = (1 << BITS) - 1, FIELD = 31 - BITS;
