@@ -298,7 +298,7 @@ sp_status sp_grouped_linear_quantized(sp_ops* o, int32_t n, int32_t k, int32_t m
   // Pieces of 16 rows while the device holds about all of their workgroups and each is through its depth soon (256 rows, 1024 -> 1024: 7.2 us
   // against 11.4 in tiles; 1024 rows, 1024 -> 512 11.1 against 10.5, 256 rows, 2048 -> 2048 20.9 against 16.0; addresses that are no multiples of 16 cost
   // them more: 256 rows of 32 groups, 1023 -> 515 21.4 against 16.6).  Tiles of 256 by 256, one to a compute unit, where there are many long ones
-  // (262144 rows, 2048 -> 2048: 1189 us against 1456 in tiles of 128 by 128, 1024 -> 1024 345 against 378; 512 -> 512 120 against 110).  y past the
+  // (262144 rows, 2048 -> 2048: 1220 us against 1510 in tiles of 128 by 128, 1024 -> 1024 362 against 412; 512 -> 512 127 against 122).  y past the
   // caches where it is longer than 128 MB, half of the last-level cache (256 -> 1024, bfloat16, past them and through them: 256 MB 83 us and 107, 512 MB 161
   // and 213; 96 MB 31.5 and 33.3, but 65 and 62 with the next reader of y).
   const bool direct = (((uintptr_t)x | (uintptr_t)w | (uintptr_t)k | (uintptr_t)x_stride) & 15u) == 0;

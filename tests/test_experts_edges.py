@@ -42,6 +42,42 @@ def test_grouped_linear_quantized_of_rows_far_from_one(gpu, ops, n, k, m, groups
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("n,k,m", [(40, 64, 70), (2100, 1024, 1000), (2100, 1019, 1000)])
+def test_grouped_linear_quantized_of_rows_as_far_apart_as_may_be(gpu, ops, n, k, m):
+    torch, _ = gpu
+    far = 8388608                                          # SP_MAX_LINEAR_STRIDE; 128 rows of it pass 2^30 bytes, all of them 2^32
+    g = torch.Generator(device=DEV).manual_seed(n + k)
+    x = torch.zeros((n - 1) * far + k, dtype=torch.int8, device=DEV).as_strided((n, k), (far, 1))
+    x.copy_(torch.randint(-127, 128, (n, k), dtype=torch.int8, device=DEV, generator=g))
+    w = torch.randint(-127, 128, (2, m, k), dtype=torch.int8, device=DEV, generator=g)
+    xs, ws = torch.rand(n, device=DEV, generator=g) + 0.01, torch.rand(2, m, device=DEV, generator=g) + 0.01
+    offsets = torch.tensor([0, n // 3, n], dtype=torch.int32, device=DEV)
+    y = torch.full((n, m), math.nan, device=DEV)
+    ops.sp_grouped_linear_quantized(x, xs, offsets, w, ws, y)
+    want, bound = quantized_layer(torch, x.contiguous(), xs, offsets, w, ws, None, False, None)
+    assert_within(torch, y, want, bound + U * (want.abs() + bound), "y")
+    del x
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n", [33, 3000])
+def test_grouped_linear_quantized_of_weights_beyond_32_bits(gpu, ops, n):
+    torch, _ = gpu
+    groups, m, k = 66, 8192, 8192                          # 4.4e9 weights
+    g = torch.Generator(device=DEV).manual_seed(n)
+    w = torch.randint(-127, 128, (groups, m, k), dtype=torch.int8, device=DEV, generator=g)
+    x = torch.randint(-127, 128, (n, k), dtype=torch.int8, device=DEV, generator=g)
+    xs, ws = torch.rand(n, device=DEV, generator=g) + 0.01, torch.rand(groups, m, device=DEV, generator=g) + 0.01
+    ends = torch.zeros(groups + 1, dtype=torch.int32, device=DEV)
+    ends[32:], ends[64:], ends[65:], ends[66] = n // 4, n // 3, n // 2, n
+    y = torch.full((n, m), math.nan, device=DEV)
+    ops.sp_grouped_linear_quantized(x, xs, ends, w, ws, y)
+    want, bound = quantized_layer(torch, x, xs, ends, w, ws, None, False, None)
+    assert_within(torch, y, want, bound + U * (want.abs() + bound), "y")
+    del w
+    torch.cuda.empty_cache()
+
+
 # ---------------------------------------------------------------- many rows
 
 def routed(torch, z, top, sigmoid, bias, groups, top_groups):
